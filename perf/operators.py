@@ -423,7 +423,7 @@ def _route_exact(c, s):
     if c["train"]:
         g = torch.where(there, s["dweights"].double(), 0.0) * c["scale"]
         if c["renorm"]:
-            g = torch.where(S > 0, (g - (g * share).sum(1, keepdim=True)) / S, 0.0)
+            g = torch.where(there & (S > 0), (g - (g * share).sum(1, keepdim=True)) / S, 0.0)
         full = torch.zeros(T, E, dtype=torch.float64, device="cuda").scatter_add_(1, idx, g)
         if c["score"] == "softmax":
             out["dlogits"] = score * (full - (full * score).sum(1, keepdim=True))
