@@ -6,7 +6,8 @@ import subprocess
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB_PATH = os.path.join(HERE, "libskewadam.so")
-SOURCES = ["skew_kernels.hip", "skew_plan.cpp", "skew_api.cpp"]
+SOURCES = ["skew_kernels.hip", "skew_plan.cpp", "skew_api.cpp", "moe_route.hip", "moe_order.hip", "moe_tokens.hip",
+           "moe_product.hip", "moe_api.cpp"]
 
 
 def hipcc() -> str:
@@ -18,7 +19,7 @@ def hipcc() -> str:
 
 def build(verbose: bool = False) -> str:
     cmd = [hipcc(), "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
-           "-ffp-contract=off", "-Wall",
+           "-ffp-contract=off", "-Wall", "-parallel-jobs=8",
            # packed fp32 instructions are kept out of the device code
            "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
            "-o", LIB_PATH + ".tmp"] + [os.path.join(CSRC, s) for s in SOURCES]
