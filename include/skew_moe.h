@@ -7,7 +7,7 @@
  * (E, n, m) expert tensors and their inputs, of the embedding table).
  *
  * Conventions are those of skewadam.h: status codes, caller-owned device buffers, hipStream_t
- * as void*. Every call is stream-ordered, launches nothing when it refuses its arguments,
+ * as void*. Rows have 1 to SKEW_MAX_COLS columns. Every call is stream-ordered, launches nothing when it refuses its arguments,
  * allocates nothing, never synchronises, and can be captured in a HIP graph. Results are the
  * same bits on every run (no atomic adds of floats). Sums are float32; a result in bf16 is
  * rounded once. Row strides (ld*) are in elements. Pointers may have any alignment that their
@@ -28,6 +28,7 @@ enum { SKEW_SCORE_SOFTMAX = 0, SKEW_SCORE_SIGMOID = 1 };
 #define SKEW_MAX_EXPERTS 1024
 #define SKEW_MAX_CHOICES 16
 #define SKEW_MAX_GROUPS 64
+#define SKEW_MAX_COLS 16777216
 
 /* How tokens choose experts. For a token's logits l_0 .. l_{E-1}:
  *   scores   s = softmax(l), or s_j = 1 / (1 + exp(-l_j)).
@@ -133,8 +134,9 @@ int skew_expert_combine_backward(const skew_rows *r, const void *dout, int64_t l
  * [0, vocab) is no token: its row of `out` is zero and it adds nothing to the gradient.
  *   skew_embed       out[t] = scale * table[id_t]
  *   skew_embed_grad  dtable[v] = scale * sum of dout[t] over the t with id_t = v, every row of it
- *                    written (zero where no token has the id); each row's sum runs over the
- *                    tokens in order, in runs of 64 that are then added.
+ *                    written (zero where no token has the id); a row's tokens are added in
+ *                    order, in runs that end at multiples of 32 places of all
+ *                    tokens sorted by id, and then the runs.
  * table, out, dout and dtable share `dtype`; rows of `cols` at strides ld*. tokens < 2^31,
  * vocab < 2^31. Errors: SKEW_EINVAL, SKEW_ENOSPACE, SKEW_EHIP. */
 int skew_embed(const void *ids, int32_t id_bytes, int64_t tokens, const void *table, int64_t vocab, int64_t cols,

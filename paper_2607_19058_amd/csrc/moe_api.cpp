@@ -10,7 +10,7 @@ using namespace moe;
 namespace {
 
 constexpr int64_t kMaxPlaces = 0x7FFFFFFF;   // pairs and ids have 32-bit indices
-constexpr int64_t kMaxCols = 1 << 26;        // columns of a row
+constexpr int64_t kMaxCols = 1 << 24;        // columns of a row
 constexpr int64_t kMaxSpan = (int64_t)1 << 59;   // elements that a strided tensor may span
 
 int status(int hip_error) { return hip_error == (int)hipSuccess ? SKEW_OK : SKEW_EHIP; }

@@ -9,8 +9,6 @@
 namespace moe {
 
 constexpr int kMaxDigit = 9;             // radix digits of the sort: up to 512 bins
-constexpr int64_t kSmallSort = 16384;    // items that one work-group sorts in LDS
-constexpr int kSortBlock = 4096;         // items per work-group of the larger sort
 
 // Number of bits that hold 0 .. x.
 inline int bits_for(uint64_t x) {
@@ -25,8 +23,9 @@ struct SortPlan {
   int64_t n = 0;
   uint32_t keys = 0;
   int passes = 0, digit = 0;     // radix passes of `digit` bits
-  bool small = false;            // one work-group
-  int64_t nb = 0;                // work-groups of the larger sort
+  bool one = false;              // one work-group
+  int steps = 1;                 // items of a thread in the larger sort
+  int64_t nb = 0;                // its work-groups
   size_t off_key[2] = {0, 0}, off_idx[2] = {0, 0}, off_hist = 0, off_total = 0, bytes = 0;
 };
 SortPlan sort_plan(int64_t n, int64_t keys);
@@ -137,6 +136,31 @@ __device__ __forceinline__ void store8(float *p, int64_t n, const float *v) {
   } else {
 #pragma unroll
     for (int i = 0; i < 8; i++)
+      if (i < n) p[i] = v[i];
+  }
+}
+
+// One 16-byte access: kVec neighbouring values; n < kVec: only the first n exist.
+template <class T>
+constexpr int kVec = 16 / sizeof(T);
+__device__ __forceinline__ void load_vec(const bf16_t *p, int64_t n, float *o) { load8(p, n, o); }
+__device__ __forceinline__ void store_vec(bf16_t *p, int64_t n, const float *v) { store8(p, n, v); }
+__device__ __forceinline__ void load_vec(const float *p, int64_t n, float *o) {
+  if (n >= 4) {
+    const f32x4 a = *reinterpret_cast<const f32x4_a4 *>(p);
+#pragma unroll
+    for (int i = 0; i < 4; i++) o[i] = a[i];
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; i++) o[i] = i < n ? p[i] : 0.0f;
+  }
+}
+__device__ __forceinline__ void store_vec(float *p, int64_t n, const float *v) {
+  if (n >= 4) {
+    *reinterpret_cast<f32x4_a4 *>(p) = f32x4{v[0], v[1], v[2], v[3]};
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; i++)
       if (i < n) p[i] = v[i];
   }
 }

@@ -11,8 +11,6 @@
 // their row, so that the lanes of one LDS access fall into different banks.
 // The matrix instruction is called with W's side first: a lane then holds 4 neighbouring columns of
 // one result row, which it stores together.
-#include <stdlib.h>
-
 #include <type_traits>
 
 #include "moe_internal.h"
@@ -35,18 +33,21 @@ struct ProductArgs {
   int64_t n, m, places;           // n x m weights
   int32_t k, experts, gather, f32;
   int32_t direct;                 // 16-byte rows in both operands and lengths that are multiples of 8
-  int32_t wide;                   // 4 neighbouring results can be stored together
+  int32_t wide, chunks;           // 4 neighbouring results can be stored together; 8, and none of them is past the edge
   int64_t row_tiles;              // forward, backward: tiles of rows in the grid
 };
 
-constexpr int kBK = 32;   // contraction length of a stage: one matrix instruction's
+constexpr int kBK = 32;   // contraction length of a step: one matrix instruction's
 
 // ---- LDS tiles ------------------------------------------------------------------------------
-// Contiguous in the contraction: rows of kBK values, 4 chunks of 8, so 4 rows are as long as the banks. A 16-byte
-// read takes two cycles of 16 lanes each: rows 0-3 and 12-15 at one chunk with rows 4-11 at the next one, and the other way
-// about. With the rows' groups of 4 xor-ed by 0, 2, 3, 1 these fall into different banks (0, 1, 2, 3: a third of the reads' cycles
-// were conflicts).
-__device__ __forceinline__ int swizzle_k(int row) { return (((row >> 2) ^ (row >> 3)) & 1) << 1 | ((row >> 3) & 1); }
+// Contiguous in the contraction: rows of KS steps of kBK values, 4 KS chunks of 8. A 16-byte read takes two
+// cycles of 16 lanes each: rows 0-3 and 12-15 at one chunk with rows 4-11 at the next one, and the other way about.
+// KS = 1: 4 rows are as long as the banks; with the rows' groups of 4 xor-ed by 0, 2, 3, 1 the lanes fall into different banks
+// (with 0, 1, 2, 3 a third of the reads' cycles were conflicts). KS = 2: 2 rows are, and the row does it.
+template <int KS>
+__device__ __forceinline__ int swizzle_k(int row) {
+  return KS == 1 ? (((row >> 2) ^ (row >> 3)) & 1) << 1 | ((row >> 3) & 1) : row & 7;
+}
 // Contiguous along the result: kBK rows of W values (W / 8 chunks). A transposing read takes two
 // neighbouring chunks of 4 rows in each of 4 lane groups, which are 8 rows apart.
 template <int W>
@@ -66,17 +67,22 @@ __device__ __forceinline__ const __attribute__((address_space(3))) V *lds_at(uin
 // A wave's fragments: 8 neighbours along the contraction (8 (lane / 16) .. + 7) of each of 16 result rows (lane % 16).
 // get(buf, i): rows r0 + 16 i .. of the buffer `buf` bytes on. Contiguous in the contraction: fragments are a
 // constant apart, as the xor takes bits of the row below 16.
-template <int B>
+template <int KS>
 struct FragK {
-  uint32_t at;
+  uint32_t at[KS];
   __device__ __forceinline__ FragK(const u32x4 *tile, int r0) {
     const int lane = threadIdx.x & 63, row = lane & 15;
-    at = lds_offset(tile) + (r0 + row) * 64 + ((lane >> 4) ^ swizzle_k(row)) * 16;
+#pragma unroll
+    for (int k = 0; k < KS; k++)
+      at[k] = lds_offset(tile) + (r0 + row) * (64 * KS) + ((k * 4 + (lane >> 4)) ^ swizzle_k<KS>(row)) * 16;
   }
-  __device__ __forceinline__ bf16x8 get(uint32_t buf, int i) const {
-    return __builtin_bit_cast(bf16x8, *lds_at<u32x4>(at + buf + i * 1024));
+  __device__ __forceinline__ bf16x8 get(int step, int i) const {
+    return __builtin_bit_cast(bf16x8, *lds_at<u32x4>(at[step] + i * 1024 * KS));
   }
-  __device__ __forceinline__ void move(int32_t bytes) { at += bytes; }
+  __device__ __forceinline__ void move(int32_t bytes) {
+#pragma unroll
+    for (int k = 0; k < KS; k++) at[k] += bytes;
+  }
 };
 // Contiguous along the result: fragments are 16 columns apart, which the xor mixes with the row.
 template <int B, int F>
@@ -89,13 +95,13 @@ struct FragT {
     for (int f = 0; f < F; f++)
       at[f] = lds_offset(tile) + row * (B * 2) + ((chunk + 2 * f) ^ swizzle_t<B>(row)) * 16 + (i & 1) * 8;
   }
-  __device__ __forceinline__ bf16x8 get(uint32_t buf, int f) const {
+  __device__ __forceinline__ bf16x8 get(int step, int f) const {
     typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
     struct {
       s16x4 lo, hi;   // rows row .. + 3 and, with the same xor, row + 4 .. + 7
     } v;
-    v.lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(uintptr_t)(at[f] + buf));
-    v.hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(uintptr_t)(at[f] + buf + 4 * B * 2));
+    v.lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(uintptr_t)(at[f] + step * kBK * B * 2));
+    v.hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(uintptr_t)(at[f] + (step * kBK + 4) * B * 2));
     return __builtin_bit_cast(bf16x8, v);
   }
   __device__ __forceinline__ void move(int32_t bytes) {
@@ -180,7 +186,9 @@ __device__ __forceinline__ bool find_tile(const ProductArgs &a, int64_t tile, in
 // Written out because the compiler, which cannot tell the stage buffers apart, would wait for these loads
 // before every LDS read. It does not count them either: every use of the data comes after vm_wait() and a barrier.
 __device__ __forceinline__ void load_lds(const char *base, uint32_t offset, uint32_t to) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(offset), "s"(base) : "memory");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(__builtin_amdgcn_readfirstlane(to)),
+               "v"(offset), "s"(base)
+               : "memory");
 }
 // waits until at most N of this wave's loads are on their way
 template <int N>
@@ -230,58 +238,83 @@ struct Tile {
   int expert, K;
   int64_t r0, r1, c0, c1, first;
 };
-template <int MODE, int B>
+template <int MODE, int BM, int BN>
 __device__ __forceinline__ bool take_tile(const ProductArgs &a, Tile *t) {
   int64_t tr, tc;
   t->first = 0;
   if (MODE == kWeights) {
-    const int64_t tn = (a.n + B - 1) / B, tm = (a.m + B - 1) / B;
+    const int64_t tn = (a.n + BM - 1) / BM, tm = (a.m + BN - 1) / BN;
     if (!patch_tile(a.experts * tn, tm, &tr, &tc)) return false;
     t->expert = (int)(tr / tn);
-    t->r0 = tr % tn * B;
+    t->r0 = tr % tn * BM;
     t->r1 = a.n;
     t->c1 = a.m;
     t->first = a.offsets[t->expert];
     t->K = __builtin_amdgcn_readfirstlane(a.offsets[t->expert + 1] - (int)t->first);
   } else {
     t->c1 = MODE == kForward ? a.m : a.n;
-    if (!patch_tile(a.row_tiles, (t->c1 + B - 1) / B, &tr, &tc) || !find_tile<B>(a, tr, &t->expert, &t->r0, &t->r1)) return false;
+    if (!patch_tile(a.row_tiles, (t->c1 + BN - 1) / BN, &tr, &tc) || !find_tile<BM>(a, tr, &t->expert, &t->r0, &t->r1)) return false;
     t->expert = __builtin_amdgcn_readfirstlane(t->expert);   // the same in every lane, but found in a loop over lanes
     t->r0 = scalar(t->r0);
     t->r1 = scalar(t->r1);
     t->K = t->expert < a.experts ? (int)(MODE == kForward ? a.n : a.m) : 0;   // the places without a pair: zeros
   }
-  t->c0 = tc * B;
+  t->c0 = tc * BN;
   return true;
 }
 
-// Stores a wave's F x F blocks of 16 x 16 results from row wr and column wc of the tile. A lane holds row
+// Stores a wave's FM x FN blocks of 16 x 16 results from row wr and column wc of the tile. A lane holds row
 // lane % 16 of each block and its columns 4 (lane / 16) .. + 3.
-template <int MODE, int F>
-__device__ __forceinline__ void store_tile(const ProductArgs &a, const Tile &t, int wr, int wc, const f32x4 (&acc)[F][F]) {
+// bf16 results go through `room` (FM FN 512 bytes of LDS of this wave's own), so that a row's 32 FN bytes leave
+// together: 8-byte stores of 16 rows at once reached 3.1 TB/s on a gradient that is all output.
+template <int MODE, int FM, int FN>
+__device__ __forceinline__ void store_tile(const ProductArgs &a, const Tile &t, int wr, int wc, const f32x4 (&acc)[FM][FN],
+                                           char *room) {
   const int lane = threadIdx.x & 63;
   const int64_t row0 = t.r0 + wr + (lane & 15), col0 = t.c0 + wc + (lane >> 4) * 4;
-  float s[F];
+  float s[FM];
 #pragma unroll
-  for (int i = 0; i < F; i++) s[i] = 1.0f;
+  for (int i = 0; i < FM; i++) s[i] = 1.0f;
   if (MODE != kWeights && a.scale && t.expert < a.experts) {
 #pragma unroll
-    for (int i = 0; i < F; i++)
+    for (int i = 0; i < FM; i++)
       if (row0 + i * 16 < t.r1) s[i] = a.scale[a.rows[row0 + i * 16]];
   }
   const int64_t at = (MODE == kWeights ? (int64_t)t.expert * a.slice : 0) + row0 * a.ldy + col0;
-  if (a.wide && t.c0 + 32 * F <= t.c1) {   // every column exists
+  if (room && a.chunks && !a.f32) {
+    constexpr int kChunks = 2 * FN;   // of a row, placed with their index xor-ed with the row
 #pragma unroll
-    for (int i = 0; i < F; i++) {
+    for (int i = 0; i < FM; i++)
+#pragma unroll
+      for (int j = 0; j < FN; j++) {
+        const int row = i * 16 + (lane & 15), c = 2 * j + (lane >> 5);
+        const f32x4 v = s[i] * acc[i][j];
+        *reinterpret_cast<uint2 *>(room + row * (kChunks * 16) + (c ^ (row & 7)) * 16 + (lane >> 4 & 1) * 8) =
+            make_uint2(pack2(v[0], v[1]), pack2(v[2], v[3]));
+      }
+    __builtin_amdgcn_wave_barrier();
+    const int64_t out = (MODE == kWeights ? (int64_t)t.expert * a.slice : 0);
+#pragma unroll
+    for (int n = 0; n < FM * FN / 2; n++) {
+      const int q = n * 64 + lane, row = q / kChunks, c = q % kChunks;
+      const u32x4 v = *reinterpret_cast<const u32x4 *>(room + row * (kChunks * 16) + (c ^ (row & 7)) * 16);
+      const int64_t r = t.r0 + wr + row, col = t.c0 + wc + c * 8;
+      if (r < t.r1 && col < t.c1) *reinterpret_cast<u32x4 *>(static_cast<bf16_t *>(a.y) + out + r * a.ldy + col) = v;
+    }
+    return;
+  }
+  if (a.wide && t.c0 + 32 * FN <= t.c1) {   // every column exists
+#pragma unroll
+    for (int i = 0; i < FM; i++) {
       if (row0 + i * 16 >= t.r1) break;
       if (a.f32) {
         float *y = static_cast<float *>(a.y) + at + i * 16 * a.ldy;
 #pragma unroll
-        for (int j = 0; j < F; j++) *reinterpret_cast<f32x4 *>(y + j * 16) = s[i] * acc[i][j];
+        for (int j = 0; j < FN; j++) *reinterpret_cast<f32x4 *>(y + j * 16) = s[i] * acc[i][j];
       } else {
         bf16_t *y = static_cast<bf16_t *>(a.y) + at + i * 16 * a.ldy;
 #pragma unroll
-        for (int j = 0; j < F; j++) {
+        for (int j = 0; j < FN; j++) {
           const f32x4 v = s[i] * acc[i][j];
           *reinterpret_cast<uint2 *>(y + j * 16) = make_uint2(pack2(v[0], v[1]), pack2(v[2], v[3]));
         }
@@ -290,49 +323,50 @@ __device__ __forceinline__ void store_tile(const ProductArgs &a, const Tile &t, 
     return;
   }
 #pragma unroll
-  for (int i = 0; i < F; i++) {
+  for (int i = 0; i < FM; i++) {
     if (row0 + i * 16 >= t.r1) break;
 #pragma unroll
-    for (int j = 0; j < F; j++) store4(a, at + i * 16 * a.ldy + j * 16, t.c1 - col0 - j * 16, s[i] * acc[i][j]);
+    for (int j = 0; j < FN; j++) store4(a, at + i * 16 * a.ldy + j * 16, t.c1 - col0 - j * 16, s[i] * acc[i][j]);
   }
 }
 
 // ---- tiles whose chunks go from memory to LDS without registers ---------------------------------
 // For rows at 16-byte positions and lengths that are multiples of 8, so that a chunk is inside its row or outside.
-// Tiles of 32 F x 32 F results, 4 waves, each F x F matrix instructions a stage; kStages LDS buffers of a stage.
-// While a wave multiplies stage s from registers it reads stage s + 1 from LDS into other registers and sends for
-// stage s + kAhead, in F steps of one load, one fragment of each side and F matrix instructions. A load's address
-// is a scalar, which moves from stage to stage, plus a lane's 32-bit offset, which stays.
+// Tiles of 32 FM x 32 FN results, 4 waves, each FM x FN matrix instructions a stage; NS LDS buffers of a stage.
+// A stage is KS steps. While a wave multiplies one step from registers it reads the next one from LDS into other registers
+// and sends for a stage further on, one load or fragment after every few matrix instructions. A load's address is a
+// scalar, which moves from stage to stage, plus a lane's 32-bit offset, which stays.
 // Rows and columns past the edge of the result repeat the last one inside and are not stored; past the end of the
 // contraction both operands are zero, so nothing there meets a NaN.
-constexpr int kList = 2048;   // places whose rows kWeights looks up at once
+constexpr int kList = 1024;   // places whose rows kWeights looks up at once
 
-template <int MODE, int F>
-__global__ __launch_bounds__(256, F == 8 ? 1 : 2) void tile_kernel(ProductArgs a) {
-  constexpr int B = 32 * F, kThreads = 256;
-  constexpr int kC = B * kBK / 8, kP = kC / kThreads;   // chunks of a stage's tile, and of a thread in it
-  constexpr int kBytes = kC * 16;
-  static_assert(2 * kP == F, "one load a step");
-  // LDS buffers of a stage: all that fit at F = 8 (160 KiB, and kWeights' list), 64 KiB at F = 4 for two work-groups
-  constexpr int kStages = F == 8 && MODE != kWeights ? 5 : 4, kAhead = kStages - 1;
-  __shared__ u32x4 lds[2 * kStages * kC + (MODE == kWeights ? kList / 4 : 0)];
-  u32x4 *const ta = lds, *const tb = lds + kStages * kC;
-  uint32_t *const list = reinterpret_cast<uint32_t *>(tb + kStages * kC);   // byte offsets of x's rows
+template <int MODE, int FM, int FN, int NS, int KS>
+__global__ __launch_bounds__(256, FM * FN * KS >= 64 ? 1 : FM * FN == 8 ? 3 : 2) void tile_kernel(ProductArgs a) {
+  constexpr int BM = 32 * FM, BN = 32 * FN, BK = KS * kBK, kThreads = 256;
+  constexpr int kCA = BM * BK / 8, kCB = BN * BK / 8, kPA = kCA / kThreads, kPB = kCB / kThreads;   // chunks of a stage
+  constexpr int kBytesA = kCA * 16, kBytesB = kCB * 16, kLoads = kPA + kPB;
+  constexpr bool kInA = FM * FN == 64;
+  constexpr int kAhead = KS == 1 ? NS - 1 : NS;   // a stage of two steps is sent for when its buffer's second step was read
+  static_assert(FM * FN * 512 * 4 <= NS * (kBytesA + kBytesB), "room for the results");
+  static_assert(kPA * kThreads == kCA && kPB * kThreads == kCB, "whole chunks per thread");
+  __shared__ u32x4 lds[NS * (kCA + kCB) + (MODE == kWeights ? kList / 4 : 0)];
+  u32x4 *const ta = lds, *const tb = lds + NS * kCA;
+  uint32_t *const list = reinterpret_cast<uint32_t *>(tb + NS * kCB);   // byte offsets of x's rows
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int wr = (wave >> 1) * (B / 2), wc = (wave & 1) * (B / 2);
+  const int wr = (wave >> 1) * (BM / 2), wc = (wave & 1) * (BN / 2);
   Tile t;
-  if (!take_tile<MODE, B>(a, &t)) return;
+  if (!take_tile<MODE, BM, BN>(a, &t)) return;
   const int K = t.K;
 
-  f32x4 acc[F][F];
+  f32x4 acc[FM][FN];
 #pragma unroll
-  for (int i = 0; i < F; i++)
+  for (int i = 0; i < FM; i++)
 #pragma unroll
-    for (int j = 0; j < F; j++) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int j = 0; j < FN; j++) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 
   // Slot i of this thread is chunk q = tid + i kThreads of a stage's tile in LDS. A tile that is contiguous in the
-  // contraction holds result row q / 4 and chunk (q % 4) ^ swizzle there; one that is not holds contraction row
-  // q / (B / 8) likewise. ka, kb: the slot's contraction index in its stage; oa, ob: its byte offset from xa, xb, where
+  // contraction holds result row q / (4 KS) and chunk (q % (4 KS)) ^ swizzle there; one that is not holds contraction row
+  // q / (tile width / 8) likewise. ka, kb: the slot's contraction index in its stage; oa, ob: its byte offset from xa, xb, where
   // the next stage that is sent for begins (kWeights: oa without the row of x).
   const char *xa = reinterpret_cast<const char *>(a.x), *xb = reinterpret_cast<const char *>(a.w);
   int64_t step_a = 0, step_b;
@@ -341,111 +375,132 @@ __global__ __launch_bounds__(256, F == 8 ? 1 : 2) void tile_kernel(ProductArgs a
   } else {
     xb += 2 * (int64_t)(K ? t.expert : 0) * a.slice;
     if (!a.gather) xa += 2 * t.r0 * a.ldx;
-    step_a = 2 * kBK;
+    step_a = 2 * BK;
   }
-  step_b = MODE == kBackward ? 2 * kBK : 2 * kBK * a.ldw;
+  step_b = MODE == kBackward ? 2 * BK : 2 * BK * a.ldw;
   if (MODE == kBackward) xb += 2 * t.c0 * a.ldw;
   xa = scalar(xa);
   xb = scalar(xb);
   step_b = scalar(step_b);
-  uint32_t oa[kP], ob[kP];
-  int ka[kP], kb[kP];
+  uint32_t oa[kPA], ob[kPB];
+  int ka[kPA], kb[kPB];
 #pragma unroll
-  for (int i = 0; i < kP; i++) {
+  for (int i = 0; i < kPA; i++) {
     const int q = tid + i * kThreads;
     if (MODE == kWeights) {
-      const int row = q / (B / 8), c = (q % (B / 8)) ^ swizzle_t<B>(row);
+      const int row = q / (BM / 8), c = (q % (BM / 8)) ^ swizzle_t<BM>(row);
       ka[i] = row;
       oa[i] = (uint32_t)(2 * (t.r0 + c * 8 < t.r1 ? t.r0 + c * 8 : t.r1 - 8));
     } else {
-      const int row = q / 4, c = (q % 4) ^ swizzle_k(row);
+      const int row = q / (4 * KS), c = (q % (4 * KS)) ^ swizzle_k<KS>(row);
       const int r = t.r0 + row < t.r1 ? row : (int)(t.r1 - 1 - t.r0);
       ka[i] = c * 8;
       oa[i] = (uint32_t)((K > 0 && a.gather ? (int64_t)(a.rows[t.r0 + r] / a.k) : r) * a.ldx + c * 8) * 2;
     }
+  }
+#pragma unroll
+  for (int i = 0; i < kPB; i++) {
+    const int q = tid + i * kThreads;
     if (MODE == kBackward) {
-      const int row = q / 4, c = (q % 4) ^ swizzle_k(row);
+      const int row = q / (4 * KS), c = (q % (4 * KS)) ^ swizzle_k<KS>(row);
       kb[i] = c * 8;
       ob[i] = (uint32_t)((t.c0 + row < t.c1 ? row : t.c1 - 1 - t.c0) * a.ldw + c * 8) * 2;
     } else {
-      const int row = q / (B / 8), c = (q % (B / 8)) ^ swizzle_t<B>(row);
+      const int row = q / (BN / 8), c = (q % (BN / 8)) ^ swizzle_t<BN>(row);
       kb[i] = row;
       ob[i] = (uint32_t)(row * a.ldw + (t.c0 + c * 8 < t.c1 ? t.c0 + c * 8 : t.c1 - 8)) * 2;
     }
+  }
+  // W's rows in the contraction are a power of two apart in most models, so that tiles at the same place of their rows ask the
+  // same memory channels: the tiles of a row of tiles begin at different stages and go round.
+  int turn = -1, sent_at = 0;
+  if (MODE == kBackward && K % BK == 0 && K > 0) {
+    turn = K / BK;
+    sent_at = __builtin_amdgcn_readfirstlane((int)((t.c0 / BN * 3 + t.expert) % turn));
+    xa += sent_at * step_a;
+    xb += sent_at * step_b;
   }
   const uint32_t la = lds_address(ta + wave * 64), lb = lds_address(tb + wave * 64);
 
   int reading = 0, sending = 0;   // buffers of the stages that are read, and sent for, next
   int base = 0, end = K;   // the contraction [base, end) of this round (kWeights: the places in the list)
-  uint32_t row_next[kP];   // kWeights: the rows of x of the next stage that is sent for
+  uint32_t row_next[kPA];   // kWeights: the rows of x of the next stage that is sent for
   auto look_up = [&](int stage) {
     if (MODE == kWeights) {
 #pragma unroll
-      for (int i = 0; i < kP; i++) row_next[i] = list[(stage * kBK + ka[i]) & (kList - 1)];
+      for (int i = 0; i < kPA; i++) row_next[i] = list[(stage * BK + ka[i]) & (kList - 1)];
     }
   };
   // load i of a stage: the slots of a, then those of b
-  auto send = [&](int i, uint32_t buf) {
-    if (i < kP) load_lds(xa, oa[i] + (MODE == kWeights ? row_next[i] : 0), la + buf + i * kThreads * 16);
-    else load_lds(xb, ob[i - kP], lb + buf + (i - kP) * kThreads * 16);
+  auto send = [&](int i) {
+    if (i < kPA) load_lds(xa, oa[i < kPA ? i : 0] + (MODE == kWeights ? row_next[i < kPA ? i : 0] : 0),
+                          la + sending * kBytesA + i * kThreads * 16);
+    else load_lds(xb, ob[i < kPA ? 0 : i - kPA], lb + sending * kBytesB + (i - kPA) * kThreads * 16);
   };
   auto sent_all = [&]() {
     xa += step_a;
     xb += step_b;
-    sending = sending + 1 == kStages ? 0 : sending + 1;
+    sending = sending + 1 == NS ? 0 : sending + 1;
+    if (MODE == kBackward && ++sent_at == turn) {   // round the end of the contraction
+      xa -= turn * step_a;
+      xb -= turn * step_b;
+      sent_at = 0;
+    }
   };
   // the same for any stage, also one that the contraction ends in
   auto send_stage = [&](int stage) {
-    const uint32_t buf = sending * kBytes;
-    const int left = end - base - stage * kBK;
+    const int left = end - base - stage * BK;
     look_up(stage);
-    if (left >= kBK) {
+    if (left >= BK) {
 #pragma unroll
-      for (int i = 0; i < F; i++) send(i, buf);
+      for (int i = 0; i < kLoads; i++) send(i);
     } else {
 #pragma unroll
-      for (int i = 0; i < F; i++) {
-        const bool is_a = i < kP;
-        const int sl = is_a ? i : i - kP;
-        if ((is_a ? ka[sl] : kb[sl]) < left) send(i, buf);
-        else (is_a ? ta : tb)[sending * kC + tid + sl * kThreads] = u32x4{0, 0, 0, 0};
+      for (int i = 0; i < kLoads; i++) {
+        const bool is_a = i < kPA;
+        const int sl = is_a ? i : i - kPA;
+        if ((is_a ? ka[is_a ? sl : 0] : kb[is_a ? 0 : sl]) < left) send(i);
+        else if (is_a) ta[sending * kCA + tid + sl * kThreads] = u32x4{0, 0, 0, 0};
+        else tb[sending * kCB + tid + sl * kThreads] = u32x4{0, 0, 0, 0};
       }
     }
     sent_all();
   };
 
   // this lane's fragments, in the buffer of the stage that is read next
-  FragK<B> ra_k(ta, wr), rb_k(tb, wc);
-  FragT<B, F> ra_t(ta, wr), rb_t(tb, wc);
-  auto move = [&](int32_t bytes) {
-    if (MODE == kWeights) ra_t.move(bytes);
-    else ra_k.move(bytes);
-    if (MODE == kBackward) rb_k.move(bytes);
-    else rb_t.move(bytes);
-  };
-  bf16x8 fa[2][F], fb[2][F];
-  auto read_a = [&](int i, bf16x8 *d) { d[i] = MODE == kWeights ? ra_t.get(0, i) : ra_k.get(0, i); };
-  auto read_b = [&](int i, bf16x8 *d) { d[i] = MODE == kBackward ? rb_k.get(0, i) : rb_t.get(0, i); };
-  auto after = [&](int buf) { return buf + 1 == kStages ? 0 : buf + 1; };
+  FragK<KS> ra_k(ta, wr), rb_k(tb, wc);
+  FragT<BM, FM> ra_t(ta, wr);
+  FragT<BN, FN> rb_t(tb, wc);
+  bf16x8 fa[2][FM], fb[2][FN];
+  auto read_a = [&](int k, int i, bf16x8 *d) { d[i] = MODE == kWeights ? ra_t.get(k, i) : ra_k.get(k, i); };
+  auto read_b = [&](int k, int i, bf16x8 *d) { d[i] = MODE == kBackward ? rb_k.get(k, i) : rb_t.get(k, i); };
   auto advance = [&]() {
-    move(reading + 1 == kStages ? -(kStages - 1) * kBytes : kBytes);
-    reading = after(reading);
+    const bool wrap = reading + 1 == NS;
+    const int32_t by_a = wrap ? -(NS - 1) * kBytesA : kBytesA, by_b = wrap ? -(NS - 1) * kBytesB : kBytesB;
+    if (MODE == kWeights) ra_t.move(by_a);
+    else ra_k.move(by_a);
+    if (MODE == kBackward) rb_k.move(by_b);
+    else rb_t.move(by_b);
+    reading = wrap ? 0 : reading + 1;
   };
-  // multiply fragments X; NEXT: read the next stage into the others; MORE: send for a stage
-  auto stage = [&](auto X, auto NEXT, auto MORE) {
-    constexpr int x = X, y = 1 - x;
+  // multiply fragments X; NEXT: read step k of the stage that is read next into the others; MORE: send for a
+  // stage. The loads come first.
+  auto step = [&](auto X, auto NEXT, auto MORE, int k) {
+    constexpr int x = X, y = 1 - x, kDo = (MORE ? kLoads : 0) + (NEXT ? FM + FN : 0);
+    auto due = [](int m) { return m >= FM * FN - 2 ? kDo : m * kDo / (FM * FN - 2); };   // how many come before instruction m
 #pragma unroll
-    for (int i = 0; i < F; i++) {
+    for (int m = 0; m < FM * FN; m++) {
+      mfma<kInA>(acc[m / FN][m % FN], fb[x][m % FN], fa[x][m / FN]);
 #pragma unroll
-      for (int j = 0; j < F; j++) {
-        mfma<F == 8>(acc[i][j], fb[x][j], fa[x][i]);
-        if (MORE && j == 0) send(i, sending * kBytes);
-        if (NEXT && j == F / 4) read_a(i, fa[y]);
-        if (NEXT && j == F / 2) read_b(i, fb[y]);
+      for (int d = due(m); d < due(m + 1); d++) {
+        const int r = d - (MORE ? kLoads : 0);
+        if (r < 0) send(d);
+        else if (r < FM) read_a(k, r, fa[y]);
+        else read_b(k, r - FM, fb[y]);
       }
     }
     if (MORE) sent_all();
-    if (NEXT) advance();
+    if (NEXT && k == KS - 1) advance();
   };
   const std::integral_constant<int, 0> even;
   const std::integral_constant<int, 1> odd;
@@ -462,64 +517,87 @@ __global__ __launch_bounds__(256, F == 8 ? 1 : 2) void tile_kernel(ProductArgs a
       }
       __syncthreads();
     }
-    const int S = (end - base + kBK - 1) / kBK;
+    const int S = (end - base + BK - 1) / BK;
     for (int i = 0; i < kAhead && i < S; i++) send_stage(i);
     // of the stages that were sent for, all but `n` have arrived in every wave
     auto meet = [&](bool whole, auto n) {
-      if (whole) vm_wait<n * F>();
-      else vm_wait<0>();   // the last stage may have sent for less than F loads
+      if (whole) vm_wait<n * kLoads>();
+      else vm_wait<0>();   // the last stage may have sent for less than kLoads loads
       __syncthreads();
     };
     const std::integral_constant<int, kAhead - 1> one;    // one stage is there
     const std::integral_constant<int, kAhead - 2> two;
     meet(S > kAhead, one);
 #pragma unroll
-    for (int i = 0; i < F; i++) {
-      read_a(i, fa[0]);
-      read_b(i, fb[0]);
-    }
-    advance();
-    // Before stage s: stage s + 1 is there, and the buffer of stage s + kAhead is no longer read.
+    for (int i = 0; i < FM; i++) read_a(0, i, fa[0]);
+#pragma unroll
+    for (int i = 0; i < FN; i++) read_b(0, i, fb[0]);
+    if (KS == 1) advance();
     int s = 0;
-    look_up(kAhead);
-    for (; s + kAhead + 2 < S; s += 2) {    // sends for stages s + kAhead and s + kAhead + 1, which are whole
-      meet(true, two);
-      stage(even, yes, yes);
-      look_up(s + kAhead + 1);
-      meet(true, two);
-      stage(odd, yes, yes);
-      look_up(s + kAhead + 2);
+    if constexpr (KS == 1) {
+      // Before stage s: stage s + 1 is there, and the buffer of stage s + kAhead is no longer read.
+      look_up(kAhead);
+      for (; s + kAhead + 2 < S; s += 2) {    // sends for stages s + kAhead and s + kAhead + 1, which are whole
+        meet(true, two);
+        step(even, yes, yes, 0);
+        look_up(s + kAhead + 1);
+        meet(true, two);
+        step(odd, yes, yes, 0);
+        look_up(s + kAhead + 2);
+      }
+      for (; s + 1 < S; s += 2) {
+        meet(s + kAhead < S, two);
+        if (s + kAhead < S) send_stage(s + kAhead);
+        step(even, yes, no, 0);
+        meet(s + kAhead + 1 < S, two);
+        if (s + kAhead + 1 < S) send_stage(s + kAhead + 1);
+        step(odd, yes, no, 0);   // at the end of an even number of stages this reads what is not used
+      }
+      if (s < S) step(even, no, no, 0);
+    } else {
+      // Between a stage's steps: stage s + 1 is there, and the buffer of stage s, the one of s + kAhead, is no longer read.
+      auto first_step = [&]() {
+        step(even, yes, no, 1);
+      };
+      for (; s + kAhead + 1 < S; s++) {   // sends for stage s + kAhead, which is whole
+        first_step();
+        meet(true, two);
+        step(odd, yes, yes, 0);
+      }
+      for (; s < S; s++) {
+        first_step();
+        meet(s + kAhead < S, two);
+        if (s + kAhead < S) send_stage(s + kAhead);
+        step(odd, yes, no, 0);   // of the last stage: reads what is not used
+      }
     }
-    for (; s + 1 < S; s += 2) {
-      meet(s + kAhead < S, two);
-      if (s + kAhead < S) send_stage(s + kAhead);
-      stage(even, yes, no);
-      meet(s + kAhead + 1 < S, two);
-      if (s + kAhead + 1 < S) send_stage(s + kAhead + 1);
-      stage(odd, yes, no);   // at the end of an even number of stages this reads what is not used
-    }
-    if (s < S) stage(even, no, no);
     // the next round, if any, starts in the buffer that is sent for next
     while (reading != sending) advance();
     __syncthreads();   // the buffers are no longer read
   }
-  if (F == 8) mfma_done();
-  store_tile<MODE, F>(a, t, wr, wc, acc);
+  if (kInA) mfma_done();
+  store_tile<MODE, FM, FN>(a, t, wr, wc, acc, reinterpret_cast<char *>(lds) + wave * (FM * FN * 512));
 }
 
 // ---- tiles of any shape ---------------------------------------------------------------------
-// The same tiles through registers: chunks are loaded from any position, at the ends of rows element by element,
-// while the stage before is multiplied.
+// The same tiles through registers: the next stage's chunks are loaded from any position while a stage is multiplied. Where
+// the result is at least a tile wide, its last tile is moved back inside (its results are computed twice, from the same
+// numbers in the same order), so that all chunks but those at the end of the contraction are whole; else, and
+// there, chunks are loaded element by element.
 template <int MODE, int F>
 __global__ __launch_bounds__(256, 2) void any_kernel(ProductArgs a) {
   constexpr int B = 32 * F, kThreads = 256;
   constexpr int kC = B * kBK / 8, kP = kC / kThreads, kBytes = kC * 16;
   __shared__ u32x4 ta[2 * kC], tb[2 * kC];
-  const int tid = threadIdx.x, wave = tid >> 6;
+  __shared__ int32_t list[MODE == kWeights ? kList : 1];   // x's rows
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wr = (wave >> 1) * (B / 2), wc = (wave & 1) * (B / 2);
   Tile t;
-  if (!take_tile<MODE, B>(a, &t)) return;
+  if (!take_tile<MODE, B, B>(a, &t)) return;
+  if (t.c0 + B > t.c1 && t.c1 >= B) t.c0 = t.c1 - B;
+  if (MODE == kWeights && t.r0 + B > t.r1 && t.r1 >= B) t.r0 = t.r1 - B;
   const int K = t.K;
+  const bool inside = t.c0 + B <= t.c1 && (MODE != kWeights || t.r0 + B <= t.r1);
 
   f32x4 acc[F][F];
 #pragma unroll
@@ -541,14 +619,14 @@ __global__ __launch_bounds__(256, 2) void any_kernel(ProductArgs a) {
       na[i] = clip(t.r1 - (t.r0 + c * 8));
       pa[i] = a.x + t.r0 + c * 8;
     } else {
-      const int row = q / 4, c = (q % 4) ^ swizzle_k(row);
+      const int row = q / 4, c = (q % 4) ^ swizzle_k<1>(row);
       const int64_t p = t.r0 + row < t.r1 ? t.r0 + row : t.r1 - 1;
       ka[i] = c * 8;
       na[i] = 8;
       pa[i] = a.x + (K > 0 && a.gather ? (int64_t)(a.rows[p] / a.k) : p) * a.ldx + c * 8;
     }
     if (MODE == kBackward) {
-      const int row = q / 4, c = (q % 4) ^ swizzle_k(row);
+      const int row = q / 4, c = (q % 4) ^ swizzle_k<1>(row);
       kb[i] = c * 8;
       nb[i] = 8;
       pb[i] = w + (t.c0 + row < t.c1 ? t.c0 + row : t.c1 - 1) * a.ldw + c * 8;
@@ -561,17 +639,25 @@ __global__ __launch_bounds__(256, 2) void any_kernel(ProductArgs a) {
   }
   const int64_t step_b = MODE == kBackward ? kBK : kBK * a.ldw;
   u32x4 ga[kP], gb[kP];
-  auto load = [&](int k0) {
+  auto load = [&](int k0, int in_list) {   // in_list: k0 from the list's first place on
+    if (inside && k0 + kBK <= K) {
+#pragma unroll
+      for (int i = 0; i < kP; i++) {
+        const bf16_t *p = pa[i] + (MODE == kWeights ? list[in_list + ka[i]] * a.ldx : 0);
+        ga[i] = *reinterpret_cast<const u32x4_a2 *>(p);
+        gb[i] = *reinterpret_cast<const u32x4_a2 *>(pb[i]);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < kP; i++) {
+        const int la = K - k0 - ka[i], lb = K - k0 - kb[i];   // contraction values from this chunk on
+        const bf16_t *p = pa[i] + (MODE == kWeights && la > 0 ? list[in_list + ka[i]] * a.ldx : 0);
+        ga[i] = la > 0 ? load_chunk(p, MODE == kWeights ? na[i] : la) : u32x4{0, 0, 0, 0};
+        gb[i] = lb > 0 ? load_chunk(pb[i], MODE == kBackward ? lb : nb[i]) : u32x4{0, 0, 0, 0};
+      }
+    }
 #pragma unroll
     for (int i = 0; i < kP; i++) {
-      const int la = K - k0 - ka[i], lb = K - k0 - kb[i];   // contraction values from this chunk on
-      const bf16_t *p = pa[i];
-      if (MODE == kWeights && la > 0) {
-        const int64_t place = t.first + k0 + ka[i];
-        p += (a.gather ? (int64_t)(a.rows[place] / a.k) : place) * a.ldx;
-      }
-      ga[i] = la > 0 ? load_chunk(p, MODE == kWeights ? na[i] : la) : u32x4{0, 0, 0, 0};
-      gb[i] = lb > 0 ? load_chunk(pb[i], MODE == kBackward ? lb : nb[i]) : u32x4{0, 0, 0, 0};
       if (MODE != kWeights) pa[i] += kBK;
       pb[i] += step_b;
     }
@@ -583,57 +669,89 @@ __global__ __launch_bounds__(256, 2) void any_kernel(ProductArgs a) {
       tb[buf * kC + tid + i * kThreads] = gb[i];
     }
   };
-  const FragK<B> ra_k(ta, wr), rb_k(tb, wc);
-  const FragT<B, F> ra_t(ta, wr), rb_t(tb, wc);
-  if (K > 0) {
-    load(0);
-    put_stage(0);
-  }
+  FragK<1> ra_k(ta, wr), rb_k(tb, wc);
+  FragT<B, F> ra_t(ta, wr), rb_t(tb, wc);
   int buf = 0;
-  for (int k0 = 0; k0 < K; k0 += kBK) {
-    __syncthreads();
-    const bool more = k0 + kBK < K;
-    if (more) load(k0 + kBK);
-    bf16x8 fa[F], fb[F];
-#pragma unroll
-    for (int i = 0; i < F; i++) {
-      fa[i] = MODE == kWeights ? ra_t.get(buf * kBytes, i) : ra_k.get(buf * kBytes, i);
-      fb[i] = MODE == kBackward ? rb_k.get(buf * kBytes, i) : rb_t.get(buf * kBytes, i);
+  for (int base = 0, end; base < K; base = end) {   // kWeights: rounds of the places in the list
+    end = MODE == kWeights && base + kList < K ? base + kList : K;
+    if (MODE == kWeights) {
+      __syncthreads();
+      for (int i = tid; i < end - base; i += kThreads)
+        list[i] = a.gather ? a.rows[t.first + base + i] / a.k : (int32_t)(t.first + base + i);
+      __syncthreads();
     }
+    load(base, 0);
+    put_stage(buf);
+    for (int k0 = base; k0 < end; k0 += kBK) {
+      __syncthreads();
+      const bool more = k0 + kBK < end;
+      if (more) load(k0 + kBK, k0 + kBK - base);
+      bf16x8 fa[F], fb[F];
 #pragma unroll
-    for (int i = 0; i < F; i++)
+      for (int i = 0; i < F; i++) {
+        fa[i] = MODE == kWeights ? ra_t.get(0, i) : ra_k.get(0, i);
+        fb[i] = MODE == kBackward ? rb_k.get(0, i) : rb_t.get(0, i);
+      }
+      const int32_t across = buf ? -kBytes : kBytes;   // to the other buffer
+      if (MODE == kWeights) ra_t.move(across);
+      else ra_k.move(across);
+      if (MODE == kBackward) rb_k.move(across);
+      else rb_t.move(across);
 #pragma unroll
-      for (int j = 0; j < F; j++)
-        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[j], fa[i], acc[i][j], 0, 0, 0);
-    buf ^= 1;
-    if (more) put_stage(buf);
+      for (int i = 0; i < F; i++)
+#pragma unroll
+        for (int j = 0; j < F; j++)
+          acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[j], fa[i], acc[i][j], 0, 0, 0);
+      buf ^= 1;
+      if (more) put_stage(buf);
+    }
   }
-  store_tile<MODE, F>(a, t, wr, wc, acc);
+  store_tile<MODE, F, F>(a, t, wr, wc, acc, nullptr);
 }
 
-template <int MODE, int F, bool DIRECT>
-int launch(ProductArgs a, void *stream) {
-  constexpr int B = 32 * F;
-  int64_t grid;
-  if (MODE == kWeights) {
-    grid = patch_grid(a.experts * ((a.n + B - 1) / B), (a.m + B - 1) / B);
-  } else {
-    const int64_t cols = MODE == kForward ? a.m : a.n;
-    // an expert (and the places without a pair) ends in at most one tile that is not full
-    a.row_tiles = a.places / B + a.experts + 1 < a.places ? a.places / B + a.experts + 1 : a.places;
-    grid = patch_grid(a.row_tiles, (cols + B - 1) / B);
-  }
+// The grid of a tiled kernel.
+template <int MODE>
+int64_t tiles(ProductArgs &a, int64_t bm, int64_t bn) {
+  if (MODE == kWeights) return patch_grid(a.experts * ((a.n + bm - 1) / bm), (a.m + bn - 1) / bn);
+  // an expert (and the places without a pair) ends in at most one tile that is not full
+  a.row_tiles = a.places / bm + a.experts + 1 < a.places ? a.places / bm + a.experts + 1 : a.places;
+  return patch_grid(a.row_tiles, ((MODE == kForward ? a.m : a.n) + bn - 1) / bn);
+}
+
+template <int MODE, int FM, int FN, int NS, int KS = 1>
+int launch_tile(ProductArgs a, void *stream) {
+  const int64_t grid = tiles<MODE>(a, 32 * FM, 32 * FN);
   if (grid > 0x7FFFFFFF) return (int)hipErrorInvalidConfiguration;
-  hipStream_t s = static_cast<hipStream_t>(stream);
-  if constexpr (DIRECT) tile_kernel<MODE, F><<<(unsigned)grid, 256, 0, s>>>(a);
-  else any_kernel<MODE, F><<<(unsigned)grid, 256, 0, s>>>(a);
+  tile_kernel<MODE, FM, FN, NS, KS><<<(unsigned)grid, 256, 0, static_cast<hipStream_t>(stream)>>>(a);
+  return (int)hipGetLastError();
+}
+template <int MODE, int F>
+int launch_any(ProductArgs a, void *stream) {
+  const int64_t grid = tiles<MODE>(a, 32 * F, 32 * F);
+  if (grid > 0x7FFFFFFF) return (int)hipErrorInvalidConfiguration;
+  any_kernel<MODE, F><<<(unsigned)grid, 256, 0, static_cast<hipStream_t>(stream)>>>(a);
   return (int)hipGetLastError();
 }
 
 template <int MODE>
 int launch_mode(const ProductArgs &a, void *stream) {
-  if (!a.direct) return launch<MODE, 4, false>(a, stream);
-  return getenv("MOE_F4") ? launch<MODE, 4, true>(a, stream) : launch<MODE, 8, true>(a, stream);
+  if (!a.direct) return launch_any<MODE, 4>(a, stream);
+  // By the rows an expert has on average, and so that the chip has tiles. Measured (us) on 32 experts of 2048 x 8192
+  // and 8192 x 2048, rows spread evenly over the experts, at 64 / 128 / 256 wide rows of tiles:
+  //   forward   32 rows 199 / 189 / 259, 128 rows 258 / 199 / 257, 256 rows 418 / 326 / 291, 512 rows 752 / 594 / 515
+  //   backward  32 rows 196 / 204 / 263, 128 rows 251 / 225 / 266, 256 rows 407 / 367 / 290, 512 rows 728 / 671 / 516
+  //   weights   32 rows 430 / 242 / 281, 128 rows 688 / 339 / 402, 256 rows 826 / 523 / 515, 512 rows 1275 / 737 / 709
+  const int64_t rows = a.places / a.experts;
+  auto enough = [&](int64_t bm, int64_t bn) {   // two rounds of work-groups, roughly
+    const int64_t full = MODE == kWeights ? a.experts * ((a.n + bm - 1) / bm) : (a.places + bm - 1) / bm;
+    return full * (((MODE == kBackward ? a.n : a.m) + bn - 1) / bn) >= 512;
+  };
+  if (rows >= (MODE == kForward ? 384 : 256) && enough(256, 256)) return launch_tile<MODE, 8, 8, MODE == kBackward ? 2 : 4, MODE == kBackward ? 2 : 1>(a, stream);
+  if ((rows >= 64 || MODE == kWeights) && enough(128, 256)) return launch_tile<MODE, 4, 8, 3, MODE == kBackward ? 2 : 1>(a, stream);
+  if constexpr (MODE != kWeights) {
+    if (enough(64, 256)) return launch_tile<MODE, 2, 8, MODE == kBackward ? 2 : 4, MODE == kBackward ? 2 : 1>(a, stream);
+  }
+  return launch_tile<MODE, 2, 4, MODE == kBackward ? 2 : 4, MODE == kBackward ? 2 : 1>(a, stream);
 }
 
 ProductArgs args_of(const skew_rows &r, const skew_product_desc &p) {
@@ -672,6 +790,7 @@ int launch_product(const skew_rows &r, const skew_product_desc &p, char *, void 
   a.direct = chunks(a.x, a.ldx) && chunks(a.w, a.ldw) && a.slice % 8 == 0 && a.n % 8 == 0 && a.m % 8 == 0 &&
              short_rows(a.gather ? r.tokens : kMaxTile, a.ldx) && short_rows(kMaxTile, a.ldw);
   a.wide = ((uintptr_t)a.y & 15) == 0 && a.ldy % 4 == 0;
+  a.chunks = a.wide && a.ldy % 8 == 0 && (p.flags & SKEW_TRANSPOSE ? a.n : a.m) % 8 == 0;
   return p.flags & SKEW_TRANSPOSE ? launch_mode<kBackward>(a, stream) : launch_mode<kForward>(a, stream);
 }
 
@@ -685,6 +804,7 @@ int launch_product_grad(const skew_rows &r, const skew_product_desc &p, void *st
   a.direct = chunks(a.x, a.ldx) && chunks(a.w, a.ldw) && a.n % 8 == 0 && a.m % 8 == 0 &&
              short_rows(a.gather ? r.tokens : a.places, a.ldx) && short_rows(kMaxTile, a.ldw);
   a.wide = ((uintptr_t)a.y & 15) == 0 && a.ldy % 4 == 0 && a.slice % 4 == 0;
+  a.chunks = a.wide && a.ldy % 8 == 0 && a.slice % 8 == 0 && a.m % 8 == 0;
   return launch_mode<kWeights>(a, stream);
 }
 

@@ -70,13 +70,16 @@ __device__ __forceinline__ void load_row(const T *p, int n, float *o) {
 }
 
 __device__ __forceinline__ float sigmoid(float l) { return 1.0f / (1.0f + expf(-l)); }
+// For scores that only order the experts: the hardware's exponential and reciprocal, off by some 1e-6 of the score at
+// most, where the weights take the exact ones.
+__device__ __forceinline__ float fast_exp(float x) { return __expf(x); }
+__device__ __forceinline__ float fast_rcp(float x) { return __builtin_amdgcn_rcpf(x); }
 
 template <int L, int V, class T>
 __global__ __launch_bounds__(kThreads) void route_kernel(skew_route_desc d, const T *logits, const float *bias,
                                                          float *weights, int32_t *chosen) {
   constexpr int kTokens = kThreads / L;
   __shared__ float gval[kTokens][kMaxGroups];
-  __shared__ float pick_l[kTokens][SKEW_MAX_CHOICES];
   __shared__ int32_t pick_e[kTokens][SKEW_MAX_CHOICES];
   const int lane = threadIdx.x % L, slot = threadIdx.x / L;
   const int64_t t = (int64_t)blockIdx.x * kTokens + slot;
@@ -98,20 +101,26 @@ __global__ __launch_bounds__(kThreads) void route_kernel(skew_route_desc d, cons
     mx = mx == kClosed ? 0.0f : mx;   // no open expert: every exp is 0
 #pragma unroll
     for (int v = 0; v < V; v++) {
-      c[v] = expf(l[v] - mx);
+      c[v] = d.renormalize ? fast_exp(l[v] - mx) : expf(l[v] - mx);   // the sum is in the weights without renormalisation
       sum += c[v];
     }
     sum = sum_over<L>(sum);
   }
+  if (bias != nullptr) {
+    float add[V];
+    load_row<V>(bias + (n > 0 ? e0 : 0), n, add);
+    const float r = fast_rcp(sum);
 #pragma unroll
-  for (int v = 0; v < V; v++) {
-    float x = l[v];
-    if (bias != nullptr) {
-      x = (d.score == SKEW_SCORE_SOFTMAX ? c[v] / sum : sigmoid(l[v])) + (v < n ? bias[e0 + v] : 0.0f);
-      if (l[v] == kClosed) x = kClosed;
+    for (int v = 0; v < V; v++) {
+      const float x = (d.score == SKEW_SCORE_SOFTMAX ? c[v] * r : fast_rcp(1.0f + fast_exp(-l[v]))) + add[v];
+      c[v] = l[v] == kClosed ? kClosed : x;
     }
-    c[v] = x != x ? INFINITY : x;
+  } else {
+#pragma unroll
+    for (int v = 0; v < V; v++) c[v] = l[v];
   }
+#pragma unroll
+  for (int v = 0; v < V; v++) c[v] = c[v] != c[v] ? INFINITY : c[v];
 
   if (d.top_groups < d.groups) {
     const int per = d.experts / d.groups;
@@ -172,27 +181,22 @@ __global__ __launch_bounds__(kThreads) void route_kernel(skew_route_desc d, cons
     uint64_t b = __ballot(head == m && m != kClosed);
     if (L < 64) b = (b >> (threadIdx.x & 63 & ~(L - 1))) & ((1ull << (L & 63)) - 1);
     const int win = b != 0 ? (int)__builtin_ctzll(b) : -1;
-    bool mine = lane == win;
-    if (mine) {
+    bool open = lane == win;   // this lane holds it: the first of its values that equals m
+    int at = 0;
 #pragma unroll
-      for (int v = 0; v < V; v++)
-        if (mine && c[v] == m) {
-          pick_e[slot][j] = e0 + v;
-          pick_l[slot][j] = l[v];
-          c[v] = kClosed;
-          mine = false;
-        }
+    for (int v = 0; v < V; v++) {
+      const bool hit = open && c[v] == m;
+      at = hit ? v : at;
+      c[v] = hit ? kClosed : c[v];
+      open = open && !hit;
     }
-    if (win < 0 && lane == 0) {
-      pick_e[slot][j] = -1;
-      pick_l[slot][j] = kClosed;
-    }
+    if (lane == win || (win < 0 && lane == 0)) pick_e[slot][j] = win < 0 ? -1 : e0 + at;
   }
   __syncthreads();
   if (!on) return;
   const bool has = lane < d.k;
   const int e = has ? pick_e[slot][lane] : -1;
-  const float x = e >= 0 ? pick_l[slot][lane] : kClosed;
+  const float x = e >= 0 ? to_f32(logits[t * d.ld + e]) : kClosed;
   float s;
   if (d.score == SKEW_SCORE_SOFTMAX) {
     if (d.renormalize) {   // the softmax over the chosen logits

@@ -68,31 +68,36 @@ __global__ __launch_bounds__(kThreads) void combine_backward_kernel(const int32_
     for (int64_t col = threadIdx.x * 8; col < m; col += kThreads * 8) store8(dy + p * lddy + col, m - col, zero);
 }
 
+// A wave takes one token, 64 16-byte pieces of its row at a time.
 template <class I, class T>
-__global__ __launch_bounds__(kThreads) void embed_kernel(const I *ids, const T *table, int64_t vocab, int64_t cols,
-                                                         int64_t ldt, T *out, int64_t ldo, float scale) {
-  const int64_t t = blockIdx.x, col = ((int64_t)blockIdx.y * kThreads + threadIdx.x) * 8;
-  if (col >= cols) return;
+__global__ __launch_bounds__(kThreads) void embed_kernel(const I *ids, int64_t n, const T *table, int64_t vocab,
+                                                         int64_t cols, int64_t ldt, T *out, int64_t ldo, float scale) {
+  const int64_t t = (int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6);
+  if (t >= n) return;
   const int64_t id = ids[t];
-  float v[8] = {};
-  if ((uint64_t)id < (uint64_t)vocab) {
-    load8(table + id * ldt + col, cols - col, v);
+  const bool there = (uint64_t)id < (uint64_t)vocab;
+#pragma unroll 4
+  for (int64_t col = (threadIdx.x & 63) * kVec<T>; col < cols; col += 64 * kVec<T>) {
+    float v[kVec<T>] = {};
+    if (there) {
+      load_vec(table + id * ldt + col, cols - col, v);
 #pragma unroll
-    for (int i = 0; i < 8; i++) v[i] *= scale;
+      for (int i = 0; i < kVec<T>; i++) v[i] *= scale;
+    }
+    store_vec(out + t * ldo + col, cols - col, v);
   }
-  store8(out + t * ldo + col, cols - col, v);
 }
 
-// The table's gradient from the tokens sorted by id. An id with more than kRun tokens would keep one
-// work-group busy while the others are done, so the sorted places are cut every kRun: a work-group per
-// cut sums the parts of such long ids (at most the id it begins in and the id it ends in, and what of the
-// two is the same id is one) into `part`, 2 rows of float a cut. Then a work-group per row of the table
-// adds its tokens (up to kRun) or its parts in order, scales once and rounds once.
-constexpr int kRun = 64;
+// The table's gradient from the tokens sorted by id. An id with many tokens would keep one wave busy while the
+// others are done, so the sorted places are cut every kRun: a wave per cut and 64 16-byte pieces sums what the cut
+// holds of the ids that reach over its ends (the one it begins in and the one it ends in; where the two are the
+// same id it is one part) into `part`, 2 rows of float a cut. Then a work-group per kIds rows of the table finds
+// their places, and a wave per row and 64 pieces adds the row's tokens, or its parts in order, scales once and
+// rounds once.
+constexpr int kRun = 32, kIds = 32;
 
-// the first sorted place whose key is at least v
-__device__ __forceinline__ int64_t lower_bound(const uint32_t *key, int64_t n, uint32_t v) {
-  int64_t lo = 0, hi = n;
+// the first sorted place in [lo, hi) whose key is at least v, else hi
+__device__ __forceinline__ int64_t lower_bound(const uint32_t *key, int64_t lo, int64_t hi, uint32_t v) {
   while (lo < hi) {
     const int64_t mid = (lo + hi) >> 1;
     if (key[mid] < v) lo = mid + 1;
@@ -100,67 +105,110 @@ __device__ __forceinline__ int64_t lower_bound(const uint32_t *key, int64_t n, u
   }
   return lo;
 }
+// the same in [0, n) by a whole wave, which looks at 64 places at a time
+__device__ __forceinline__ int64_t wave_lower_bound(const uint32_t *key, int64_t n, uint32_t v) {
+  int64_t lo = 0, len = n;
+  while (len > 0) {
+    const int64_t step = (len + 63) / 64, at = (threadIdx.x & 63) * step;
+    // keys rise, so the lanes whose key is below v come first
+    const int below = __popcll(__ballot(at < len && key[lo + (at < len ? at : 0)] < v));
+    if (below == 0) return lo;
+    lo += (below - 1) * step + 1;   // past the last probe that is below
+    const int64_t rest = len - ((below - 1) * step + 1);
+    len = rest < step - 1 ? rest : step - 1;
+  }
+  return lo;
+}
 
-// the sum of dout's rows idx[lo .. hi) in this thread's 8 columns
+// Adds dout's rows idx[lo .. hi), at most 64, in this lane's columns, 8 rows' loads on their way together.
 template <class T>
 __device__ __forceinline__ void sum_rows(const int32_t *idx, int64_t lo, int64_t hi, const T *dout, int64_t ldo,
                                          int64_t col, int64_t cols, float *acc) {
-  for (int64_t i = lo; i < hi; i++) {
-    float v[8];
-    load8(dout + idx[i] * ldo + col, cols - col, v);
+  const int lane = threadIdx.x & 63, n = __builtin_amdgcn_readfirstlane((int)(hi - lo));
+  const int32_t mine = lane < n ? idx[lo + lane] : 0;
+  int r = 0;
+  for (; r + 8 <= n; r += 8) {
+    float v[8][kVec<T>];
 #pragma unroll
-    for (int q = 0; q < 8; q++) acc[q] += v[q];
+    for (int u = 0; u < 8; u++)
+      load_vec(dout + __builtin_amdgcn_readlane(mine, r + u) * ldo + col, cols - col, v[u]);
+#pragma unroll
+    for (int u = 0; u < 8; u++)
+#pragma unroll
+      for (int q = 0; q < kVec<T>; q++) acc[q] += v[u][q];
+  }
+  for (; r < n; r++) {
+    float v[kVec<T>];
+    load_vec(dout + __builtin_amdgcn_readlane(mine, r) * ldo + col, cols - col, v);
+#pragma unroll
+    for (int q = 0; q < kVec<T>; q++) acc[q] += v[q];
   }
 }
 
 template <class T>
-__global__ __launch_bounds__(kThreads) void embed_parts(const uint32_t *key, const int32_t *idx, int64_t n,
-                                                        const T *dout, int64_t ldo, int64_t vocab, int64_t cols,
-                                                        int64_t ldp, float *part) {
+__global__ __launch_bounds__(64) void embed_parts(const uint32_t *key, const int32_t *idx, int64_t n, const T *dout,
+                                                  int64_t ldo, int64_t vocab, int64_t cols, int64_t ldp, float *part) {
+  constexpr int V = kVec<T>;
   const int64_t lo = (int64_t)blockIdx.x * kRun, hi = lo + kRun < n ? lo + kRun : n;
-  const int64_t col = ((int64_t)blockIdx.y * kThreads + threadIdx.x) * 8;
-  if (col >= cols) return;
-  const uint32_t first = key[lo], last = key[hi - 1];
-  if ((int64_t)first < vocab) {   // the id that this cut begins in, as far as it goes here
-    const int64_t b = lower_bound(key, n, first), e = lower_bound(key, n, first + 1);
-    if (e - b > kRun) {
-      float acc[8] = {};
-      sum_rows(idx, lo, e < hi ? e : hi, dout, ldo, col, cols, acc);
-      store8(part + 2 * blockIdx.x * ldp + col, cols - col, acc);
+  const int64_t at = ((int64_t)blockIdx.y * 64 + threadIdx.x) * V, col = at < cols ? at : 0;   // (past the row: not stored)
+  const int lane = threadIdx.x;
+  const uint32_t mine = key[lo + lane < hi ? lo + lane : hi - 1];
+  const uint32_t first = __builtin_amdgcn_readlane(mine, 0), last = key[hi - 1];
+  const bool from_before = lo > 0 && key[lo - 1] == first, goes_on = hi < n && key[hi] == last;
+  const int64_t end = lo + __popcll(__ballot(mine == first && lo + lane < hi));    // of the first id, here
+  const int64_t begin = hi - __popcll(__ballot(mine == last && lo + lane < hi));   // of the last one
+  auto add = [&](int64_t b, int64_t e, int64_t row) {
+    float acc[V] = {};
+    sum_rows(idx, b, e, dout, ldo, col, cols, acc);
+    if (at < cols) {
+#pragma unroll
+      for (int q = 0; q < V; q += 4) store_vec(part + row * ldp + at + q, 4, acc + q);
     }
-  }
-  if (last != first && (int64_t)last < vocab) {
-    const int64_t b = lower_bound(key, n, last), e = lower_bound(key, n, last + 1);
-    if (e - b > kRun) {
-      float acc[8] = {};
-      sum_rows(idx, b, hi, dout, ldo, col, cols, acc);
-      store8(part + (2 * blockIdx.x + 1) * ldp + col, cols - col, acc);
-    }
-  }
+  };
+  if ((int64_t)first < vocab && (from_before || (end == hi && goes_on))) add(lo, end, 2 * blockIdx.x);
+  if ((int64_t)last < vocab && last != first && goes_on) add(begin, hi, 2 * blockIdx.x + 1);
 }
 
 template <class T>
 __global__ __launch_bounds__(kThreads) void embed_rows(const uint32_t *key, const int32_t *idx, int64_t n,
-                                                       const T *dout, int64_t ldo, T *dtable, int64_t cols,
-                                                       int64_t ldt, int64_t ldp, const float *part, float scale) {
-  const int64_t v = blockIdx.x, col = ((int64_t)blockIdx.y * kThreads + threadIdx.x) * 8;
-  if (col >= cols) return;
-  const int64_t b = lower_bound(key, n, (uint32_t)v), e = lower_bound(key, n, (uint32_t)v + 1);
-  float acc[8] = {};
-  if (e - b <= kRun) {
-    sum_rows(idx, b, e, dout, ldo, col, cols, acc);
-  } else {
-    for (int64_t c = b / kRun; c * kRun < e; c++) {   // the cuts that the id's places lie in
-      const bool begins = c * kRun >= b;              // the cut begins in this id
-      float x[8];
-      load8(part + (2 * c + (begins ? 0 : 1)) * ldp + col, cols - col, x);
-#pragma unroll
-      for (int q = 0; q < 8; q++) acc[q] += x[q];
-    }
+                                                       const T *dout, int64_t ldo, T *dtable, int64_t vocab,
+                                                       int64_t cols, int64_t ldt, int64_t ldp, const float *part,
+                                                       float scale) {
+  constexpr int V = kVec<T>;
+  __shared__ int64_t range[2];
+  __shared__ int32_t start[kIds + 1];
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int64_t v0 = (int64_t)blockIdx.x * kIds;
+  if (wave < 2) {
+    const int64_t x = wave_lower_bound(key, n, (uint32_t)(v0 + wave * kIds));
+    if ((tid & 63) == 0) range[wave] = x;
   }
+  __syncthreads();
+  if (tid <= kIds) start[tid] = (int32_t)lower_bound(key, range[0], range[1], (uint32_t)(v0 + tid));
+  __syncthreads();
+  const int64_t left = vocab - v0;
+  const int ids = left < kIds ? (int)left : kIds, pieces = (int)((cols + 64 * V - 1) / (64 * V));
+  for (int64_t item = wave; item < (int64_t)ids * pieces; item += kThreads / 64) {
+    const int r = (int)(item / pieces);
+    const int64_t at = ((item - (int64_t)r * pieces) * 64 + (tid & 63)) * V, col = at < cols ? at : 0;
+    const int64_t b = __builtin_amdgcn_readfirstlane(start[r]), e = __builtin_amdgcn_readfirstlane(start[r + 1]);
+    float acc[V] = {};
+    if (b == e || b / kRun == (e - 1) / kRun) {   // inside one cut
+      sum_rows(idx, b, e, dout, ldo, col, cols, acc);
+    } else {
+#pragma unroll 8
+      for (int64_t c = b / kRun; c < (e + kRun - 1) / kRun; c++) {   // the cuts that the id's places lie in
+        float x[V];
 #pragma unroll
-  for (int q = 0; q < 8; q++) acc[q] *= scale;
-  store8(dtable + v * ldt + col, cols - col, acc);
+        for (int q = 0; q < V; q += 4) load_vec(part + (2 * c + (c * kRun >= b ? 0 : 1)) * ldp + col + q, 4, x + q);   // 0: begins in the id
+#pragma unroll
+        for (int q = 0; q < V; q++) acc[q] += x[q];
+      }
+    }
+#pragma unroll
+    for (int q = 0; q < V; q++) acc[q] *= scale;
+    if (at < cols) store_vec(dtable + (v0 + r) * ldt + at, cols - at, acc);
+  }
 }
 
 inline unsigned col_groups(int64_t cols) { return (unsigned)((cols + kThreads * 8 - 1) / (kThreads * 8)); }
@@ -199,15 +247,15 @@ int launch_combine_backward(const skew_rows &r, const void *dout, int64_t ldo, c
 
 int launch_embed(const void *ids, int id_bytes, int64_t n, const void *table, int64_t vocab, int64_t cols, int64_t ldt,
                  void *out, int64_t ldo, int dtype, float scale, void *stream) {
-  const dim3 grid((unsigned)n, col_groups(cols));
+  const unsigned grid = (unsigned)((n + kThreads / 64 - 1) / (kThreads / 64));
   hipStream_t s = static_cast<hipStream_t>(stream);
   by_type(dtype, [&](auto T) {
     typedef decltype(T) E;
     if (id_bytes == 8)
-      embed_kernel<<<grid, kThreads, 0, s>>>(static_cast<const int64_t *>(ids), static_cast<const E *>(table), vocab,
+      embed_kernel<<<grid, kThreads, 0, s>>>(static_cast<const int64_t *>(ids), n, static_cast<const E *>(table), vocab,
                                              cols, ldt, static_cast<E *>(out), ldo, scale);
     else
-      embed_kernel<<<grid, kThreads, 0, s>>>(static_cast<const int32_t *>(ids), static_cast<const E *>(table), vocab,
+      embed_kernel<<<grid, kThreads, 0, s>>>(static_cast<const int32_t *>(ids), n, static_cast<const E *>(table), vocab,
                                              cols, ldt, static_cast<E *>(out), ldo, scale);
   });
   return (int)hipGetLastError();
@@ -227,12 +275,12 @@ int launch_embed_grad(const SortOut &o, int64_t n, const void *dout, int64_t ldo
   float *part = reinterpret_cast<float *>(partials);
   by_type(dtype, [&](auto T) {
     typedef decltype(T) E;
-    if (n > kRun)   // no id can have more than kRun tokens otherwise
-      embed_parts<<<dim3((unsigned)((n + kRun - 1) / kRun), col_groups(cols)), kThreads, 0, s>>>(
+    if (n > kRun)   // else there is one cut
+      embed_parts<<<dim3((unsigned)((n + kRun - 1) / kRun), (unsigned)((cols + 64 * kVec<E> - 1) / (64 * kVec<E>))), 64, 0, s>>>(
           o.key, o.idx, n, static_cast<const E *>(dout), ldo, vocab, cols, part_stride(cols), part);
-    embed_rows<<<dim3((unsigned)vocab, col_groups(cols)), kThreads, 0, s>>>(
-        o.key, o.idx, n, static_cast<const E *>(dout), ldo, static_cast<E *>(dtable), cols, ldt, part_stride(cols),
-        part, scale);
+    embed_rows<<<(unsigned)((vocab + kIds - 1) / kIds), kThreads, 0, s>>>(
+        o.key, o.idx, n, static_cast<const E *>(dout), ldo, static_cast<E *>(dtable), vocab, cols, ldt,
+        part_stride(cols), part, scale);
   });
   return (int)hipGetLastError();
 }

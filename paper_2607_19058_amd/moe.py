@@ -35,7 +35,7 @@ BF16, F32 = 0, 1
 SCORES = {"softmax": 0, "sigmoid": 1}
 GATHER, TRANSPOSE = 1, 2
 MAX_EXPERTS, MAX_CHOICES, MAX_GROUPS = 1024, 16, 64
-MAX_PLACES, MAX_COLS = 2**31 - 1, 1 << 26
+MAX_PLACES, MAX_COLS = 2**31 - 1, 1 << 24
 
 # names that include/skew_moe.h declares (checked by the CPU test suite)
 EXPORTS = ("skew_route", "skew_route_backward", "skew_order_bytes", "skew_expert_rows", "skew_expert_matmul_bytes",
