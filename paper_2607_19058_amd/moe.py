@@ -26,6 +26,7 @@ from __future__ import annotations
 
 import contextlib
 import ctypes
+import functools
 import math
 from typing import NamedTuple
 
@@ -112,7 +113,7 @@ def _tensor(t, what, dtypes, dims, device=None):
     """Type, device and rank of one tensor argument."""
     if t.dtype not in dtypes:
         raise TypeError(f"{what} must be {' or '.join(str(d).replace('torch.', '') for d in dtypes)}, not {t.dtype}")
-    if t.device.type != "cuda" or (device is not None and t.device != device):
+    if not t.is_cuda or (device is not None and t.device != device):
         raise TypeError(f"{what} must live on the HIP device of the other tensors")
     if t.dim() != dims:
         raise ValueError(f"{what} must have {dims} dimensions, not {t.dim()}")
@@ -130,25 +131,41 @@ def _ld(t, what):
 
 
 def _dense(t, what, shape):
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != shape:
         raise ValueError(f"{what} must have shape {tuple(shape)}, not {tuple(t.shape)}")
     if not t.is_contiguous():
         raise ValueError(f"{what} must be contiguous")
 
 
-@contextlib.contextmanager
-def _on(device, stream):
-    """The device, the stream of the call as the current one (outputs and scratch are allocated on it), its handle."""
+_HERE = contextlib.nullcontext()
+
+
+def _on(device, stream, *inputs):
+    """(handle, context): the stream of the call, and what makes its device and it the current ones, so that outputs
+    and scratch are allocated on it. The memory of inputs is not given away before another stream has used them."""
     import torch
-    with torch.cuda.device(device):
-        current = torch.cuda.current_stream()
-        if stream is None or getattr(stream, "cuda_stream", stream) == current.cuda_stream:
-            yield current.cuda_stream
-            return
-        if not hasattr(stream, "cuda_stream"):
-            stream = torch.cuda.ExternalStream(stream, device=device)
-        with torch.cuda.stream(stream):
-            yield stream.cuda_stream
+    if stream is None:
+        index = device.index
+        s = torch._C._cuda_getCurrentRawStream(index)
+        return s, (_HERE if index == torch.cuda.current_device() else torch.cuda.device(device))
+    handle = getattr(stream, "cuda_stream", stream)
+    if handle == torch._C._cuda_getCurrentRawStream(device.index) and device.index == torch.cuda.current_device():
+        return handle, _HERE
+    if not hasattr(stream, "cuda_stream"):
+        stream = torch.cuda.ExternalStream(stream, device=device)
+    elif stream.device != device:
+        raise ValueError(f"the stream is on {stream.device}, the tensors on {device}")
+    for t in inputs:
+        if t is not None:
+            t.record_stream(stream)
+    return handle, torch.cuda.stream(stream)
+
+
+@functools.lru_cache(maxsize=4096)
+def _order_bytes(n, keys, cols):
+    nbytes = ctypes.c_size_t()
+    _check(_lib().skew_order_bytes(n, keys, cols, ctypes.byref(nbytes)), "skew_order_bytes")
+    return nbytes.value
 
 
 def _check(rc, what):
@@ -162,7 +179,7 @@ def _scratch(nbytes, device):
 
 
 def _ptr(t):
-    return None if t is None or t.numel() == 0 else t.data_ptr()
+    return None if t is None else t.data_ptr() or None
 
 
 # ---- routing ----------------------------------------------------------------------------------
@@ -206,7 +223,8 @@ def route(logits, k, *, score="softmax", bias=None, groups=1, top_groups=None, g
     if bias is not None:
         _tensor(bias, "bias", (torch.float32,), 1, logits.device)
         _dense(bias, "bias", (d.experts,))
-    with _on(logits.device, stream) as s:
+    s, here = _on(logits.device, stream, logits, bias)
+    with here:
         weights = torch.empty((d.tokens, k), dtype=torch.float32, device=logits.device)
         experts = torch.empty((d.tokens, k), dtype=torch.int32, device=logits.device)
         _check(_lib().skew_route(ctypes.byref(d), _ptr(logits), _ptr(bias) if bias is not None else None,
@@ -222,7 +240,8 @@ def route_backward(logits, experts, dweights, *, score="softmax", renormalize=Tr
     _dense(experts, "experts", (d.tokens, d.k))
     _tensor(dweights, "dweights", (torch.float32,), 2, logits.device)
     _dense(dweights, "dweights", (d.tokens, d.k))
-    with _on(logits.device, stream) as s:
+    s, here = _on(logits.device, stream, logits, experts, dweights)
+    with here:
         dlogits = torch.empty((d.tokens, d.experts), dtype=logits.dtype, device=logits.device)
         _check(_lib().skew_route_backward(ctypes.byref(d), _ptr(logits), _ptr(experts), _ptr(dweights),
                                           _ptr(dlogits), s), "skew_route_backward")
@@ -240,15 +259,15 @@ def expert_rows(experts, n_experts, *, stream=None) -> ExpertRows:
     if not 1 <= k <= MAX_CHOICES or T * k > MAX_PLACES:
         raise ValueError(f"experts must hold 1 to {MAX_CHOICES} choices a token, of fewer than 2^31 pairs")
     L, n, dev = _lib(), T * k, experts.device
-    nbytes = ctypes.c_size_t()
-    _check(L.skew_order_bytes(n, n_experts, 0, ctypes.byref(nbytes)), "skew_order_bytes")
-    with _on(dev, stream) as s:
+    nbytes = _order_bytes(n, n_experts, 0)
+    s, here = _on(dev, stream, experts)
+    with here:
         plan = ExpertRows(torch.empty(n_experts + 1, dtype=torch.int32, device=dev),
                           torch.empty(n, dtype=torch.int32, device=dev),
                           torch.empty((T, k), dtype=torch.int32, device=dev))
-        ws = _scratch(nbytes.value, dev)
+        ws = _scratch(nbytes, dev)
         _check(L.skew_expert_rows(_ptr(experts), n, n_experts, _ptr(plan.offsets), _ptr(plan.rows), _ptr(plan.slots),
-                                  _ptr(ws), nbytes.value, s), "skew_expert_rows")
+                                  _ptr(ws), nbytes, s), "skew_expert_rows")
     return plan
 
 
@@ -282,7 +301,7 @@ def _stack(w, what, E):
 
 
 def _rows_of(t, what, rows, cols):
-    if tuple(t.shape) != (rows, cols):
+    if t.shape != (rows, cols):
         raise ValueError(f"{what} must have shape {(rows, cols)}, not {tuple(t.shape)}")
     return _ld(t, what)
 
@@ -307,7 +326,8 @@ def expert_matmul(x, w, plan, *, gather=False, transpose=False, scale=None, dtyp
     dtype = torch.bfloat16 if dtype is None else dtype
     code, cols = _dtype_code(dtype, "dtype"), n if transpose else m
     L = _lib()
-    with _on(x.device, stream) as s:
+    s, here = _on(x.device, stream, x, w, scale, *plan)
+    with here:
         y = torch.empty((r.tokens * r.k, cols), dtype=dtype, device=x.device)
         p = ProductDesc(_ptr(x), _ptr(w), _ptr(y), _ptr(scale), n, m, ldx, ldw, step, cols,
                         (GATHER if gather else 0) | (TRANSPOSE if transpose else 0), code)
@@ -330,7 +350,8 @@ def expert_matmul_grad(x, dy, plan, *, gather=False, out=None, stream=None):
     n, m = x.shape[1], dy.shape[1]
     ldx = _rows_of(x, "x", r.tokens if gather else r.tokens * r.k, n)
     ldy = _rows_of(dy, "dy", r.tokens * r.k, m)
-    with _on(x.device, stream) as s:
+    s, here = _on(x.device, stream, x, dy, out, *plan)
+    with here:
         if out is None:
             out = torch.empty((r.experts, n, m), dtype=torch.bfloat16, device=x.device)
         _tensor(out, "out", (torch.bfloat16,), 3, x.device)
@@ -357,7 +378,8 @@ def expert_combine(y, plan, weights=None, *, dtype=None, stream=None):
         _dense(weights, "weights", (r.tokens, r.k))
     dtype = y.dtype if dtype is None else dtype
     code = _dtype_code(dtype, "dtype")
-    with _on(y.device, stream) as s:
+    s, here = _on(y.device, stream, y, weights, *plan)
+    with here:
         out = torch.empty((r.tokens, m), dtype=dtype, device=y.device)
         _check(_lib().skew_expert_combine(ctypes.byref(r), _ptr(y), _dtype_code(y.dtype, "y"), ldy, _ptr(weights),
                                           _ptr(out), code, m, m, s), "skew_expert_combine")
@@ -377,7 +399,8 @@ def expert_combine_backward(dout, y, plan, weights=None, *, stream=None):
     if weights is not None:
         _tensor(weights, "weights", (torch.float32,), 2, dout.device)
         _dense(weights, "weights", (r.tokens, r.k))
-    with _on(dout.device, stream) as s:
+    s, here = _on(dout.device, stream, dout, y, weights, *plan)
+    with here:
         dy = torch.empty((r.tokens * r.k, m), dtype=torch.bfloat16, device=dout.device)
         dweights = torch.empty((r.tokens, r.k), dtype=torch.float32, device=dout.device)
         _check(_lib().skew_expert_combine_backward(ctypes.byref(r), _ptr(dout), ldo, _ptr(y), _dtype_code(y.dtype, "y"),
@@ -408,7 +431,8 @@ def embed(tokens, table, *, scale=1.0, stream=None):
     if not math.isfinite(scale):
         raise ValueError("scale must be finite")
     ld = _ld(table, "table")
-    with _on(table.device, stream) as s:
+    s, here = _on(table.device, stream, tokens, table)
+    with here:
         out = torch.empty((T, D), dtype=table.dtype, device=table.device)
         _check(_lib().skew_embed(_ptr(tokens), size, T, _ptr(table), V, D, ld, _ptr(out), D,
                                  _dtype_code(table.dtype, "table"), scale, s), "skew_embed")
@@ -429,14 +453,14 @@ def embed_grad(tokens, dout, vocab, *, scale=1.0, out=None, stream=None):
     if not math.isfinite(scale):
         raise ValueError("scale must be finite")
     ldo, L, dev = _ld(dout, "dout"), _lib(), dout.device
-    nbytes = ctypes.c_size_t()
-    _check(L.skew_order_bytes(T, vocab, D, ctypes.byref(nbytes)), "skew_order_bytes")
-    with _on(dev, stream) as s:
+    nbytes = _order_bytes(T, vocab, D)
+    s, here = _on(dev, stream, tokens, dout, out)
+    with here:
         if out is None:
             out = torch.empty((vocab, D), dtype=dout.dtype, device=dev)
         _tensor(out, "out", (dout.dtype,), 2, dev)
         ldt = _rows_of(out, "out", vocab, D)
-        ws = _scratch(nbytes.value, dev)
+        ws = _scratch(nbytes, dev)
         _check(L.skew_embed_grad(_ptr(tokens), size, T, _ptr(dout), ldo, out.data_ptr(), vocab, D, ldt,
-                                 _dtype_code(dout.dtype, "dout"), scale, _ptr(ws), nbytes.value, s), "skew_embed_grad")
+                                 _dtype_code(dout.dtype, "dout"), scale, _ptr(ws), nbytes, s), "skew_embed_grad")
     return out
