@@ -35,6 +35,8 @@ struct ProductArgs {
   int32_t direct;                 // 16-byte rows in both operands and lengths that are multiples of 8
   int32_t wide, chunks;           // 4 neighbouring results can be stored together; 8, and none of them is past the edge
   int64_t row_tiles;              // forward, backward: tiles of rows in the grid
+  int32_t in_patches;             // how tiles are given out (patch_tile)
+  int32_t part;                   // forward, backward: contraction length of a work-group (a multiple of its stages)
 };
 
 constexpr int kBK = 32;   // contraction length of a step: one matrix instruction's
@@ -208,13 +210,21 @@ __device__ __forceinline__ const char *scalar(const char *p) {
 
 // Which tile a work-group takes. Work-groups go to the 8 dies in turn (id % 8), and each die has its own L2, so
 // patches of kPatchR x kPatchC tiles (one for each of a die's 32 compute units) go to the dies in turn: a
-// patch's tiles share their operands' rows and columns in one L2. Returns false where the patch passes the edge.
-constexpr int kDies = 8, kPatchR = 4, kPatchC = 8;
-__host__ __device__ inline int64_t patch_grid(int64_t rows, int64_t cols) {
-  const int64_t p = ((rows + kPatchR - 1) / kPatchR) * ((cols + kPatchC - 1) / kPatchC);
-  return (p + kDies - 1) / kDies * kDies * (kPatchR * kPatchC);
+// patch's tiles share their operands' rows and columns in one L2. patch_tile: false where the patch passes the edge.
+// Fewer patches than kMinPatches would leave dies idle: then single tiles go to the dies in turn.
+constexpr int kDies = 8, kPatchR = 4, kPatchC = 8, kMinPatches = 4 * kDies;
+inline int64_t patches(int64_t rows, int64_t cols) {
+  return ((rows + kPatchR - 1) / kPatchR) * ((cols + kPatchC - 1) / kPatchC);
 }
-__device__ __forceinline__ bool patch_tile(int64_t rows, int64_t cols, int64_t *row, int64_t *col) {
+inline int64_t patch_grid(int64_t rows, int64_t cols, bool in_patches) {
+  return in_patches ? (patches(rows, cols) + kDies - 1) / kDies * kDies * (kPatchR * kPatchC) : rows * cols;
+}
+__device__ __forceinline__ bool patch_tile(bool in_patches, int64_t rows, int64_t cols, int64_t *row, int64_t *col) {
+  if (!in_patches) {
+    *row = blockIdx.x / (uint32_t)cols;
+    *col = blockIdx.x % (uint32_t)cols;
+    return true;
+  }
   const uint32_t i = blockIdx.x / kDies, in = i % (kPatchR * kPatchC);
   const uint32_t patch = i / (kPatchR * kPatchC) * kDies + blockIdx.x % kDies, pc = (uint32_t)((cols + kPatchC - 1) / kPatchC);
   *row = (int64_t)(patch / pc) * kPatchR + in % kPatchR;
@@ -244,7 +254,7 @@ __device__ __forceinline__ bool take_tile(const ProductArgs &a, Tile *t) {
   t->first = 0;
   if (MODE == kWeights) {
     const int64_t tn = (a.n + BM - 1) / BM, tm = (a.m + BN - 1) / BN;
-    if (!patch_tile(a.experts * tn, tm, &tr, &tc)) return false;
+    if (!patch_tile(a.in_patches, a.experts * tn, tm, &tr, &tc)) return false;
     t->expert = (int)(tr / tn);
     t->r0 = tr % tn * BM;
     t->r1 = a.n;
@@ -253,7 +263,7 @@ __device__ __forceinline__ bool take_tile(const ProductArgs &a, Tile *t) {
     t->K = __builtin_amdgcn_readfirstlane(a.offsets[t->expert + 1] - (int)t->first);
   } else {
     t->c1 = MODE == kForward ? a.m : a.n;
-    if (!patch_tile(a.row_tiles, (t->c1 + BN - 1) / BN, &tr, &tc) || !find_tile<BM>(a, tr, &t->expert, &t->r0, &t->r1)) return false;
+    if (!patch_tile(a.in_patches, a.row_tiles, (t->c1 + BN - 1) / BN, &tr, &tc) || !find_tile<BM>(a, tr, &t->expert, &t->r0, &t->r1)) return false;
     t->expert = __builtin_amdgcn_readfirstlane(t->expert);   // the same in every lane, but found in a loop over lanes
     t->r0 = scalar(t->r0);
     t->r1 = scalar(t->r1);
@@ -356,7 +366,7 @@ __global__ __launch_bounds__(256, FM * FN * KS >= 64 ? 1 : FM * FN == 8 ? 3 : 2)
   const int wr = (wave >> 1) * (BM / 2), wc = (wave & 1) * (BN / 2);
   Tile t;
   if (!take_tile<MODE, BM, BN>(a, &t)) return;
-  const int K = t.K;
+  int K = t.K;
 
   f32x4 acc[FM][FN];
 #pragma unroll
@@ -378,6 +388,14 @@ __global__ __launch_bounds__(256, FM * FN * KS >= 64 ? 1 : FM * FN == 8 ? 3 : 2)
     step_a = 2 * BK;
   }
   step_b = MODE == kBackward ? 2 * BK : 2 * BK * a.ldw;
+  if (MODE != kWeights && a.part) {   // this work-group's part of a contraction that several share
+    const int k0 = (int)blockIdx.y * a.part;
+    K = K - k0 < a.part ? (K > k0 ? K - k0 : 0) : a.part;
+    if (K > 0) {
+      xa += k0 / BK * step_a;
+      xb += k0 / BK * step_b;
+    }
+  }
   if (MODE == kBackward) xb += 2 * t.c0 * a.ldw;
   xa = scalar(xa);
   xb = scalar(xb);
@@ -576,6 +594,7 @@ __global__ __launch_bounds__(256, FM * FN * KS >= 64 ? 1 : FM * FN == 8 ? 3 : 2)
     __syncthreads();   // the buffers are no longer read
   }
   if (kInA) mfma_done();
+  if (MODE != kWeights && a.part) a.y = static_cast<float *>(a.y) + (int64_t)blockIdx.y * a.places * a.ldy;
   store_tile<MODE, FM, FN>(a, t, wr, wc, acc, reinterpret_cast<char *>(lds) + wave * (FM * FN * 512));
 }
 
@@ -637,42 +656,65 @@ __global__ __launch_bounds__(256, 2) void any_kernel(ProductArgs a) {
       pb[i] = w + row * a.ldw + t.c0 + c * 8;
     }
   }
-  const int64_t step_b = MODE == kBackward ? kBK : kBK * a.ldw;
-  u32x4 ga[kP], gb[kP];
-  auto load = [&](int k0, int in_list) {   // in_list: k0 from the list's first place on
-    if (inside && k0 + kBK <= K) {
-#pragma unroll
-      for (int i = 0; i < kP; i++) {
-        const bf16_t *p = pa[i] + (MODE == kWeights ? list[in_list + ka[i]] * a.ldx : 0);
-        ga[i] = *reinterpret_cast<const u32x4_a2 *>(p);
-        gb[i] = *reinterpret_cast<const u32x4_a2 *>(pb[i]);
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < kP; i++) {
-        const int la = K - k0 - ka[i], lb = K - k0 - kb[i];   // contraction values from this chunk on
-        const bf16_t *p = pa[i] + (MODE == kWeights && la > 0 ? list[in_list + ka[i]] * a.ldx : 0);
-        ga[i] = la > 0 ? load_chunk(p, MODE == kWeights ? na[i] : la) : u32x4{0, 0, 0, 0};
-        gb[i] = lb > 0 ? load_chunk(pb[i], MODE == kBackward ? lb : nb[i]) : u32x4{0, 0, 0, 0};
-      }
-    }
+  // kSets stages are on their way into registers, set by set
+  constexpr int kSets = 3;
+  u32x4 ga[kSets][kP], gb[kSets][kP];
+  int base = 0, end = 0;   // kWeights: the places in the list
+  auto load = [&](auto SET, auto WHOLE, int k0) {
+    const int64_t ob = MODE == kBackward ? k0 : k0 * a.ldw;
 #pragma unroll
     for (int i = 0; i < kP; i++) {
-      if (MODE != kWeights) pa[i] += kBK;
-      pb[i] += step_b;
+      if (WHOLE) {
+        const bf16_t *p = pa[i] + (MODE == kWeights ? list[k0 - base + ka[i]] * a.ldx : k0);
+        ga[SET][i] = *reinterpret_cast<const u32x4_a2 *>(p);
+        gb[SET][i] = *reinterpret_cast<const u32x4_a2 *>(pb[i] + ob);
+      } else {
+        const int la = end - k0 - ka[i], lb = end - k0 - kb[i];   // contraction values from this chunk on
+        const bf16_t *p = pa[i] + (MODE != kWeights ? k0 : la > 0 ? list[k0 - base + ka[i]] * a.ldx : 0);
+        ga[SET][i] = la > 0 ? load_chunk(p, MODE == kWeights ? na[i] : la) : u32x4{0, 0, 0, 0};
+        gb[SET][i] = lb > 0 ? load_chunk(pb[i] + ob, MODE == kBackward ? lb : nb[i]) : u32x4{0, 0, 0, 0};
+      }
     }
   };
-  auto put_stage = [&](int buf) {
+  auto put_stage = [&](auto SET, int buf) {
 #pragma unroll
     for (int i = 0; i < kP; i++) {
-      ta[buf * kC + tid + i * kThreads] = ga[i];
-      tb[buf * kC + tid + i * kThreads] = gb[i];
+      ta[buf * kC + tid + i * kThreads] = ga[SET][i];
+      tb[buf * kC + tid + i * kThreads] = gb[SET][i];
     }
   };
   FragK<1> ra_k(ta, wr), rb_k(tb, wc);
   FragT<B, F> ra_t(ta, wr), rb_t(tb, wc);
-  int buf = 0;
-  for (int base = 0, end; base < K; base = end) {   // kWeights: rounds of the places in the list
+  int buf = 0;   // the buffer of the stage that is multiplied
+  // one stage: the next one goes from SET to the other buffer, and the stage at `ahead` is sent for into SET
+  auto stage = [&](auto SET, auto WHOLE, int ahead) {
+    __syncthreads();
+    put_stage(SET, buf ^ 1);
+    load(SET, WHOLE, ahead);
+    bf16x8 fa[F], fb[F];
+#pragma unroll
+    for (int i = 0; i < F; i++) {
+      fa[i] = MODE == kWeights ? ra_t.get(0, i) : ra_k.get(0, i);
+      fb[i] = MODE == kBackward ? rb_k.get(0, i) : rb_t.get(0, i);
+    }
+    const int32_t across = buf ? -kBytes : kBytes;   // to the other buffer
+    if (MODE == kWeights) ra_t.move(across);
+    else ra_k.move(across);
+    if (MODE == kBackward) rb_k.move(across);
+    else rb_t.move(across);
+#pragma unroll
+    for (int i = 0; i < F; i++)
+#pragma unroll
+      for (int j = 0; j < F; j++)
+        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[j], fa[i], acc[i][j], 0, 0, 0);
+    buf ^= 1;
+  };
+  const std::integral_constant<int, 0> set0;
+  const std::integral_constant<int, 1> set1;
+  const std::integral_constant<int, 2> set2;
+  const std::true_type whole;
+  const std::false_type any;
+  for (; base < K; base = end) {   // kWeights: rounds of the places in the list
     end = MODE == kWeights && base + kList < K ? base + kList : K;
     if (MODE == kWeights) {
       __syncthreads();
@@ -680,78 +722,122 @@ __global__ __launch_bounds__(256, 2) void any_kernel(ProductArgs a) {
         list[i] = a.gather ? a.rows[t.first + base + i] / a.k : (int32_t)(t.first + base + i);
       __syncthreads();
     }
-    load(base, 0);
-    put_stage(buf);
-    for (int k0 = base; k0 < end; k0 += kBK) {
-      __syncthreads();
-      const bool more = k0 + kBK < end;
-      if (more) load(k0 + kBK, k0 + kBK - base);
-      bf16x8 fa[F], fb[F];
-#pragma unroll
-      for (int i = 0; i < F; i++) {
-        fa[i] = MODE == kWeights ? ra_t.get(0, i) : ra_k.get(0, i);
-        fb[i] = MODE == kBackward ? rb_k.get(0, i) : rb_t.get(0, i);
+    load(set0, any, base);
+    load(set1, any, base + kBK);
+    load(set2, any, base + 2 * kBK);
+    put_stage(set0, buf);
+    load(set0, any, base + 3 * kBK);
+    int k0 = base;
+    if (inside)
+      for (; k0 + 7 * kBK <= end; k0 += 3 * kBK) {   // sends for three whole stages
+        stage(set1, whole, k0 + 4 * kBK);
+        stage(set2, whole, k0 + 5 * kBK);
+        stage(set0, whole, k0 + 6 * kBK);
       }
-      const int32_t across = buf ? -kBytes : kBytes;   // to the other buffer
-      if (MODE == kWeights) ra_t.move(across);
-      else ra_k.move(across);
-      if (MODE == kBackward) rb_k.move(across);
-      else rb_t.move(across);
-#pragma unroll
-      for (int i = 0; i < F; i++)
-#pragma unroll
-        for (int j = 0; j < F; j++)
-          acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[j], fa[i], acc[i][j], 0, 0, 0);
-      buf ^= 1;
-      if (more) put_stage(buf);
+    for (; k0 < end; k0 += 3 * kBK) {
+      stage(set1, any, k0 + 4 * kBK);
+      if (k0 + kBK < end) stage(set2, any, k0 + 5 * kBK);
+      if (k0 + 2 * kBK < end) stage(set0, any, k0 + 6 * kBK);
     }
   }
   store_tile<MODE, F, F>(a, t, wr, wc, acc, nullptr);
 }
 
+// Sums the parts of a contraction that several work-groups shared, in order: y[p] = s_p sum of part[i][p].
+__global__ __launch_bounds__(256) void join_kernel(ProductArgs a, const float *part, int parts, int64_t cols, int held_at) {
+  const int64_t p = blockIdx.x, col = ((int64_t)blockIdx.y * 256 + threadIdx.x) * 4;
+  if (col >= cols) return;
+  f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+  for (int i = 0; i < parts; i++) acc += *reinterpret_cast<const f32x4 *>(part + ((int64_t)i * a.places + p) * cols + col);
+  if (a.scale && p < a.offsets[held_at]) acc *= a.scale[a.rows[p]];
+  store4(a, p * a.ldy + col, cols - col, acc);
+}
+
 // The grid of a tiled kernel.
 template <int MODE>
 int64_t tiles(ProductArgs &a, int64_t bm, int64_t bn) {
-  if (MODE == kWeights) return patch_grid(a.experts * ((a.n + bm - 1) / bm), (a.m + bn - 1) / bn);
   // an expert (and the places without a pair) ends in at most one tile that is not full
   a.row_tiles = a.places / bm + a.experts + 1 < a.places ? a.places / bm + a.experts + 1 : a.places;
-  return patch_grid(a.row_tiles, ((MODE == kForward ? a.m : a.n) + bn - 1) / bn);
+  const int64_t rows = MODE == kWeights ? a.experts * ((a.n + bm - 1) / bm) : a.row_tiles;
+  const int64_t cols = ((MODE == kBackward ? a.n : a.m) + bn - 1) / bn;
+  a.in_patches = patches(rows, cols) >= kMinPatches;
+  return patch_grid(rows, cols, a.in_patches);
 }
 
-template <int MODE, int FM, int FN, int NS, int KS = 1>
-int launch_tile(ProductArgs a, void *stream) {
+// Which kernel, by the rows an expert has on average and so that there are tiles for the chip. Times (us) on 32
+// experts of 2048 x 8192 with even rows, for tiles of 64 x 256, 128 x 256 and 256 x 256 (forward, backward), weights of the
+// last two:
+//   rows an expert   forward            backward           weights
+//    32              199  189  259      196  204  263      242  281
+//   128              258  199  257      251  225  266      339  402
+//   256              418  326  291      407  367  290      523  515
+//   512              752  594  515      728  671  516      737  709
+// Where even tiles of 64 x 128 are few, several work-groups share a contraction and join_kernel adds their parts.
+struct Choice {
+  int fm, fn, parts;
+};
+template <int MODE>
+Choice choose(const ProductArgs &a) {
+  const int64_t rows = a.places / a.experts, cols = MODE == kBackward ? a.n : a.m, K = MODE == kForward ? a.n : a.m;
+  auto count = [&](int64_t bm, int64_t bn) {   // tiles, if the rows fill theirs
+    return (MODE == kWeights ? a.experts * ((a.n + bm - 1) / bm) : (a.places + bm - 1) / bm) * ((cols + bn - 1) / bn);
+  };
+  constexpr int64_t kEnough = 512;   // two for each compute unit
+  if (rows >= (MODE == kForward ? 384 : 256) && count(256, 256) >= kEnough) return {8, 8, 1};
+  if ((rows >= 64 || MODE == kWeights) && count(128, 256) >= kEnough) return {4, 8, 1};
+  if (MODE == kWeights) return {2, 4, 1};
+  const int64_t part_full = a.places / 64 + a.experts;   // row tiles with those that are not full
+  const int64_t row_tiles = part_full < a.places ? part_full : a.places;
+  if (row_tiles * ((cols + 255) / 256) >= kEnough) return {2, 8, 1};
+  // (below 2048 the join, 3 us, costs what the shorter contractions save)
+  int64_t parts = K < 2048 ? 1 : kEnough / (row_tiles * ((cols + 127) / 128));
+  if (parts > K / 256) parts = K / 256;
+  return {2, 4, parts > 1 ? (int)parts : 1};
+}
+
+template <int MODE, int FM, int FN, int NS, int KS>
+int launch_tile(ProductArgs a, int parts, void *stream) {
   const int64_t grid = tiles<MODE>(a, 32 * FM, 32 * FN);
   if (grid > 0x7FFFFFFF) return (int)hipErrorInvalidConfiguration;
-  tile_kernel<MODE, FM, FN, NS, KS><<<(unsigned)grid, 256, 0, static_cast<hipStream_t>(stream)>>>(a);
+  tile_kernel<MODE, FM, FN, NS, KS><<<dim3((unsigned)grid, parts), 256, 0, static_cast<hipStream_t>(stream)>>>(a);
   return (int)hipGetLastError();
 }
-template <int MODE, int F>
+template <int MODE>
 int launch_any(ProductArgs a, void *stream) {
-  const int64_t grid = tiles<MODE>(a, 32 * F, 32 * F);
+  const int64_t grid = tiles<MODE>(a, 128, 128);
   if (grid > 0x7FFFFFFF) return (int)hipErrorInvalidConfiguration;
-  any_kernel<MODE, F><<<(unsigned)grid, 256, 0, static_cast<hipStream_t>(stream)>>>(a);
+  any_kernel<MODE, 4><<<(unsigned)grid, 256, 0, static_cast<hipStream_t>(stream)>>>(a);
   return (int)hipGetLastError();
 }
 
+// Stages of two steps where W's rows run along the contraction: whole 128-byte lines of them.
 template <int MODE>
-int launch_mode(const ProductArgs &a, void *stream) {
-  if (!a.direct) return launch_any<MODE, 4>(a, stream);
-  // By the rows an expert has on average, and so that the chip has tiles. Measured (us) on 32 experts of 2048 x 8192
-  // and 8192 x 2048, rows spread evenly over the experts, at 64 / 128 / 256 wide rows of tiles:
-  //   forward   32 rows 199 / 189 / 259, 128 rows 258 / 199 / 257, 256 rows 418 / 326 / 291, 512 rows 752 / 594 / 515
-  //   backward  32 rows 196 / 204 / 263, 128 rows 251 / 225 / 266, 256 rows 407 / 367 / 290, 512 rows 728 / 671 / 516
-  //   weights   32 rows 430 / 242 / 281, 128 rows 688 / 339 / 402, 256 rows 826 / 523 / 515, 512 rows 1275 / 737 / 709
-  const int64_t rows = a.places / a.experts;
-  auto enough = [&](int64_t bm, int64_t bn) {   // two rounds of work-groups, roughly
-    const int64_t full = MODE == kWeights ? a.experts * ((a.n + bm - 1) / bm) : (a.places + bm - 1) / bm;
-    return full * (((MODE == kBackward ? a.n : a.m) + bn - 1) / bn) >= 512;
-  };
-  if (rows >= (MODE == kForward ? 384 : 256) && enough(256, 256)) return launch_tile<MODE, 8, 8, MODE == kBackward ? 2 : 4, MODE == kBackward ? 2 : 1>(a, stream);
-  if ((rows >= 64 || MODE == kWeights) && enough(128, 256)) return launch_tile<MODE, 4, 8, 3, MODE == kBackward ? 2 : 1>(a, stream);
+int launch_mode(const ProductArgs &a, char *ws, void *stream) {
+  constexpr bool kTwo = MODE == kBackward;
+  if (!a.direct) return launch_any<MODE>(a, stream);
+  const Choice c = choose<MODE>(a);
+  if (c.fm == 8) return launch_tile<MODE, 8, 8, kTwo ? 2 : 4, kTwo ? 2 : 1>(a, 1, stream);
+  if (c.fm == 4) return launch_tile<MODE, 4, 8, 3, kTwo ? 2 : 1>(a, 1, stream);
   if constexpr (MODE != kWeights) {
-    if (enough(64, 256)) return launch_tile<MODE, 2, 8, MODE == kBackward ? 2 : 4, MODE == kBackward ? 2 : 1>(a, stream);
+    if (c.fn == 8) return launch_tile<MODE, 2, 8, kTwo ? 2 : 4, kTwo ? 2 : 1>(a, 1, stream);
+    if (c.parts > 1) {
+      const int64_t cols = MODE == kBackward ? a.n : a.m, K = MODE == kForward ? a.n : a.m;
+      ProductArgs b = a;
+      b.part = (int32_t)(((K + c.parts - 1) / c.parts + 63) / 64 * 64);
+      b.y = ws;
+      b.scale = nullptr;
+      b.ldy = cols;
+      b.f32 = b.wide = 1;   // cols is a multiple of 8
+      b.chunks = 0;
+      const int parts = (int)((K + b.part - 1) / b.part);
+      const int e = launch_tile<MODE, 2, 4, kTwo ? 2 : 4, kTwo ? 2 : 1>(b, parts, stream);
+      if (e != (int)hipSuccess) return e;
+      join_kernel<<<dim3((unsigned)a.places, (unsigned)((cols + 1023) / 1024)), 256, 0, static_cast<hipStream_t>(stream)>>>(
+          a, reinterpret_cast<const float *>(ws), parts, cols, a.experts);
+      return (int)hipGetLastError();
+    }
   }
-  return launch_tile<MODE, 2, 4, MODE == kBackward ? 2 : 4, MODE == kBackward ? 2 : 1>(a, stream);
+  return launch_tile<MODE, 2, 4, kTwo ? 2 : 4, kTwo ? 2 : 1>(a, 1, stream);
 }
 
 ProductArgs args_of(const skew_rows &r, const skew_product_desc &p) {
@@ -783,15 +869,26 @@ bool chunks(const void *p, int64_t ld) { return ((uintptr_t)p & 15) == 0 && ld %
 
 }  // namespace
 
-size_t product_scratch(const skew_rows &, const skew_product_desc &) { return 0; }
-
-int launch_product(const skew_rows &r, const skew_product_desc &p, char *, void *stream) {
+ProductArgs product_args(const skew_rows &r, const skew_product_desc &p) {
   ProductArgs a = args_of(r, p);
   a.direct = chunks(a.x, a.ldx) && chunks(a.w, a.ldw) && a.slice % 8 == 0 && a.n % 8 == 0 && a.m % 8 == 0 &&
              short_rows(a.gather ? r.tokens : kMaxTile, a.ldx) && short_rows(kMaxTile, a.ldw);
   a.wide = ((uintptr_t)a.y & 15) == 0 && a.ldy % 4 == 0;
   a.chunks = a.wide && a.ldy % 8 == 0 && (p.flags & SKEW_TRANSPOSE ? a.n : a.m) % 8 == 0;
-  return p.flags & SKEW_TRANSPOSE ? launch_mode<kBackward>(a, stream) : launch_mode<kForward>(a, stream);
+  return a;
+}
+
+size_t product_scratch(const skew_rows &r, const skew_product_desc &p) {
+  if (r.tokens == 0) return 0;
+  const ProductArgs a = product_args(r, p);
+  const bool back = (p.flags & SKEW_TRANSPOSE) != 0;
+  const int parts = back ? choose<kBackward>(a).parts : choose<kForward>(a).parts;   // whatever the alignment
+  return parts > 1 ? (size_t)parts * (size_t)a.places * (size_t)(back ? a.n : a.m) * 4 : 0;
+}
+
+int launch_product(const skew_rows &r, const skew_product_desc &p, char *ws, void *stream) {
+  const ProductArgs a = product_args(r, p);
+  return p.flags & SKEW_TRANSPOSE ? launch_mode<kBackward>(a, ws, stream) : launch_mode<kForward>(a, ws, stream);
 }
 
 int launch_product_grad(const skew_rows &r, const skew_product_desc &p, void *stream) {
@@ -805,7 +902,7 @@ int launch_product_grad(const skew_rows &r, const skew_product_desc &p, void *st
              short_rows(a.gather ? r.tokens : a.places, a.ldx) && short_rows(kMaxTile, a.ldw);
   a.wide = ((uintptr_t)a.y & 15) == 0 && a.ldy % 4 == 0 && a.slice % 4 == 0;
   a.chunks = a.wide && a.ldy % 8 == 0 && a.slice % 8 == 0 && a.m % 8 == 0;
-  return launch_mode<kWeights>(a, stream);
+  return launch_mode<kWeights>(a, nullptr, stream);
 }
 
 }  // namespace moe
