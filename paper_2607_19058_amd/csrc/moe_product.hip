@@ -290,8 +290,7 @@ __device__ __forceinline__ void store_tile(const ProductArgs &a, const Tile &t, 
     for (int i = 0; i < FM; i++)
       if (row0 + i * 16 < t.r1) s[i] = a.scale[a.rows[row0 + i * 16]];
   }
-  const int64_t at = (MODE == kWeights ? (int64_t)t.expert * a.slice : 0) + row0 * a.ldy + col0;
-  if (room && a.chunks && !a.f32) {
+  if (!a.f32) {
     constexpr int kChunks = 2 * FN;   // of a row, placed with their index xor-ed with the row
 #pragma unroll
     for (int i = 0; i < FM; i++)
@@ -309,34 +308,37 @@ __device__ __forceinline__ void store_tile(const ProductArgs &a, const Tile &t, 
       const int q = n * 64 + lane, row = q / kChunks, c = q % kChunks;
       const u32x4 v = *reinterpret_cast<const u32x4 *>(room + row * (kChunks * 16) + (c ^ (row & 7)) * 16);
       const int64_t r = t.r0 + wr + row, col = t.c0 + wc + c * 8;
-      if (r < t.r1 && col < t.c1) *reinterpret_cast<u32x4 *>(static_cast<bf16_t *>(a.y) + out + r * a.ldy + col) = v;
-    }
-    return;
-  }
-  if (a.wide && t.c0 + 32 * FN <= t.c1) {   // every column exists
-#pragma unroll
-    for (int i = 0; i < FM; i++) {
-      if (row0 + i * 16 >= t.r1) break;
-      if (a.f32) {
-        float *y = static_cast<float *>(a.y) + at + i * 16 * a.ldy;
-#pragma unroll
-        for (int j = 0; j < FN; j++) *reinterpret_cast<f32x4 *>(y + j * 16) = s[i] * acc[i][j];
+      if (r >= t.r1 || col >= t.c1) continue;
+      bf16_t *y = static_cast<bf16_t *>(a.y) + out + r * a.ldy + col;
+      if (a.chunks) {
+        *reinterpret_cast<u32x4 *>(y) = v;
+      } else if (col + 8 <= t.c1) {
+        *reinterpret_cast<u32x4_a2 *>(y) = v;
       } else {
-        bf16_t *y = static_cast<bf16_t *>(a.y) + at + i * 16 * a.ldy;
 #pragma unroll
-        for (int j = 0; j < FN; j++) {
-          const f32x4 v = s[i] * acc[i][j];
-          *reinterpret_cast<uint2 *>(y + j * 16) = make_uint2(pack2(v[0], v[1]), pack2(v[2], v[3]));
-        }
+        for (int e = 0; e < 7; e++)
+          if (col + e < t.c1) y[e].v = (uint16_t)(v[e >> 1] >> (16 * (e & 1)));
       }
     }
     return;
   }
+  float *y = static_cast<float *>(a.y) + (MODE == kWeights ? (int64_t)t.expert * a.slice : 0) + row0 * a.ldy + col0;
 #pragma unroll
   for (int i = 0; i < FM; i++) {
     if (row0 + i * 16 >= t.r1) break;
 #pragma unroll
-    for (int j = 0; j < FN; j++) store4(a, at + i * 16 * a.ldy + j * 16, t.c1 - col0 - j * 16, s[i] * acc[i][j]);
+    for (int j = 0; j < FN; j++) {
+      const f32x4 v = s[i] * acc[i][j];
+      float *at = y + i * 16 * a.ldy + j * 16;
+      const int64_t n = t.c1 - col0 - j * 16;
+      if (n >= 4) {
+        *reinterpret_cast<f32x4_a4 *>(at) = v;
+      } else {
+#pragma unroll
+        for (int q = 0; q < 3; q++)
+          if (q < n) at[q] = v[q];
+      }
+    }
   }
 }
 
@@ -603,37 +605,43 @@ __global__ __launch_bounds__(256, FM * FN * KS >= 64 ? 1 : FM * FN == 8 ? 3 : 2)
 // the result is at least a tile wide, its last tile is moved back inside (its results are computed twice, from the same
 // numbers in the same order), so that all chunks but those at the end of the contraction are whole; else, and
 // there, chunks are loaded element by element.
-template <int MODE, int F>
+template <int MODE, int FM, int FN>
 __global__ __launch_bounds__(256, 2) void any_kernel(ProductArgs a) {
-  constexpr int B = 32 * F, kThreads = 256;
-  constexpr int kC = B * kBK / 8, kP = kC / kThreads, kBytes = kC * 16;
-  __shared__ u32x4 ta[2 * kC], tb[2 * kC];
+  constexpr int BM = 32 * FM, BN = 32 * FN, kThreads = 256;
+  constexpr int kCA = BM * kBK / 8, kCB = BN * kBK / 8, kPA = kCA / kThreads, kPB = kCB / kThreads;
+  static_assert(kPA * kThreads == kCA && kPB * kThreads == kCB, "whole chunks per thread");
+  __shared__ u32x4 lds[2 * kCA + 2 * kCB];
+  u32x4 *const ta = lds, *const tb = lds + 2 * kCA;
   __shared__ int32_t list[MODE == kWeights ? kList : 1];   // x's rows
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int wr = (wave >> 1) * (B / 2), wc = (wave & 1) * (B / 2);
+  const int wr = (wave >> 1) * (BM / 2), wc = (wave & 1) * (BN / 2);
   Tile t;
-  if (!take_tile<MODE, B, B>(a, &t)) return;
-  if (t.c0 + B > t.c1 && t.c1 >= B) t.c0 = t.c1 - B;
-  if (MODE == kWeights && t.r0 + B > t.r1 && t.r1 >= B) t.r0 = t.r1 - B;
-  const int K = t.K;
-  const bool inside = t.c0 + B <= t.c1 && (MODE != kWeights || t.r0 + B <= t.r1);
+  if (!take_tile<MODE, BM, BN>(a, &t)) return;
+  if (t.c0 + BN > t.c1 && t.c1 >= BN) t.c0 = t.c1 - BN;
+  if (MODE == kWeights && t.r0 + BM > t.r1 && t.r1 >= BM) t.r0 = t.r1 - BM;
+  int K = t.K, k_first = 0;   // this work-group's part of the contraction
+  if (MODE != kWeights && a.part) {
+    k_first = (int)blockIdx.y * a.part;
+    K = K - k_first < a.part ? (K > k_first ? K - k_first : 0) : a.part;
+  }
+  const bool inside = t.c0 + BN <= t.c1 && (MODE != kWeights || t.r0 + BM <= t.r1);
 
-  f32x4 acc[F][F];
+  f32x4 acc[FM][FN];
 #pragma unroll
-  for (int i = 0; i < F; i++)
+  for (int i = 0; i < FM; i++)
 #pragma unroll
-    for (int j = 0; j < F; j++) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int j = 0; j < FN; j++) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 
   // slots as in tile_kernel; na, nb: how many of the chunk's values are in the row
   const bf16_t *w = MODE == kWeights ? a.w + t.first * a.ldw : a.w + (int64_t)(K ? t.expert : 0) * a.slice;
-  const bf16_t *pa[kP], *pb[kP];
-  int ka[kP], kb[kP], na[kP], nb[kP];
+  const bf16_t *pa[kPA], *pb[kPB];
+  int ka[kPA], kb[kPB], na[kPA], nb[kPB];
   auto clip = [](int64_t x) { return (int)(x < 0 ? 0 : x > 8 ? 8 : x); };
 #pragma unroll
-  for (int i = 0; i < kP; i++) {
+  for (int i = 0; i < kPA; i++) {
     const int q = tid + i * kThreads;
     if (MODE == kWeights) {
-      const int row = q / (B / 8), c = (q % (B / 8)) ^ swizzle_t<B>(row);
+      const int row = q / (BM / 8), c = (q % (BM / 8)) ^ swizzle_t<BM>(row);
       ka[i] = row;
       na[i] = clip(t.r1 - (t.r0 + c * 8));
       pa[i] = a.x + t.r0 + c * 8;
@@ -642,70 +650,73 @@ __global__ __launch_bounds__(256, 2) void any_kernel(ProductArgs a) {
       const int64_t p = t.r0 + row < t.r1 ? t.r0 + row : t.r1 - 1;
       ka[i] = c * 8;
       na[i] = 8;
-      pa[i] = a.x + (K > 0 && a.gather ? (int64_t)(a.rows[p] / a.k) : p) * a.ldx + c * 8;
+      pa[i] = a.x + (K > 0 && a.gather ? (int64_t)(a.rows[p] / a.k) : p) * a.ldx + k_first + c * 8;
     }
+  }
+#pragma unroll
+  for (int i = 0; i < kPB; i++) {
+    const int q = tid + i * kThreads;
     if (MODE == kBackward) {
       const int row = q / 4, c = (q % 4) ^ swizzle_k<1>(row);
       kb[i] = c * 8;
       nb[i] = 8;
-      pb[i] = w + (t.c0 + row < t.c1 ? t.c0 + row : t.c1 - 1) * a.ldw + c * 8;
+      pb[i] = w + (t.c0 + row < t.c1 ? t.c0 + row : t.c1 - 1) * a.ldw + k_first + c * 8;
     } else {
-      const int row = q / (B / 8), c = (q % (B / 8)) ^ swizzle_t<B>(row);
+      const int row = q / (BN / 8), c = (q % (BN / 8)) ^ swizzle_t<BN>(row);
       kb[i] = row;
       nb[i] = clip(t.c1 - (t.c0 + c * 8));
-      pb[i] = w + row * a.ldw + t.c0 + c * 8;
+      pb[i] = w + (int64_t)(k_first + row) * a.ldw + t.c0 + c * 8;
     }
   }
   // kSets stages are on their way into registers, set by set
   constexpr int kSets = 3;
-  u32x4 ga[kSets][kP], gb[kSets][kP];
+  u32x4 ga[kSets][kPA], gb[kSets][kPB];
   int base = 0, end = 0;   // kWeights: the places in the list
   auto load = [&](auto SET, auto WHOLE, int k0) {
     const int64_t ob = MODE == kBackward ? k0 : k0 * a.ldw;
 #pragma unroll
-    for (int i = 0; i < kP; i++) {
-      if (WHOLE) {
-        const bf16_t *p = pa[i] + (MODE == kWeights ? list[k0 - base + ka[i]] * a.ldx : k0);
-        ga[SET][i] = *reinterpret_cast<const u32x4_a2 *>(p);
-        gb[SET][i] = *reinterpret_cast<const u32x4_a2 *>(pb[i] + ob);
-      } else {
-        const int la = end - k0 - ka[i], lb = end - k0 - kb[i];   // contraction values from this chunk on
-        const bf16_t *p = pa[i] + (MODE != kWeights ? k0 : la > 0 ? list[k0 - base + ka[i]] * a.ldx : 0);
-        ga[SET][i] = la > 0 ? load_chunk(p, MODE == kWeights ? na[i] : la) : u32x4{0, 0, 0, 0};
-        gb[SET][i] = lb > 0 ? load_chunk(pb[i] + ob, MODE == kBackward ? lb : nb[i]) : u32x4{0, 0, 0, 0};
-      }
+    for (int i = 0; i < kPA; i++) {
+      const int left = end - k0 - ka[i];   // contraction values from this chunk on
+      const bf16_t *p = pa[i] + (MODE != kWeights ? k0 : WHOLE || left > 0 ? list[k0 - base + ka[i]] * a.ldx : 0);
+      if (WHOLE) ga[SET][i] = *reinterpret_cast<const u32x4_a2 *>(p);
+      else ga[SET][i] = left > 0 ? load_chunk(p, MODE == kWeights ? na[i] : left) : u32x4{0, 0, 0, 0};
+    }
+#pragma unroll
+    for (int i = 0; i < kPB; i++) {
+      const int left = end - k0 - kb[i];
+      if (WHOLE) gb[SET][i] = *reinterpret_cast<const u32x4_a2 *>(pb[i] + ob);
+      else gb[SET][i] = left > 0 ? load_chunk(pb[i] + ob, MODE == kBackward ? left : nb[i]) : u32x4{0, 0, 0, 0};
     }
   };
   auto put_stage = [&](auto SET, int buf) {
 #pragma unroll
-    for (int i = 0; i < kP; i++) {
-      ta[buf * kC + tid + i * kThreads] = ga[SET][i];
-      tb[buf * kC + tid + i * kThreads] = gb[SET][i];
-    }
+    for (int i = 0; i < kPA; i++) ta[buf * kCA + tid + i * kThreads] = ga[SET][i];
+#pragma unroll
+    for (int i = 0; i < kPB; i++) tb[buf * kCB + tid + i * kThreads] = gb[SET][i];
   };
   FragK<1> ra_k(ta, wr), rb_k(tb, wc);
-  FragT<B, F> ra_t(ta, wr), rb_t(tb, wc);
+  FragT<BM, FM> ra_t(ta, wr);
+  FragT<BN, FN> rb_t(tb, wc);
   int buf = 0;   // the buffer of the stage that is multiplied
   // one stage: the next one goes from SET to the other buffer, and the stage at `ahead` is sent for into SET
   auto stage = [&](auto SET, auto WHOLE, int ahead) {
     __syncthreads();
     put_stage(SET, buf ^ 1);
     load(SET, WHOLE, ahead);
-    bf16x8 fa[F], fb[F];
+    bf16x8 fa[FM], fb[FN];
 #pragma unroll
-    for (int i = 0; i < F; i++) {
-      fa[i] = MODE == kWeights ? ra_t.get(0, i) : ra_k.get(0, i);
-      fb[i] = MODE == kBackward ? rb_k.get(0, i) : rb_t.get(0, i);
-    }
-    const int32_t across = buf ? -kBytes : kBytes;   // to the other buffer
-    if (MODE == kWeights) ra_t.move(across);
-    else ra_k.move(across);
-    if (MODE == kBackward) rb_k.move(across);
-    else rb_t.move(across);
+    for (int i = 0; i < FM; i++) fa[i] = MODE == kWeights ? ra_t.get(0, i) : ra_k.get(0, i);
 #pragma unroll
-    for (int i = 0; i < F; i++)
+    for (int i = 0; i < FN; i++) fb[i] = MODE == kBackward ? rb_k.get(0, i) : rb_t.get(0, i);
+    const int32_t by_a = buf ? -kCA * 16 : kCA * 16, by_b = buf ? -kCB * 16 : kCB * 16;   // to the other buffer
+    if (MODE == kWeights) ra_t.move(by_a);
+    else ra_k.move(by_a);
+    if (MODE == kBackward) rb_k.move(by_b);
+    else rb_t.move(by_b);
 #pragma unroll
-      for (int j = 0; j < F; j++)
+    for (int i = 0; i < FM; i++)
+#pragma unroll
+      for (int j = 0; j < FN; j++)
         acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[j], fa[i], acc[i][j], 0, 0, 0);
     buf ^= 1;
   };
@@ -740,15 +751,19 @@ __global__ __launch_bounds__(256, 2) void any_kernel(ProductArgs a) {
       if (k0 + 2 * kBK < end) stage(set0, any, k0 + 6 * kBK);
     }
   }
-  store_tile<MODE, F, F>(a, t, wr, wc, acc, nullptr);
+  if (MODE != kWeights && a.part) a.y = static_cast<float *>(a.y) + (int64_t)blockIdx.y * a.places * a.ldy;
+  __syncthreads();   // the buffers are no longer read
+  static_assert(FM * FN * 2048 <= (2 * kCA + 2 * kCB) * 16, "room for the results");
+  store_tile<MODE, FM, FN>(a, t, wr, wc, acc, reinterpret_cast<char *>(lds) + wave * (FM * FN * 512));
 }
 
+__host__ __device__ inline int64_t part_stride(int64_t cols) { return (cols + 3) / 4 * 4; }
 // Sums the parts of a contraction that several work-groups shared, in order: y[p] = s_p sum of part[i][p].
 __global__ __launch_bounds__(256) void join_kernel(ProductArgs a, const float *part, int parts, int64_t cols, int held_at) {
   const int64_t p = blockIdx.x, col = ((int64_t)blockIdx.y * 256 + threadIdx.x) * 4;
   if (col >= cols) return;
   f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
-  for (int i = 0; i < parts; i++) acc += *reinterpret_cast<const f32x4 *>(part + ((int64_t)i * a.places + p) * cols + col);
+  for (int i = 0; i < parts; i++) acc += *reinterpret_cast<const f32x4 *>(part + ((int64_t)i * a.places + p) * part_stride(cols) + col);
   if (a.scale && p < a.offsets[held_at]) acc *= a.scale[a.rows[p]];
   store4(a, p * a.ldy + col, cols - col, acc);
 }
@@ -784,7 +799,7 @@ Choice choose(const ProductArgs &a) {
   };
   constexpr int64_t kEnough = 512;   // two for each compute unit
   if (rows >= (MODE == kForward ? 384 : 256) && count(256, 256) >= kEnough) return {8, 8, 1};
-  if ((rows >= 64 || MODE == kWeights) && count(128, 256) >= kEnough) return {4, 8, 1};
+  if ((rows >= 64 || MODE == kWeights) && count(128, a.direct ? 256 : 128) >= kEnough) return {4, 8, 1};
   if (MODE == kWeights) return {2, 4, 1};
   const int64_t part_full = a.places / 64 + a.experts;   // row tiles with those that are not full
   const int64_t row_tiles = part_full < a.places ? part_full : a.places;
@@ -802,42 +817,42 @@ int launch_tile(ProductArgs a, int parts, void *stream) {
   tile_kernel<MODE, FM, FN, NS, KS><<<dim3((unsigned)grid, parts), 256, 0, static_cast<hipStream_t>(stream)>>>(a);
   return (int)hipGetLastError();
 }
-template <int MODE>
-int launch_any(ProductArgs a, void *stream) {
-  const int64_t grid = tiles<MODE>(a, 128, 128);
+template <int MODE, int FM, int FN>
+int launch_any(ProductArgs a, int parts, void *stream) {
+  const int64_t grid = tiles<MODE>(a, 32 * FM, 32 * FN);
   if (grid > 0x7FFFFFFF) return (int)hipErrorInvalidConfiguration;
-  any_kernel<MODE, 4><<<(unsigned)grid, 256, 0, static_cast<hipStream_t>(stream)>>>(a);
+  any_kernel<MODE, FM, FN><<<dim3((unsigned)grid, parts), 256, 0, static_cast<hipStream_t>(stream)>>>(a);
   return (int)hipGetLastError();
 }
 
 // Stages of two steps where W's rows run along the contraction: whole 128-byte lines of them.
 template <int MODE>
 int launch_mode(const ProductArgs &a, char *ws, void *stream) {
-  constexpr bool kTwo = MODE == kBackward;
-  if (!a.direct) return launch_any<MODE>(a, stream);
+  constexpr int kSteps = MODE == kBackward ? 2 : 1;
   const Choice c = choose<MODE>(a);
-  if (c.fm == 8) return launch_tile<MODE, 8, 8, kTwo ? 2 : 4, kTwo ? 2 : 1>(a, 1, stream);
-  if (c.fm == 4) return launch_tile<MODE, 4, 8, 3, kTwo ? 2 : 1>(a, 1, stream);
+  if (a.direct && c.fm == 8) return launch_tile<MODE, 8, 8, 4 / kSteps, kSteps>(a, 1, stream);
+  if (a.direct && c.fm == 4) return launch_tile<MODE, 4, 8, 3, kSteps>(a, 1, stream);
+  if (c.fm >= 4) return launch_any<MODE, 4, 4>(a, 1, stream);
   if constexpr (MODE != kWeights) {
-    if (c.fn == 8) return launch_tile<MODE, 2, 8, kTwo ? 2 : 4, kTwo ? 2 : 1>(a, 1, stream);
+    if (a.direct && c.fn == 8) return launch_tile<MODE, 2, 8, 4 / kSteps, kSteps>(a, 1, stream);
     if (c.parts > 1) {
       const int64_t cols = MODE == kBackward ? a.n : a.m, K = MODE == kForward ? a.n : a.m;
       ProductArgs b = a;
       b.part = (int32_t)(((K + c.parts - 1) / c.parts + 63) / 64 * 64);
       b.y = ws;
       b.scale = nullptr;
-      b.ldy = cols;
-      b.f32 = b.wide = 1;   // cols is a multiple of 8
+      b.ldy = part_stride(cols);
+      b.f32 = b.wide = 1;
       b.chunks = 0;
       const int parts = (int)((K + b.part - 1) / b.part);
-      const int e = launch_tile<MODE, 2, 4, kTwo ? 2 : 4, kTwo ? 2 : 1>(b, parts, stream);
+      const int e = a.direct ? launch_tile<MODE, 2, 4, 4 / kSteps, kSteps>(b, parts, stream) : launch_any<MODE, 2, 4>(b, parts, stream);
       if (e != (int)hipSuccess) return e;
       join_kernel<<<dim3((unsigned)a.places, (unsigned)((cols + 1023) / 1024)), 256, 0, static_cast<hipStream_t>(stream)>>>(
           a, reinterpret_cast<const float *>(ws), parts, cols, a.experts);
       return (int)hipGetLastError();
     }
   }
-  return launch_tile<MODE, 2, 4, kTwo ? 2 : 4, kTwo ? 2 : 1>(a, 1, stream);
+  return a.direct ? launch_tile<MODE, 2, 4, 4 / kSteps, kSteps>(a, 1, stream) : launch_any<MODE, 2, 4>(a, 1, stream);
 }
 
 ProductArgs args_of(const skew_rows &r, const skew_product_desc &p) {
@@ -883,7 +898,7 @@ size_t product_scratch(const skew_rows &r, const skew_product_desc &p) {
   const ProductArgs a = product_args(r, p);
   const bool back = (p.flags & SKEW_TRANSPOSE) != 0;
   const int parts = back ? choose<kBackward>(a).parts : choose<kForward>(a).parts;   // whatever the alignment
-  return parts > 1 ? (size_t)parts * (size_t)a.places * (size_t)(back ? a.n : a.m) * 4 : 0;
+  return parts > 1 ? (size_t)parts * (size_t)a.places * (size_t)part_stride(back ? a.n : a.m) * 4 : 0;
 }
 
 int launch_product(const skew_rows &r, const skew_product_desc &p, char *ws, void *stream) {
