@@ -7,7 +7,7 @@
 //   up to 64 items     one wave: an item's place is the number of items before it
 //   up to 4096 items   one work-group of 16 waves, all passes in LDS (a key and an index share 32 bits)
 //   more               per pass a histogram per work-group of 1024 to 4096 items and the scatter, whose work-groups
-//                      add up the histograms themselves up to 64 of them, or (beyond) find the sums in place of them
+//                      add up the histograms themselves up to 256 of them, or (beyond) find the sums in place of them
 // All of it is latency: 16384 places of 128 experts took 30 us in one work-group, 9 us in 16.
 #include "moe_internal.h"
 
@@ -18,7 +18,7 @@ constexpr int kThreads = 1024, kWaves = kThreads / 64;
 constexpr int kMaxSteps = 4;                        // items of a thread
 constexpr int64_t kOneGroup = kThreads * kMaxSteps;  // items that one work-group sorts in LDS
 constexpr int kIndexBits = 12;                       // of an index below kOneGroup
-constexpr int64_t kOwnSums = 64;                     // histograms that the scatter adds up itself
+constexpr int64_t kOwnSums = 256;                    // histograms that the scatter adds up itself
 }  // namespace
 
 SortPlan sort_plan(int64_t n, int64_t keys) {
@@ -247,22 +247,34 @@ __global__ __launch_bounds__(kThreads) void sort_scatter(const void *ids, int id
     const int64_t i = sort_item(steps, s);
     key[s] = s < steps && i < n ? (key_in ? key_in[i] : key_of(ids, id_bytes, i, keys)) : 0;
   }
-  for (int i = tid; i < kWaves * bins; i += kThreads) cnt[i] = 0;
-  // thread d: the digit's total and its count in the groups before
+  // thread d: the digit's total and its count in the groups before. Where sort_sums did not run, all threads add up,
+  // kThreads / bins of them a digit.
   uint32_t all = 0, before = 0;
-  if (tid < bins) {
-    if (total) {
+  if (total) {
+    if (tid < bins) {
       all = total[tid];
       before = hist[(int64_t)blockIdx.x * bins + tid];
-    } else {
-#pragma unroll 8
-      for (int b = 0; b < nb; b++) {
-        const uint32_t h = hist[(int64_t)b * bins + tid];
-        all += h;
-        before += b < (int)blockIdx.x ? h : 0;
-      }
     }
+  } else {
+    uint32_t *sums = cnt;   // 2 kThreads words
+#pragma unroll 8
+    for (int b = tid >> digit; b < nb; b += kThreads >> digit) {
+      const uint32_t h = hist[((int64_t)b << digit) + (tid & (bins - 1))];
+      all += h;
+      before += b < (int)blockIdx.x ? h : 0;
+    }
+    sums[tid] = all;
+    sums[kThreads + tid] = before;
+    __syncthreads();
+    all = before = 0;
+    if (tid < bins)
+      for (int i = tid; i < kThreads; i += bins) {
+        all += sums[i];
+        before += sums[kThreads + i];
+      }
+    __syncthreads();
   }
+  for (int i = tid; i < kWaves * bins; i += kThreads) cnt[i] = 0;
   const uint32_t start = block_exclusive(all, tmp);   // (its barrier also ends the clearing of cnt)
   if (offsets && blockIdx.x == 0 && tid <= (int)keys && tid < bins) offsets[tid] = (int32_t)start;
 #pragma unroll
@@ -284,7 +296,7 @@ __global__ __launch_bounds__(kThreads) void sort_scatter(const void *ids, int id
     if (s < steps && i < n) {
       const uint32_t at = cnt[w * bins + ((key[s] >> shift) & (bins - 1))] + rank[s];
       const int32_t j = idx_in ? idx_in[i] : (int32_t)i;
-      key_out[at] = key[s];
+      if (!rows || !offsets) key_out[at] = key[s];
       if (rows) {
         rows[at] = key[s] < keys ? j : -1;
         slots[j] = key[s] < keys ? (int32_t)at : -1;
@@ -335,7 +347,7 @@ int launch_sort(const SortPlan &p, const void *ids, int id_bytes, char *ws, Sort
     if (sums) sort_sums<<<1u << p.digit, 64, 0, s>>>(hist, p.nb, 1 << p.digit, total);
     sort_scatter<<<(unsigned)p.nb, kThreads, 0, s>>>(ids, id_bytes, key_in, idx_in, p.n, p.keys, p.steps, shift, p.digit,
                                                      hist, (int)p.nb, sums ? total : nullptr, key(to), idx(to),
-                                                     p.passes == 1 ? out->offsets : nullptr,
+                                                     p.passes == 1 ? out->offsets : nullptr,   // (then no one reads the keys)
                                                      last ? out->rows : nullptr, last ? out->slots : nullptr);
     key_in = key(to);
     idx_in = idx(to);

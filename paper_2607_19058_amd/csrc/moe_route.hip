@@ -131,17 +131,24 @@ __global__ __launch_bounds__(kThreads) void route_kernel(skew_route_desc d, cons
 #pragma unroll
       for (int v = 0; v < V; v++) top2(a1, a2, c[v], kClosed);
     }
-    for (int g = 0; g < d.groups; g++) {
-      float b1 = kClosed, b2 = kClosed;
-      if (whole_lanes) {
-        b1 = own == g ? a1 : kClosed;
-        b2 = own == g ? a2 : kClosed;
-      } else {
+    auto value = [&](float v1, float v2) { return d.group_sum == 2 && v2 != kClosed ? v1 + v2 : v1; };
+    const int lanes = per / V;
+    if (whole_lanes && (lanes & (lanes - 1)) == 0) {   // all groups at once: each is 1, 2, 4 .. lanes
+      for (int o = 1; o < lanes; o <<= 1) top2(a1, a2, __shfl_xor(a1, o), __shfl_xor(a2, o));
+      if (lane % lanes == 0 && own < d.groups) gval[slot][own] = value(a1, a2);
+    } else {
+      for (int g = 0; g < d.groups; g++) {
+        float b1 = kClosed, b2 = kClosed;
+        if (whole_lanes) {
+          b1 = own == g ? a1 : kClosed;
+          b2 = own == g ? a2 : kClosed;
+        } else {
 #pragma unroll
-        for (int v = 0; v < V; v++) top2(b1, b2, (unsigned)(e0 + v - g * per) < (unsigned)per ? c[v] : kClosed, kClosed);
+          for (int v = 0; v < V; v++) top2(b1, b2, (unsigned)(e0 + v - g * per) < (unsigned)per ? c[v] : kClosed, kClosed);
+        }
+        top2_over<L>(b1, b2);
+        if (lane == 0) gval[slot][g] = value(b1, b2);
       }
-      top2_over<L>(b1, b2);
-      if (lane == 0) gval[slot][g] = d.group_sum == 2 && b2 != kClosed ? b1 + b2 : b1;
     }
     __syncthreads();
     // a group is kept if fewer than top_groups are before it

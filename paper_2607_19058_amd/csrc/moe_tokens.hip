@@ -94,7 +94,7 @@ __global__ __launch_bounds__(kThreads) void embed_kernel(const I *ids, int64_t n
 // same id it is one part) into `part`, 2 rows of float a cut. Then a work-group per kIds rows of the table finds
 // their places, and a wave per row and 64 pieces adds the row's tokens, or its parts in order, scales once and
 // rounds once.
-constexpr int kRun = 32, kIds = 32;
+constexpr int kRun = 32, kIds = 16;
 
 // the first sorted place in [lo, hi) whose key is at least v, else hi
 __device__ __forceinline__ int64_t lower_bound(const uint32_t *key, int64_t lo, int64_t hi, uint32_t v) {
