@@ -219,16 +219,17 @@ inline int64_t patches(int64_t rows, int64_t cols) {
 inline int64_t patch_grid(int64_t rows, int64_t cols, bool in_patches) {
   return in_patches ? (patches(rows, cols) + kDies - 1) / kDies * kDies * (kPatchR * kPatchC) : rows * cols;
 }
-__device__ __forceinline__ bool patch_tile(bool in_patches, int64_t rows, int64_t cols, int64_t *row, int64_t *col) {
+__device__ __forceinline__ bool patch_tile(bool in_patches, uint32_t rows, uint32_t cols, uint32_t *row, uint32_t *col) {
   if (!in_patches) {
-    *row = blockIdx.x / (uint32_t)cols;
-    *col = blockIdx.x % (uint32_t)cols;
+    *row = blockIdx.x / cols;
+    *col = blockIdx.x - *row * cols;
     return true;
   }
   const uint32_t i = blockIdx.x / kDies, in = i % (kPatchR * kPatchC);
-  const uint32_t patch = i / (kPatchR * kPatchC) * kDies + blockIdx.x % kDies, pc = (uint32_t)((cols + kPatchC - 1) / kPatchC);
-  *row = (int64_t)(patch / pc) * kPatchR + in % kPatchR;
-  *col = (int64_t)(patch % pc) * kPatchC + in / kPatchR;
+  const uint32_t patch = i / (kPatchR * kPatchC) * kDies + blockIdx.x % kDies, pc = (cols + kPatchC - 1) / kPatchC;
+  const uint32_t pr = patch / pc;
+  *row = pr * kPatchR + in % kPatchR;
+  *col = (patch - pr * pc) * kPatchC + in / kPatchR;
   return *row < rows && *col < cols;
 }
 
@@ -250,26 +251,27 @@ struct Tile {
 };
 template <int MODE, int BM, int BN>
 __device__ __forceinline__ bool take_tile(const ProductArgs &a, Tile *t) {
-  int64_t tr, tc;
+  uint32_t tr, tc;   // (the grid has fewer than 2^31 tiles)
   t->first = 0;
+  t->c1 = MODE == kBackward ? a.n : a.m;
+  const uint32_t cols = ((uint32_t)t->c1 + BN - 1) / BN;
   if (MODE == kWeights) {
-    const int64_t tn = (a.n + BM - 1) / BM, tm = (a.m + BN - 1) / BN;
-    if (!patch_tile(a.in_patches, a.experts * tn, tm, &tr, &tc)) return false;
-    t->expert = (int)(tr / tn);
-    t->r0 = tr % tn * BM;
+    const uint32_t tn = ((uint32_t)a.n + BM - 1) / BM;
+    if (!patch_tile(a.in_patches, a.experts * tn, cols, &tr, &tc)) return false;
+    t->expert = __builtin_amdgcn_readfirstlane(tr / tn);
+    t->r0 = (int64_t)(tr - t->expert * tn) * BM;
     t->r1 = a.n;
-    t->c1 = a.m;
     t->first = a.offsets[t->expert];
     t->K = __builtin_amdgcn_readfirstlane(a.offsets[t->expert + 1] - (int)t->first);
   } else {
-    t->c1 = MODE == kForward ? a.m : a.n;
-    if (!patch_tile(a.in_patches, a.row_tiles, (t->c1 + BN - 1) / BN, &tr, &tc) || !find_tile<BM>(a, tr, &t->expert, &t->r0, &t->r1)) return false;
+    if (!patch_tile(a.in_patches, (uint32_t)a.row_tiles, cols, &tr, &tc) || !find_tile<BM>(a, tr, &t->expert, &t->r0, &t->r1))
+      return false;
     t->expert = __builtin_amdgcn_readfirstlane(t->expert);   // the same in every lane, but found in a loop over lanes
     t->r0 = scalar(t->r0);
     t->r1 = scalar(t->r1);
     t->K = t->expert < a.experts ? (int)(MODE == kForward ? a.n : a.m) : 0;   // the places without a pair: zeros
   }
-  t->c0 = tc * BN;
+  t->c0 = (int64_t)tc * BN;
   return true;
 }
 
@@ -302,22 +304,26 @@ __device__ __forceinline__ void store_tile(const ProductArgs &a, const Tile &t, 
             make_uint2(pack2(v[0], v[1]), pack2(v[2], v[3]));
       }
     __builtin_amdgcn_wave_barrier();
-    const int64_t out = (MODE == kWeights ? (int64_t)t.expert * a.slice : 0);
+    constexpr int kRows = 64 / kChunks;   // rows of one store
+    const int c = lane % kChunks, row_in = lane / kChunks;
+    const int64_t col = t.c0 + wc + c * 8, left = t.r1 - (t.r0 + wr);
+    const int rows = left < 16 * FM ? (int)left : 16 * FM, n = (int)(t.c1 - col < 8 ? t.c1 - col : 8);   // of the wave's; of the lane's 8 columns
+    bf16_t *y = static_cast<bf16_t *>(a.y) + (MODE == kWeights ? (int64_t)t.expert * a.slice : 0) +
+                (t.r0 + wr + row_in) * a.ldy + col;
+    const int64_t step = kRows * a.ldy;
 #pragma unroll
-    for (int n = 0; n < FM * FN / 2; n++) {
-      const int q = n * 64 + lane, row = q / kChunks, c = q % kChunks;
+    for (int i = 0; i < 16 * FM / kRows; i++, y += step) {
+      const int row = i * kRows + row_in;
       const u32x4 v = *reinterpret_cast<const u32x4 *>(room + row * (kChunks * 16) + (c ^ (row & 7)) * 16);
-      const int64_t r = t.r0 + wr + row, col = t.c0 + wc + c * 8;
-      if (r >= t.r1 || col >= t.c1) continue;
-      bf16_t *y = static_cast<bf16_t *>(a.y) + out + r * a.ldy + col;
+      if (row >= rows || n <= 0) continue;
       if (a.chunks) {
         *reinterpret_cast<u32x4 *>(y) = v;
-      } else if (col + 8 <= t.c1) {
+      } else if (n == 8) {
         *reinterpret_cast<u32x4_a2 *>(y) = v;
       } else {
 #pragma unroll
         for (int e = 0; e < 7; e++)
-          if (col + e < t.c1) y[e].v = (uint16_t)(v[e >> 1] >> (16 * (e & 1)));
+          if (e < n) y[e].v = (uint16_t)(v[e >> 1] >> (16 * (e & 1)));
       }
     }
     return;
