@@ -611,12 +611,13 @@ __global__ __launch_bounds__(256, FM * FN * KS >= 64 ? 1 : FM * FN == 8 ? 3 : 2)
 // the result is at least a tile wide, its last tile is moved back inside (its results are computed twice, from the same
 // numbers in the same order), so that all chunks but those at the end of the contraction are whole; else, and
 // there, chunks are loaded element by element.
-template <int MODE, int FM, int FN>
+template <int MODE, int FM, int FN, int kSets>
 __global__ __launch_bounds__(256, 2) void any_kernel(ProductArgs a) {
   constexpr int BM = 32 * FM, BN = 32 * FN, kThreads = 256;
   constexpr int kCA = BM * kBK / 8, kCB = BN * kBK / 8, kPA = kCA / kThreads, kPB = kCB / kThreads;
   static_assert(kPA * kThreads == kCA && kPB * kThreads == kCB, "whole chunks per thread");
-  __shared__ u32x4 lds[2 * kCA + 2 * kCB];
+  constexpr int kRoom = FM * FN * 128;   // chunks of the tile's bf16 results
+  __shared__ u32x4 lds[kRoom > 2 * kCA + 2 * kCB ? kRoom : 2 * kCA + 2 * kCB];
   u32x4 *const ta = lds, *const tb = lds + 2 * kCA;
   __shared__ int32_t list[MODE == kWeights ? kList : 1];   // x's rows
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -675,7 +676,6 @@ __global__ __launch_bounds__(256, 2) void any_kernel(ProductArgs a) {
     }
   }
   // kSets stages are on their way into registers, set by set
-  constexpr int kSets = 3;
   u32x4 ga[kSets][kPA], gb[kSets][kPB];
   int base = 0, end = 0;   // kWeights: the places in the list
   auto load = [&](auto SET, auto WHOLE, int k0) {
@@ -728,7 +728,7 @@ __global__ __launch_bounds__(256, 2) void any_kernel(ProductArgs a) {
   };
   const std::integral_constant<int, 0> set0;
   const std::integral_constant<int, 1> set1;
-  const std::integral_constant<int, 2> set2;
+  const std::integral_constant<int, kSets - 1> last_set;
   const std::true_type whole;
   const std::false_type any;
   for (; base < K; base = end) {   // kWeights: rounds of the places in the list
@@ -741,25 +741,24 @@ __global__ __launch_bounds__(256, 2) void any_kernel(ProductArgs a) {
     }
     load(set0, any, base);
     load(set1, any, base + kBK);
-    load(set2, any, base + 2 * kBK);
+    if (kSets == 3) load(last_set, any, base + 2 * kBK);
     put_stage(set0, buf);
-    load(set0, any, base + 3 * kBK);
+    load(set0, any, base + kSets * kBK);
+    // a round of kSets stages; each sends for the stage kSets + 1 further on
+    auto round = [&](auto WHOLE, int k0) {
+      stage(set1, WHOLE, k0 + (kSets + 1) * kBK);
+      if (WHOLE || k0 + kBK < end) {
+        if (kSets == 3) stage(last_set, WHOLE, k0 + (kSets + 2) * kBK);
+        else stage(set0, WHOLE, k0 + (kSets + 2) * kBK);
+      }
+      if (kSets == 3 && (WHOLE || k0 + 2 * kBK < end)) stage(set0, WHOLE, k0 + (kSets + 3) * kBK);
+    };
     int k0 = base;
     if (inside)
-      for (; k0 + 7 * kBK <= end; k0 += 3 * kBK) {   // sends for three whole stages
-        stage(set1, whole, k0 + 4 * kBK);
-        stage(set2, whole, k0 + 5 * kBK);
-        stage(set0, whole, k0 + 6 * kBK);
-      }
-    for (; k0 < end; k0 += 3 * kBK) {
-      stage(set1, any, k0 + 4 * kBK);
-      if (k0 + kBK < end) stage(set2, any, k0 + 5 * kBK);
-      if (k0 + 2 * kBK < end) stage(set0, any, k0 + 6 * kBK);
-    }
+      for (; k0 + (2 * kSets + 1) * kBK <= end; k0 += kSets * kBK) round(whole, k0);
+    for (; k0 < end; k0 += kSets * kBK) round(any, k0);
   }
-  if (MODE != kWeights && a.part) a.y = static_cast<float *>(a.y) + (int64_t)blockIdx.y * a.places * a.ldy;
   __syncthreads();   // the buffers are no longer read
-  static_assert(FM * FN * 2048 <= (2 * kCA + 2 * kCB) * 16, "room for the results");
   store_tile<MODE, FM, FN>(a, t, wr, wc, acc, reinterpret_cast<char *>(lds) + wave * (FM * FN * 512));
 }
 
@@ -805,7 +804,7 @@ Choice choose(const ProductArgs &a) {
   };
   constexpr int64_t kEnough = 512;   // two for each compute unit
   if (rows >= (MODE == kForward ? 384 : 256) && count(256, 256) >= kEnough) return {8, 8, 1};
-  if ((rows >= 64 || MODE == kWeights) && count(128, a.direct ? 256 : 128) >= kEnough) return {4, 8, 1};
+  if ((rows >= 64 || MODE == kWeights) && count(128, 256) >= (a.direct ? kEnough : kEnough / 2)) return {4, 8, 1};
   if (MODE == kWeights) return {2, 4, 1};
   const int64_t part_full = a.places / 64 + a.experts;   // row tiles with those that are not full
   const int64_t row_tiles = part_full < a.places ? part_full : a.places;
@@ -823,11 +822,11 @@ int launch_tile(ProductArgs a, int parts, void *stream) {
   tile_kernel<MODE, FM, FN, NS, KS><<<dim3((unsigned)grid, parts), 256, 0, static_cast<hipStream_t>(stream)>>>(a);
   return (int)hipGetLastError();
 }
-template <int MODE, int FM, int FN>
+template <int MODE, int FM, int FN, int kSets>
 int launch_any(ProductArgs a, int parts, void *stream) {
   const int64_t grid = tiles<MODE>(a, 32 * FM, 32 * FN);
   if (grid > 0x7FFFFFFF) return (int)hipErrorInvalidConfiguration;
-  any_kernel<MODE, FM, FN><<<dim3((unsigned)grid, parts), 256, 0, static_cast<hipStream_t>(stream)>>>(a);
+  any_kernel<MODE, FM, FN, kSets><<<dim3((unsigned)grid, parts), 256, 0, static_cast<hipStream_t>(stream)>>>(a);
   return (int)hipGetLastError();
 }
 
@@ -838,7 +837,7 @@ int launch_mode(const ProductArgs &a, char *ws, void *stream) {
   const Choice c = choose<MODE>(a);
   if (a.direct && c.fm == 8) return launch_tile<MODE, 8, 8, 4 / kSteps, kSteps>(a, 1, stream);
   if (a.direct && c.fm == 4) return launch_tile<MODE, 4, 8, 3, kSteps>(a, 1, stream);
-  if (c.fm >= 4) return launch_any<MODE, 4, 4>(a, 1, stream);
+  if (c.fm >= 4) return launch_any<MODE, 4, 8, 2>(a, 1, stream);
   if constexpr (MODE != kWeights) {
     if (a.direct && c.fn == 8) return launch_tile<MODE, 2, 8, 4 / kSteps, kSteps>(a, 1, stream);
     if (c.parts > 1) {
@@ -851,14 +850,14 @@ int launch_mode(const ProductArgs &a, char *ws, void *stream) {
       b.f32 = b.wide = 1;
       b.chunks = 0;
       const int parts = (int)((K + b.part - 1) / b.part);
-      const int e = a.direct ? launch_tile<MODE, 2, 4, 4 / kSteps, kSteps>(b, parts, stream) : launch_any<MODE, 2, 4>(b, parts, stream);
+      const int e = a.direct ? launch_tile<MODE, 2, 4, 4 / kSteps, kSteps>(b, parts, stream) : launch_any<MODE, 2, 4, 3>(b, parts, stream);
       if (e != (int)hipSuccess) return e;
       join_kernel<<<dim3((unsigned)a.places, (unsigned)((cols + 1023) / 1024)), 256, 0, static_cast<hipStream_t>(stream)>>>(
           a, reinterpret_cast<const float *>(ws), parts, cols, a.experts);
       return (int)hipGetLastError();
     }
   }
-  return a.direct ? launch_tile<MODE, 2, 4, 4 / kSteps, kSteps>(a, 1, stream) : launch_any<MODE, 2, 4>(a, 1, stream);
+  return a.direct ? launch_tile<MODE, 2, 4, 4 / kSteps, kSteps>(a, 1, stream) : launch_any<MODE, 2, 4, 3>(a, 1, stream);
 }
 
 ProductArgs args_of(const skew_rows &r, const skew_product_desc &p) {
