@@ -32,8 +32,8 @@ struct ProductArgs {
   int64_t ldx, ldw, slice, ldy;   // kWeights: ldw is d's row stride, ldy and slice are dW's
   int64_t n, m, places;           // n x m weights
   int32_t k, experts, gather, f32;
-  int32_t direct;                 // 16-byte rows in both operands and lengths that are multiples of 8
-  int32_t wide, chunks;           // 4 neighbouring results can be stored together; 8, and none of them is past the edge
+  int32_t direct;                 // 16-byte rows in both operands (and in a bf16 result), lengths that are multiples of 8
+  int32_t wide;                   // 4 neighbouring results can be stored together
   int64_t row_tiles;              // forward, backward: tiles of rows in the grid
   int32_t in_patches;             // how tiles are given out (patch_tile)
   int32_t part;                   // forward, backward: contraction length of a work-group (a multiple of its stages)
@@ -279,7 +279,7 @@ __device__ __forceinline__ bool take_tile(const ProductArgs &a, Tile *t) {
 // lane % 16 of each block and its columns 4 (lane / 16) .. + 3.
 // bf16 results go through `room` (FM FN 512 bytes of LDS of this wave's own), so that a row's 32 FN bytes leave
 // together: 8-byte stores of 16 rows at once reached 3.1 TB/s on a gradient that is all output.
-template <int MODE, int FM, int FN>
+template <int MODE, int FM, int FN, bool CHUNKS>
 __device__ __forceinline__ void store_tile(const ProductArgs &a, const Tile &t, int wr, int wc, const f32x4 (&acc)[FM][FN],
                                            char *room) {
   const int lane = threadIdx.x & 63;
@@ -292,7 +292,7 @@ __device__ __forceinline__ void store_tile(const ProductArgs &a, const Tile &t, 
     for (int i = 0; i < FM; i++)
       if (row0 + i * 16 < t.r1) s[i] = a.scale[a.rows[row0 + i * 16]];
   }
-  if (!a.f32) {
+  if (MODE == kWeights || !a.f32) {
     constexpr int kChunks = 2 * FN;   // of a row, placed with their index xor-ed with the row
 #pragma unroll
     for (int i = 0; i < FM; i++)
@@ -311,14 +311,23 @@ __device__ __forceinline__ void store_tile(const ProductArgs &a, const Tile &t, 
     bf16_t *y = static_cast<bf16_t *>(a.y) + (MODE == kWeights ? (int64_t)t.expert * a.slice : 0) +
                 (t.r0 + wr + row_in) * a.ldy + col;
     const int64_t step = kRows * a.ldy;
+    auto read = [&](int i) {
+      const int row = i * kRows + row_in;
+      return *reinterpret_cast<const u32x4 *>(room + row * (kChunks * 16) + (c ^ (row & 7)) * 16);
+    };
+    if (CHUNKS) {   // not a case of the loop below: its reads wait for each other, and its code is in the registers' way
+#pragma unroll
+      for (int i = 0; i < 16 * FM / kRows; i++, y += step) {
+        const u32x4 v = read(i);
+        if (i * kRows + row_in < rows && n > 0) *reinterpret_cast<u32x4 *>(y) = v;
+      }
+      return;
+    }
 #pragma unroll
     for (int i = 0; i < 16 * FM / kRows; i++, y += step) {
-      const int row = i * kRows + row_in;
-      const u32x4 v = *reinterpret_cast<const u32x4 *>(room + row * (kChunks * 16) + (c ^ (row & 7)) * 16);
-      if (row >= rows || n <= 0) continue;
-      if (a.chunks) {
-        *reinterpret_cast<u32x4 *>(y) = v;
-      } else if (n == 8) {
+      const u32x4 v = read(i);
+      if (i * kRows + row_in >= rows || n <= 0) continue;
+      if (n == 8) {
         *reinterpret_cast<u32x4_a2 *>(y) = v;
       } else {
 #pragma unroll
@@ -603,7 +612,7 @@ __global__ __launch_bounds__(256, FM * FN * KS >= 64 ? 1 : FM * FN == 8 ? 3 : 2)
   }
   if (kInA) mfma_done();
   if (MODE != kWeights && a.part) a.y = static_cast<float *>(a.y) + (int64_t)blockIdx.y * a.places * a.ldy;
-  store_tile<MODE, FM, FN>(a, t, wr, wc, acc, reinterpret_cast<char *>(lds) + wave * (FM * FN * 512));
+  store_tile<MODE, FM, FN, true>(a, t, wr, wc, acc, reinterpret_cast<char *>(lds) + wave * (FM * FN * 512));
 }
 
 // ---- tiles of any shape ---------------------------------------------------------------------
@@ -758,8 +767,9 @@ __global__ __launch_bounds__(256, 2) void any_kernel(ProductArgs a) {
       for (; k0 + (2 * kSets + 1) * kBK <= end; k0 += kSets * kBK) round(whole, k0);
     for (; k0 < end; k0 += kSets * kBK) round(any, k0);
   }
+  if (MODE != kWeights && a.part) a.y = static_cast<float *>(a.y) + (int64_t)blockIdx.y * a.places * a.ldy;
   __syncthreads();   // the buffers are no longer read
-  store_tile<MODE, FM, FN>(a, t, wr, wc, acc, reinterpret_cast<char *>(lds) + wave * (FM * FN * 512));
+  store_tile<MODE, FM, FN, false>(a, t, wr, wc, acc, reinterpret_cast<char *>(lds) + wave * (FM * FN * 512));
 }
 
 __host__ __device__ inline int64_t part_stride(int64_t cols) { return (cols + 3) / 4 * 4; }
@@ -848,7 +858,6 @@ int launch_mode(const ProductArgs &a, char *ws, void *stream) {
       b.scale = nullptr;
       b.ldy = part_stride(cols);
       b.f32 = b.wide = 1;
-      b.chunks = 0;
       const int parts = (int)((K + b.part - 1) / b.part);
       const int e = a.direct ? launch_tile<MODE, 2, 4, 4 / kSteps, kSteps>(b, parts, stream) : launch_any<MODE, 2, 4, 3>(b, parts, stream);
       if (e != (int)hipSuccess) return e;
@@ -894,7 +903,7 @@ ProductArgs product_args(const skew_rows &r, const skew_product_desc &p) {
   a.direct = chunks(a.x, a.ldx) && chunks(a.w, a.ldw) && a.slice % 8 == 0 && a.n % 8 == 0 && a.m % 8 == 0 &&
              short_rows(a.gather ? r.tokens : kMaxTile, a.ldx) && short_rows(kMaxTile, a.ldw);
   a.wide = ((uintptr_t)a.y & 15) == 0 && a.ldy % 4 == 0;
-  a.chunks = a.wide && a.ldy % 8 == 0 && (p.flags & SKEW_TRANSPOSE ? a.n : a.m) % 8 == 0;
+  if (!a.f32) a.direct = a.direct && a.wide && a.ldy % 8 == 0;
   return a;
 }
 
@@ -921,7 +930,7 @@ int launch_product_grad(const skew_rows &r, const skew_product_desc &p, void *st
   a.direct = chunks(a.x, a.ldx) && chunks(a.w, a.ldw) && a.n % 8 == 0 && a.m % 8 == 0 &&
              short_rows(a.gather ? r.tokens : a.places, a.ldx) && short_rows(kMaxTile, a.ldw);
   a.wide = ((uintptr_t)a.y & 15) == 0 && a.ldy % 4 == 0 && a.slice % 4 == 0;
-  a.chunks = a.wide && a.ldy % 8 == 0 && a.slice % 8 == 0 && a.m % 8 == 0;
+  a.direct = a.direct && a.wide && a.ldy % 8 == 0 && a.slice % 8 == 0;
   return launch_mode<kWeights>(a, nullptr, stream);
 }
 
