@@ -118,6 +118,14 @@ int skew_expert_matmul(const skew_rows *r, const skew_product_desc *p, void *wor
  * Errors: SKEW_EINVAL, SKEW_EHIP. */
 int skew_expert_matmul_grad(const skew_rows *r, const skew_product_desc *p, void *stream);
 
+/* The same with d in float32 (ldy in floats). The matrix cores take it as the sum of two bf16 numbers,
+ * which leaves out at most 2^-16 of a value; the contraction is twice as long, so it takes up to twice the time.
+ * tokens * k < 2^30. skew_expert_matmul_grad_f32_bytes() gives the scratch (host only; it depends on
+ * shapes alone). Errors: SKEW_EINVAL, SKEW_ENOSPACE, SKEW_EHIP. */
+int skew_expert_matmul_grad_f32_bytes(const skew_rows *r, const skew_product_desc *p, size_t *bytes);
+int skew_expert_matmul_grad_f32(const skew_rows *r, const skew_product_desc *p, void *workspace,
+                                size_t workspace_bytes, void *stream);
+
 /* out[t] = sum over t's choices j of weights[t, j] y[place of (t, j)] (weights NULL: 1). A token without
  * experts gets zeros. y: tokens * k rows of m in y_dtype; out: tokens rows in out_dtype.
  * Errors: SKEW_EINVAL, SKEW_EHIP. */
@@ -130,6 +138,12 @@ int skew_expert_combine(const skew_rows *r, const void *y, int32_t y_dtype, int6
 int skew_expert_combine_backward(const skew_rows *r, const void *dout, int64_t ldo, const void *y, int32_t y_dtype,
                                  int64_t ldy, const float *weights, void *dy, int64_t lddy, float *dweights,
                                  int64_t m, void *stream);
+
+/* The same with dy in float32, for a gradient of the weights that is rounded once:
+ * skew_expert_matmul_grad_f32() takes these rows as they are. */
+int skew_expert_combine_backward_f32(const skew_rows *r, const void *dout, int64_t ldo, const void *y, int32_t y_dtype,
+                                     int64_t ldy, const float *weights, float *dy, int64_t lddy, float *dweights,
+                                     int64_t m, void *stream);
 
 /* Rows of an embedding table. ids: int32 or int64 (id_bytes 4 or 8) [tokens]; an id outside
  * [0, vocab) is no token: its row of `out` is zero and it adds nothing to the gradient.

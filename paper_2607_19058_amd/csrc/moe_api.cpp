@@ -116,6 +116,22 @@ int skew_expert_matmul_grad(const skew_rows *r, const skew_product_desc *p, void
   return status(launch_product_grad(*r, *p, stream));
 }
 
+int skew_expert_matmul_grad_f32_bytes(const skew_rows *r, const skew_product_desc *p, size_t *bytes) {
+  if (!product_ok(r, p, true) || r->tokens * r->k > kMaxPlaces / 2 || bytes == nullptr) return SKEW_EINVAL;
+  *bytes = product_grad_f32_scratch(*r, *p);
+  return SKEW_OK;
+}
+
+int skew_expert_matmul_grad_f32(const skew_rows *r, const skew_product_desc *p, void *workspace,
+                                size_t workspace_bytes, void *stream) {
+  if (!product_ok(r, p, true) || r->tokens * r->k > kMaxPlaces / 2 || p->w == nullptr) return SKEW_EINVAL;
+  if (r->tokens == 0) return status(launch_product_grad(*r, *p, stream));   // (d is not read)
+  if (p->x == nullptr || p->y == nullptr) return SKEW_EINVAL;
+  if (workspace_bytes < product_grad_f32_scratch(*r, *p)) return SKEW_ENOSPACE;
+  if (workspace == nullptr) return SKEW_EINVAL;
+  return status(launch_product_grad_f32(*r, *p, static_cast<char *>(workspace), stream));
+}
+
 int skew_expert_combine(const skew_rows *r, const void *y, int32_t y_dtype, int64_t ldy, const float *weights,
                         void *out, int32_t out_dtype, int64_t ldo, int64_t m, void *stream) {
   if (!rows_ok(r) || !type_ok(y_dtype) || !type_ok(out_dtype) || !cols_ok(m)) return SKEW_EINVAL;
@@ -125,15 +141,29 @@ int skew_expert_combine(const skew_rows *r, const void *y, int32_t y_dtype, int6
   return status(launch_combine(*r, y, y_dtype, ldy, weights, out, out_dtype, ldo, m, stream));
 }
 
-int skew_expert_combine_backward(const skew_rows *r, const void *dout, int64_t ldo, const void *y, int32_t y_dtype,
-                                 int64_t ldy, const float *weights, void *dy, int64_t lddy, float *dweights,
-                                 int64_t m, void *stream) {
+namespace {
+int combine_backward(const skew_rows *r, const void *dout, int64_t ldo, const void *y, int32_t y_dtype, int64_t ldy,
+                     const float *weights, void *dy, int dy_dtype, int64_t lddy, float *dweights, int64_t m,
+                     void *stream) {
   if (!rows_ok(r) || !type_ok(y_dtype) || !cols_ok(m)) return SKEW_EINVAL;
   const int64_t places = r->tokens * r->k;
   if (!ld_ok(ldo, m, r->tokens) || !ld_ok(ldy, m, places) || !ld_ok(lddy, m, places)) return SKEW_EINVAL;
   if (r->tokens == 0) return SKEW_OK;
   if (dout == nullptr || y == nullptr || dy == nullptr || dweights == nullptr) return SKEW_EINVAL;
-  return status(launch_combine_backward(*r, dout, ldo, y, y_dtype, ldy, weights, dy, lddy, dweights, m, stream));
+  return status(launch_combine_backward(*r, dout, ldo, y, y_dtype, ldy, weights, dy, dy_dtype, lddy, dweights, m, stream));
+}
+}  // namespace
+
+int skew_expert_combine_backward(const skew_rows *r, const void *dout, int64_t ldo, const void *y, int32_t y_dtype,
+                                 int64_t ldy, const float *weights, void *dy, int64_t lddy, float *dweights,
+                                 int64_t m, void *stream) {
+  return combine_backward(r, dout, ldo, y, y_dtype, ldy, weights, dy, SKEW_BF16, lddy, dweights, m, stream);
+}
+
+int skew_expert_combine_backward_f32(const skew_rows *r, const void *dout, int64_t ldo, const void *y, int32_t y_dtype,
+                                     int64_t ldy, const float *weights, float *dy, int64_t lddy, float *dweights,
+                                     int64_t m, void *stream) {
+  return combine_backward(r, dout, ldo, y, y_dtype, ldy, weights, dy, SKEW_F32, lddy, dweights, m, stream);
 }
 
 int skew_embed(const void *ids, int32_t id_bytes, int64_t tokens, const void *table, int64_t vocab, int64_t cols,

@@ -47,8 +47,8 @@ int launch_route_backward(const skew_route_desc &d, const void *logits, const in
 int launch_combine(const skew_rows &r, const void *y, int y_dtype, int64_t ldy, const float *weights, void *out,
                    int out_dtype, int64_t ldo, int64_t m, void *stream);
 int launch_combine_backward(const skew_rows &r, const void *dout, int64_t ldo, const void *y, int y_dtype,
-                            int64_t ldy, const float *weights, void *dy, int64_t lddy, float *dweights, int64_t m,
-                            void *stream);
+                            int64_t ldy, const float *weights, void *dy, int dy_dtype, int64_t lddy, float *dweights,
+                            int64_t m, void *stream);
 
 size_t embed_scratch(int64_t n, int64_t cols);   // partial sums of skew_embed_grad
 int launch_embed(const void *ids, int id_bytes, int64_t n, const void *table, int64_t vocab, int64_t cols, int64_t ldt,
@@ -59,6 +59,8 @@ int launch_embed_grad(const SortOut &s, int64_t n, const void *dout, int64_t ldo
 size_t product_scratch(const skew_rows &r, const skew_product_desc &p);
 int launch_product(const skew_rows &r, const skew_product_desc &p, char *ws, void *stream);
 int launch_product_grad(const skew_rows &r, const skew_product_desc &p, void *stream);
+size_t product_grad_f32_scratch(const skew_rows &r, const skew_product_desc &p);
+int launch_product_grad_f32(const skew_rows &r, const skew_product_desc &p, char *ws, void *stream);
 
 }  // namespace moe
 

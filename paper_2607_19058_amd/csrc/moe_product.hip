@@ -791,6 +791,41 @@ __global__ __launch_bounds__(256) void join_kernel(ProductArgs a, const float *p
   store4(a, p * a.ldy + col, cols - col, acc);
 }
 
+// d (float32) for the weights' gradient: a row of d becomes two of bf16, d = high + low up to 2^-16 of a value (high is
+// d's upper half, cut off; low, the rest, is exact before its own rounding). An expert's rows of high come before those of
+// low, so with the rows of x named twice the product of twice as many places is the gradient.
+//   offsets2[e] = 2 offsets[e];  place q of the 2 held: row rows2[q] of x and row q of d2.
+// Infinities and NaN are in high alone. 16 KB in and out a place of 2048 columns: bound by memory.
+__global__ __launch_bounds__(256) void split_kernel(ProductArgs a, const float *d, int64_t ldd, int32_t *offsets2,
+                                                    int32_t *rows2, bf16_t *d2, int64_t ld2) {
+  const int tid = threadIdx.x;
+  if (blockIdx.x == 0)
+    for (int e = tid; e <= a.experts; e += 256) offsets2[e] = 2 * a.offsets[e];
+  const int32_t held = a.offsets[a.experts];
+  for (int64_t p = blockIdx.x; p < held; p += gridDim.x) {
+    int e = 0, end = a.experts;   // the last expert that begins at p or before holds it
+    while (end - e > 1) {
+      const int mid = (e + end) >> 1;
+      if (a.offsets[mid] <= p) e = mid;
+      else end = mid;
+    }
+    const int64_t high = a.offsets[e] + p, low = a.offsets[e + 1] + p;
+    if (tid == 0) rows2[high] = rows2[low] = a.gather ? a.rows[p] / a.k : (int32_t)p;
+    for (int64_t col = tid * 8; col < a.m; col += 256 * 8) {
+      float v[8], h[8], l[8];
+      load8(d + p * ldd + col, a.m - col, v);
+#pragma unroll
+      for (int i = 0; i < 8; i++) {
+        const bool finite = (__float_as_uint(v[i]) & 0x7F800000u) != 0x7F800000u;
+        h[i] = finite ? __uint_as_float(__float_as_uint(v[i]) & 0xFFFF0000u) : v[i];
+        l[i] = finite ? v[i] - h[i] : 0.0f;
+      }
+      store8(d2 + high * ld2 + col, a.m - col, h);
+      store8(d2 + low * ld2 + col, a.m - col, l);
+    }
+  }
+}
+
 // The grid of a tiled kernel.
 template <int MODE>
 int64_t tiles(ProductArgs &a, int64_t bm, int64_t bn) {
@@ -928,7 +963,9 @@ int launch_product(const skew_rows &r, const skew_product_desc &p, char *ws, voi
   return p.flags & SKEW_TRANSPOSE ? launch_mode<kBackward>(a, ws, stream) : launch_mode<kForward>(a, ws, stream);
 }
 
-int launch_product_grad(const skew_rows &r, const skew_product_desc &p, void *stream) {
+namespace {
+// x_rows: the rows of x that places name
+int product_grad(const skew_rows &r, const skew_product_desc &p, int64_t x_rows, void *stream) {
   ProductArgs a = args_of(r, p);
   a.w = static_cast<const bf16_t *>(p.y);
   a.y = const_cast<void *>(p.w);
@@ -936,10 +973,52 @@ int launch_product_grad(const skew_rows &r, const skew_product_desc &p, void *st
   a.ldy = p.ldw;
   a.f32 = 0;
   a.direct = chunks(a.x, a.ldx) && chunks(a.w, a.ldw) && a.n % 8 == 0 && a.m % 8 == 0 &&
-             short_rows(a.gather ? r.tokens : a.places, a.ldx) && short_rows(kMaxTile, a.ldw);
+             short_rows(x_rows, a.ldx) && short_rows(kMaxTile, a.ldw);
   a.wide = ((uintptr_t)a.y & 15) == 0 && a.ldy % 4 == 0 && a.slice % 4 == 0;
   a.direct = a.direct && a.wide && a.ldy % 8 == 0 && a.slice % 8 == 0;
   return launch_mode<kWeights>(a, nullptr, stream);
+}
+
+// scratch of skew_expert_matmul_grad_f32: offsets2, rows2, d2
+struct SplitPlan {
+  size_t off_rows, off_d, bytes;
+  int64_t ld;
+};
+SplitPlan split_plan(const skew_rows &r, const skew_product_desc &p) {
+  const size_t places = (size_t)(r.tokens * r.k);
+  SplitPlan s;
+  s.ld = (p.m + 7) / 8 * 8;
+  s.off_rows = pad256(((size_t)r.experts + 1) * 4);
+  s.off_d = s.off_rows + pad256(2 * places * 4);
+  s.bytes = s.off_d + 2 * places * (size_t)s.ld * 2;
+  return s;
+}
+}  // namespace
+
+int launch_product_grad(const skew_rows &r, const skew_product_desc &p, void *stream) {
+  return product_grad(r, p, p.flags & SKEW_GATHER ? r.tokens : r.tokens * r.k, stream);
+}
+
+size_t product_grad_f32_scratch(const skew_rows &r, const skew_product_desc &p) {
+  return r.tokens == 0 ? 0 : split_plan(r, p).bytes;
+}
+
+int launch_product_grad_f32(const skew_rows &r, const skew_product_desc &p, char *ws, void *stream) {
+  const SplitPlan s = split_plan(r, p);
+  const int64_t places = r.tokens * r.k;
+  int32_t *offsets2 = reinterpret_cast<int32_t *>(ws), *rows2 = reinterpret_cast<int32_t *>(ws + s.off_rows);
+  bf16_t *d2 = reinterpret_cast<bf16_t *>(ws + s.off_d);
+  constexpr int64_t kMostGroups = 1 << 16;
+  split_kernel<<<(unsigned)(places < kMostGroups ? places : kMostGroups), 256, 0, static_cast<hipStream_t>(stream)>>>(
+      args_of(r, p), static_cast<const float *>(p.y), p.ldy, offsets2, rows2, d2, s.ld);
+  const int e = (int)hipGetLastError();
+  if (e != (int)hipSuccess) return e;
+  const skew_rows twice = {offsets2, rows2, nullptr, 2 * places, 1, r.experts};   // pairs of one choice: their own tokens
+  skew_product_desc q = p;
+  q.y = d2;
+  q.ldy = s.ld;
+  q.flags = SKEW_GATHER;
+  return product_grad(twice, q, p.flags & SKEW_GATHER ? r.tokens : places, stream);
 }
 
 }  // namespace moe

@@ -33,11 +33,13 @@ __global__ __launch_bounds__(kThreads) void combine_kernel(const int32_t *slots,
 
 // A work-group takes one token: its dout row times each weight, and the dot products with the rows of y.
 // Places from offsets[experts] on hold no pair; the work-group of token t zeroes those among t k .. t k + k - 1.
-template <class Y>
+// dy (D) is float32, or bf16 for a caller who takes one more rounding of the weights' gradient (2^-9 of each term on average)
+// for half the bytes and half the products of skew_expert_matmul_grad_f32.
+template <class Y, class D>
 __global__ __launch_bounds__(kThreads) void combine_backward_kernel(const int32_t *slots, const int32_t *held, int k,
                                                                     int64_t rows, const bf16_t *dout, int64_t ldo,
                                                                     const Y *y, int64_t ldy, const float *weights,
-                                                                    bf16_t *dy, int64_t lddy, float *dweights,
+                                                                    D *dy, int64_t lddy, float *dweights,
                                                                     int64_t m) {
   __shared__ float part[SKEW_MAX_CHOICES][kThreads / 64];
   const int64_t t = blockIdx.x;
@@ -239,12 +241,14 @@ int launch_combine(const skew_rows &r, const void *y, int y_dtype, int64_t ldy, 
 }
 
 int launch_combine_backward(const skew_rows &r, const void *dout, int64_t ldo, const void *y, int y_dtype,
-                            int64_t ldy, const float *weights, void *dy, int64_t lddy, float *dweights, int64_t m,
-                            void *stream) {
+                            int64_t ldy, const float *weights, void *dy, int dy_dtype, int64_t lddy, float *dweights,
+                            int64_t m, void *stream) {
   by_type(y_dtype, [&](auto Y) {
-    combine_backward_kernel<<<(unsigned)r.tokens, kThreads, 0, static_cast<hipStream_t>(stream)>>>(
-        r.slots, r.offsets + r.experts, r.k, r.tokens * r.k, static_cast<const bf16_t *>(dout), ldo,
-        static_cast<const decltype(Y) *>(y), ldy, weights, static_cast<bf16_t *>(dy), lddy, dweights, m);
+    by_type(dy_dtype, [&](auto D) {
+      combine_backward_kernel<<<(unsigned)r.tokens, kThreads, 0, static_cast<hipStream_t>(stream)>>>(
+          r.slots, r.offsets + r.experts, r.k, r.tokens * r.k, static_cast<const bf16_t *>(dout), ldo,
+          static_cast<const decltype(Y) *>(y), ldy, weights, static_cast<decltype(D) *>(dy), lddy, dweights, m);
+    });
   });
   return (int)hipGetLastError();
 }

@@ -13,7 +13,7 @@ A layer of experts, forward and backward::
     y = expert_matmul(a, w_down, plan, dtype=torch.float32)      # (T k, d)
     out = expert_combine(y, plan, weights, dtype=torch.bfloat16) # (T, d)
 
-    dy, dweights = expert_combine_backward(dout, y, plan, weights)
+    dy, dweights = expert_combine_backward(dout, y, plan, weights)   # dy float32: dw_down is rounded once
     da = expert_matmul(dout, w_down, plan, gather=True, transpose=True, scale=weights)
     dw_down = expert_matmul_grad(a, dy, plan)
     ...                                                          # dh = act'(h) da
@@ -40,8 +40,9 @@ MAX_PLACES, MAX_COLS = 2**31 - 1, 1 << 24
 
 # names that include/skew_moe.h declares (checked by the CPU test suite)
 EXPORTS = ("skew_route", "skew_route_backward", "skew_order_bytes", "skew_expert_rows", "skew_expert_matmul_bytes",
-           "skew_expert_matmul", "skew_expert_matmul_grad", "skew_expert_combine", "skew_expert_combine_backward",
-           "skew_embed", "skew_embed_grad")
+           "skew_expert_matmul", "skew_expert_matmul_grad", "skew_expert_matmul_grad_f32_bytes",
+           "skew_expert_matmul_grad_f32", "skew_expert_combine", "skew_expert_combine_backward",
+           "skew_expert_combine_backward_f32", "skew_embed", "skew_embed_grad")
 
 
 class RouteDesc(ctypes.Structure):
@@ -91,8 +92,11 @@ def _lib():
                 ("skew_expert_matmul_bytes", [p, p, p]),
                 ("skew_expert_matmul", [p, p, p, size, p]),
                 ("skew_expert_matmul_grad", [p, p, p]),
+                ("skew_expert_matmul_grad_f32_bytes", [p, p, p]),
+                ("skew_expert_matmul_grad_f32", [p, p, p, size, p]),
                 ("skew_expert_combine", [p, p, i32, i64, p, p, i32, i64, i64, p]),
                 ("skew_expert_combine_backward", [p, p, i64, p, i32, i64, p, p, i64, p, i64, p]),
+                ("skew_expert_combine_backward_f32", [p, p, i64, p, i32, i64, p, p, i64, p, i64, p]),
                 ("skew_embed", [p, i32, i64, p, i64, i64, i64, p, i64, i32, f32, p]),
                 ("skew_embed_grad", [p, i32, i64, p, i64, p, i64, i64, i64, i32, f32, p, size, p])):
             f = getattr(L, name)
@@ -341,12 +345,15 @@ def expert_matmul(x, w, plan, *, gather=False, transpose=False, scale=None, dtyp
 
 def expert_matmul_grad(x, dy, plan, *, gather=False, out=None, stream=None):
     """The weights' gradient bf16 (E, n, m): each expert's sum of x's rows (one a place, or with ``gather`` one a
-    token) times ``dy`` bf16 (T k, m); zero for an expert without rows. ``out`` takes an existing tensor,
-    such as the gradient that an optimizer was given."""
+    token) times ``dy`` (T k, m), bf16 or float32; zero for an expert without rows. A float32 ``dy`` is taken as
+    two bf16 numbers (2^-16 of a value is left out), in up to twice the time. ``out`` takes an existing
+    tensor, such as the gradient that an optimizer was given."""
     import torch
     _tensor(x, "x", (torch.bfloat16,), 2)
-    _tensor(dy, "dy", (torch.bfloat16,), 2, x.device)
+    _tensor(dy, "dy", (torch.bfloat16, torch.float32), 2, x.device)
     r = _plan_desc(plan, x.device)
+    if dy.dtype == torch.float32 and r.tokens * r.k > MAX_PLACES // 2:
+        raise ValueError("too many pairs: a float32 dy is taken as two rows a pair, which have 32-bit indices")
     n, m = x.shape[1], dy.shape[1]
     ldx = _rows_of(x, "x", r.tokens if gather else r.tokens * r.k, n)
     ldy = _rows_of(dy, "dy", r.tokens * r.k, m)
@@ -359,7 +366,16 @@ def expert_matmul_grad(x, dy, plan, *, gather=False, out=None, stream=None):
             raise ValueError(f"out must have shape {(r.experts, n, m)}, not {tuple(out.shape)}")
         ldw, step = _stack(out, "out", r.experts)
         p = ProductDesc(_ptr(x), _ptr(out), _ptr(dy), None, n, m, ldx, ldw, step, ldy, GATHER if gather else 0, BF16)
-        _check(_lib().skew_expert_matmul_grad(ctypes.byref(r), ctypes.byref(p), s), "skew_expert_matmul_grad")
+        L = _lib()
+        if dy.dtype == torch.bfloat16:
+            _check(L.skew_expert_matmul_grad(ctypes.byref(r), ctypes.byref(p), s), "skew_expert_matmul_grad")
+        else:
+            nbytes = ctypes.c_size_t()
+            _check(L.skew_expert_matmul_grad_f32_bytes(ctypes.byref(r), ctypes.byref(p), ctypes.byref(nbytes)),
+                   "skew_expert_matmul_grad_f32_bytes")
+            ws = _scratch(nbytes.value, x.device)
+            _check(L.skew_expert_matmul_grad_f32(ctypes.byref(r), ctypes.byref(p), _ptr(ws), nbytes.value, s),
+                   "skew_expert_matmul_grad_f32")
     return out
 
 
@@ -386,9 +402,13 @@ def expert_combine(y, plan, weights=None, *, dtype=None, stream=None):
     return out
 
 
-def expert_combine_backward(dout, y, plan, weights=None, *, stream=None):
-    """Gradients of `expert_combine`: (dy bf16 (T k, m), dweights float32 (T, k)) from ``dout`` bf16 (T, m)."""
+def expert_combine_backward(dout, y, plan, weights=None, *, dtype=None, stream=None):
+    """Gradients of `expert_combine`: (dy (T k, m), dweights float32 (T, k)) from ``dout`` bf16 (T, m). dy is float32, so
+    that a weights' gradient made from it is rounded once; ``dtype`` bf16 gives it half the bytes, and
+    `expert_matmul_grad` half the work, for a second rounding (2^-8 of each term at most)."""
     import torch
+    dtype = torch.float32 if dtype is None else dtype
+    code = _dtype_code(dtype, "dtype")
     _tensor(dout, "dout", (torch.bfloat16,), 2)
     _tensor(y, "y", (torch.bfloat16, torch.float32), 2, dout.device)
     r = _plan_desc(plan, dout.device)
@@ -401,11 +421,11 @@ def expert_combine_backward(dout, y, plan, weights=None, *, stream=None):
         _dense(weights, "weights", (r.tokens, r.k))
     s, here = _on(dout.device, stream, dout, y, weights, *plan)
     with here:
-        dy = torch.empty((r.tokens * r.k, m), dtype=torch.bfloat16, device=dout.device)
+        dy = torch.empty((r.tokens * r.k, m), dtype=dtype, device=dout.device)
         dweights = torch.empty((r.tokens, r.k), dtype=torch.float32, device=dout.device)
-        _check(_lib().skew_expert_combine_backward(ctypes.byref(r), _ptr(dout), ldo, _ptr(y), _dtype_code(y.dtype, "y"),
-                                                   ldy, _ptr(weights), _ptr(dy), m, _ptr(dweights), m, s),
-               "skew_expert_combine_backward")
+        name = "skew_expert_combine_backward" + ("_f32" if code == F32 else "")
+        _check(getattr(_lib(), name)(ctypes.byref(r), _ptr(dout), ldo, _ptr(y), _dtype_code(y.dtype, "y"), ldy,
+                                     _ptr(weights), _ptr(dy), m, _ptr(dweights), m, s), name)
     return dy, dweights
 
 
