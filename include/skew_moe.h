@@ -43,7 +43,8 @@ enum { SKEW_SCORE_SOFTMAX = 0, SKEW_SCORE_SIGMOID = 1 };
  * A logit of -inf closes its expert: score 0, never chosen, and it adds nothing to its group's value (a
  * group without an open expert is never kept). A token with fewer than k open experts has expert -1
  * and weight 0 in the places left, down to a row of logits that are all -inf. NaN and +inf count
- * as the highest value, so they are chosen and show in the weights.
+ * as the highest value, so they are chosen and show in the weights; with a bias, the other experts of
+ * such a row have no softmax and follow by their bias alone. (With a bias, the sigmoid of +inf is a score of 1 like others.)
  *   tokens >= 0; 1 <= experts <= SKEW_MAX_EXPERTS; groups <= SKEW_MAX_GROUPS divides experts;
  *   1 <= top_groups <= groups; 1 <= k <= SKEW_MAX_CHOICES, k <= top_groups * experts / groups;
  *   group_sum 2 needs a bias (sums of logits are no score);

@@ -111,7 +111,8 @@ __global__ __launch_bounds__(kThreads) void route_kernel(skew_route_desc d, cons
   if (bias != nullptr) {
     float add[V];
     load_row<V>(bias + (n > 0 ? e0 : 0), n, add);
-    const float r = fast_rcp(sum);
+    // A NaN or an infinity makes the sum NaN: its own value stays NaN, which is the highest, and the others have their bias.
+    const float r = sum != sum ? 0.0f : fast_rcp(sum);
 #pragma unroll
     for (int v = 0; v < V; v++) {
       const float x = (d.score == SKEW_SCORE_SOFTMAX ? c[v] * r : fast_rcp(1.0f + fast_exp(-l[v]))) + add[v];
