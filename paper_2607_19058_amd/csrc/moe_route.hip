@@ -72,6 +72,13 @@ __device__ __forceinline__ void load_row(const T *p, int n, float *o) {
 }
 
 __device__ __forceinline__ float sigmoid(float l) { return 1.0f / (1.0f + expf(-l)); }
+// The sigmoids of a token's chosen logits (-inf: none) up to a common factor, for weights that are renormalised: with
+// u = min(l, 0), sigmoid(l) = exp(u) / (1 + exp(-|l|)), and exp(u - max u) does not underflow for all of them.
+template <int L>
+__device__ __forceinline__ float shifted_sigmoid(float l) {
+  const float u = fminf(l, 0.0f), m = max_over<L>(u);   // (a NaN is in the divisor)
+  return l == kClosed ? 0.0f : expf(u - m) / (1.0f + expf(-fabsf(l)));
+}
 // For scores that only order the experts: the hardware's exponential and reciprocal, off by some 1e-6 of the score at
 // most, where the weights take the exact ones.
 __device__ __forceinline__ float fast_exp(float x) { return __expf(x); }
@@ -215,7 +222,7 @@ __global__ __launch_bounds__(kThreads) void route_kernel(skew_route_desc d, cons
     }
     s = e >= 0 ? expf(x - mx) / sum : 0.0f;
   } else {
-    s = e >= 0 ? sigmoid(x) : 0.0f;
+    s = d.renormalize ? shifted_sigmoid<L>(x) : e >= 0 ? sigmoid(x) : 0.0f;
   }
   if (d.renormalize) {
     const float total = sum_over<L>(s);
@@ -278,16 +285,15 @@ __global__ __launch_bounds__(kThreads) void route_backward_kernel(skew_route_des
       for (int v = 0; v < V; v++) o[v] = -o[v] * f;
     }
   } else {
-    const float s = e >= 0 ? sigmoid(x) : 0.0f;
     const float rest = e >= 0 ? sigmoid(-x) : 0.0f;   // 1 - s without its cancellation
-    float ds = dw;
     if (d.renormalize) {
+      const float s = shifted_sigmoid<L>(x);
       const float total = sum_over<L>(s);
       const float w = total == 0.0f ? 0.0f : s / total;
       const float mean = sum_over<L>(dw * w);
       g = w * rest * (dw - mean);
     } else {
-      g = ds * s * rest;
+      g = e >= 0 ? dw * sigmoid(x) * rest : 0.0f;
     }
   }
   for (int j = 0; j < d.k; j++) {

@@ -45,3 +45,33 @@ def test_one_infinite_logit_of_eight():
     l = torch.tensor([[0.0, 1.0, 2.0, 3.0, 1.0, INF, 0.0, 2.0]])
     w, e = P.route(l.to(DEV), 2, bias=torch.zeros(8, device=DEV))
     assert e.cpu().tolist() == [[5, 0]] and w.isnan().all()
+
+
+# ---- weights of sigmoid scores that are small ------------------------------------------------------
+SMALL = [[-90.0, -91.0, -95.0, -200.0], [-88.5, -89.5, -300.0, -89.0], [-3e38, -3e38, -3.2e38, -3e38], [5.0, -90.0, -100.0, -2.0],
+         [-104.0, -103.0, -120.0, -110.0], [-87.0, -88.0, -87.5, -86.0], [100.0, 90.0, -1.0, -50.0], [-1e4, -10001.0, -1e4, -10002.0]]
+
+
+@pytest.mark.parametrize("dtype", [F32, BF], ids=["f32", "bf16"])
+def test_renormalised_weights_of_small_sigmoid_scores(dtype):
+    """w = softmax of log sigmoid(l) over the chosen, of any size; its gradient w_i (1 - s_i) (dw_i - sum_j w_j dw_j).
+    An exponential's argument is a difference d of two of the logits, off by |d| half ulps."""
+    l = torch.tensor(SMALL).to(dtype)
+    k, scale = 3, 1.5
+    w, e = P.route(l.to(DEV), k, score="sigmoid", scale=scale)
+    e = e.cpu()
+    order = torch.argsort(l.float(), dim=1, descending=True, stable=True)[:, :k]
+    assert torch.equal(e, order.int())
+    x = l.double().gather(1, order)
+    log_s = torch.nn.functional.logsigmoid(x)
+    want = torch.softmax(log_s, 1)
+    d = (x.clamp(max=0) - x.clamp(max=0).max(1, keepdim=True).values).abs().clamp(max=200)
+    off = (d + 32) * 2 * ref.U32 * want + 1e-37
+    assert ((w.cpu().double() / scale - want).abs() <= off).all(), (w.cpu() / scale, want)
+    dw = torch.tensor([[1.0, -2.0, 0.5]]).expand(len(SMALL), k).contiguous()
+    got = P.route_backward(l.to(DEV), e.to(DEV), dw.to(DEV), score="sigmoid", scale=scale).cpu().double()
+    mean = (want * dw).sum(1, keepdim=True)
+    part = scale * want * torch.sigmoid(-x) * (dw - mean)
+    full = torch.zeros(l.shape, dtype=torch.float64).scatter_(1, order, part)
+    bound = torch.zeros(l.shape, dtype=torch.float64).scatter_(1, order, scale * 3 * (off + 2 * off.sum(1, keepdim=True) * want))
+    assert ((got - full).abs() <= bound + full.abs() * (ref.UBF if dtype == BF else ref.U32) + 1e-37).all(), (got, full)
