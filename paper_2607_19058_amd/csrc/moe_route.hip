@@ -226,7 +226,7 @@ __global__ __launch_bounds__(kThreads) void route_kernel(skew_route_desc d, cons
   }
   if (d.renormalize) {
     const float total = sum_over<L>(s);
-    s = total == 0.0f ? 0.0f : s / total;
+    s = e < 0 ? 0.0f : s / total;   // (a NaN in the total is not a weight of the places left over)
   }
   if (has) {
     weights[t * d.k + lane] = d.scale * s;

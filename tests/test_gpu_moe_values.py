@@ -75,3 +75,14 @@ def test_renormalised_weights_of_small_sigmoid_scores(dtype):
     full = torch.zeros(l.shape, dtype=torch.float64).scatter_(1, order, part)
     bound = torch.zeros(l.shape, dtype=torch.float64).scatter_(1, order, scale * 3 * (off + 2 * off.sum(1, keepdim=True) * want))
     assert ((got - full).abs() <= bound + full.abs() * (ref.UBF if dtype == BF else ref.U32) + 1e-37).all(), (got, full)
+
+
+# ---- places without an expert beside a weight that is NaN ------------------------------------------
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("renormalize", [True, False])
+def test_places_without_an_expert_weigh_nothing(score, renormalize):
+    l = torch.tensor([[NAN, -INF, -INF, -INF], [-INF, -INF, -INF, 1.0], [-INF] * 4])
+    for bias in (None, torch.zeros(4, device=DEV)):
+        w, e = P.route(l.to(DEV), 3, score=score, renormalize=renormalize, bias=bias)
+        assert e.cpu().tolist() == [[0, -1, -1], [3, -1, -1], [-1, -1, -1]]
+        assert w[0, 0].isnan() and not w[:, 1:].any() and not w[2].any()
