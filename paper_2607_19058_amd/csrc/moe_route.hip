@@ -79,10 +79,6 @@ __device__ __forceinline__ float shifted_sigmoid(float l) {
   const float u = fminf(l, 0.0f), m = max_over<L>(u);   // (a NaN is in the divisor)
   return l == kClosed ? 0.0f : expf(u - m) / (1.0f + expf(-fabsf(l)));
 }
-// For scores that only order the experts: the hardware's exponential and reciprocal, off by some 1e-6 of the score at
-// most, where the weights take the exact ones.
-__device__ __forceinline__ float fast_exp(float x) { return __expf(x); }
-__device__ __forceinline__ float fast_rcp(float x) { return __builtin_amdgcn_rcpf(x); }
 
 template <int L, int V, class T>
 __global__ __launch_bounds__(kThreads) void route_kernel(skew_route_desc d, const T *logits, const float *bias,
@@ -110,7 +106,7 @@ __global__ __launch_bounds__(kThreads) void route_kernel(skew_route_desc d, cons
     mx = mx == kClosed ? 0.0f : mx;   // no open expert: every exp is 0
 #pragma unroll
     for (int v = 0; v < V; v++) {
-      c[v] = d.renormalize ? fast_exp(l[v] - mx) : expf(l[v] - mx);   // the sum is in the weights without renormalisation
+      c[v] = expf(l[v] - mx);
       sum += c[v];
     }
     sum = sum_over<L>(sum);
@@ -119,10 +115,10 @@ __global__ __launch_bounds__(kThreads) void route_kernel(skew_route_desc d, cons
     float add[V];
     load_row<V>(bias + (n > 0 ? e0 : 0), n, add);
     // A NaN or an infinity makes the sum NaN: its own value stays NaN, which is the highest, and the others have their bias.
-    const float r = sum != sum ? 0.0f : fast_rcp(sum);
+    const float r = sum != sum ? 0.0f : 1.0f / sum;
 #pragma unroll
     for (int v = 0; v < V; v++) {
-      const float x = (d.score == SKEW_SCORE_SOFTMAX ? c[v] * r : fast_rcp(1.0f + fast_exp(-l[v]))) + add[v];
+      const float x = (d.score == SKEW_SCORE_SOFTMAX ? c[v] * r : sigmoid(l[v])) + add[v];
       c[v] = l[v] == kClosed ? kClosed : x;
     }
   } else {

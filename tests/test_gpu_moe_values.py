@@ -86,3 +86,28 @@ def test_places_without_an_expert_weigh_nothing(score, renormalize):
         w, e = P.route(l.to(DEV), 3, score=score, renormalize=renormalize, bias=bias)
         assert e.cpu().tolist() == [[0, -1, -1], [3, -1, -1], [-1, -1, -1]]
         assert w[0, 0].isnan() and not w[:, 1:].any() and not w[2].any()
+
+
+# ---- choices by scores that are nearly alike --------------------------------------------------------
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+def test_choice_by_scores_of_float32(score):
+    """Two experts whose values s + b are 24 half ulps of float32 apart. A float32 evaluation is off by some 12 at most:
+    2 of the exponential, 2 or 3 of the sum (1 + small), 1 of the division, 1 of adding the bias, for each of the two."""
+    g = torch.Generator().manual_seed(7)
+    wrong = 0
+    for i in range(96):
+        a, b = (-(30 + 30 * torch.rand(2, generator=g))).tolist()   # scores of 1e-13 to 1e-26
+        a, b = max(a, b), min(a, b)
+        l = torch.tensor([[0.0, a, b]] if score == "softmax" else [[10.0, a, b]])
+        x = l.double()[0]
+        s = torch.softmax(x, 0) if score == "softmax" else torch.sigmoid(x)
+        bias = torch.zeros(3)
+        bias[2] = float(s[1] * (1 + (24 if i % 2 else -24) * ref.U32) - s[2])   # the lower score is lifted to the other one
+        v = s + bias.double()
+        want = 1 if v[1] > v[2] else 2
+        if abs(float(v[1] - v[2])) < 23 * ref.U32 * float(v[1]):
+            continue   # the bias' own rounding
+        _, e = P.route(l.to(DEV), 2, score=score, bias=bias.to(DEV))
+        assert int(e[0, 0]) == 0
+        wrong += int(e[0, 1]) != want
+    assert wrong == 0, wrong
