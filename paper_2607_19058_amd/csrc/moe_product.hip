@@ -240,13 +240,20 @@ __device__ __forceinline__ bool patch_tile(bool in_patches, uint32_t rows, uint3
 
 // acc += the product of two fragments (result rows along the second). IN_A: the sums stay in the accumulation
 // registers, which the compiler, left to itself, copies to others and back when they are 256 of a lane's 512.
-// It does not know the written-out instruction's latency: mfma_done() comes before the sums are read.
+// It does not know the written-out instruction's latency: the sums go through mfma_done() before they are read.
 template <bool IN_A>
 __device__ __forceinline__ void mfma(f32x4 &acc, bf16x8 b, bf16x8 a) {
   if (IN_A) asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(acc) : "v"(b), "v"(a));
   else acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b, a, acc, 0, 0, 0);
 }
-__device__ __forceinline__ void mfma_done() { asm volatile("s_nop 15\n\ts_nop 15" ::: "memory"); }
+template <int FM, int FN>
+__device__ __forceinline__ void mfma_done(f32x4 (&acc)[FM][FN]) {
+  asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
+#pragma unroll
+  for (int i = 0; i < FM; i++)
+#pragma unroll
+    for (int j = 0; j < FN; j++) asm volatile("" : "+a"(acc[i][j]));   // what reads them depends on this, which stays behind the wait
+}
 
 // What a tiled work-group computes: rows [r0, r1) and columns [c0, c1) of the result of one expert, contraction length K;
 // kWeights: places first .. first + K - 1.
@@ -611,11 +618,11 @@ __global__ __launch_bounds__(256, FM * FN * KS >= 64 ? 1 : FM * FN == 8 ? 3 : 2)
         step(odd, yes, no, 0);   // of the last stage: reads what is not used
       }
     }
+    if (kInA) mfma_done(acc);   // here, not after the loop: where a contraction may be empty, the sums are copied on the loop's way out
     // the next round, if any, starts in the buffer that is sent for next
     while (reading != sending) advance();
     __syncthreads();   // the buffers are no longer read
   }
-  if (kInA) mfma_done();
   if (MODE != kWeights && a.part) a.y = static_cast<float *>(a.y) + (int64_t)blockIdx.y * a.places * a.ldy;
   store_tile<MODE, FM, FN, true>(a, t, wr, wc, acc, reinterpret_cast<char *>(lds) + wave * (FM * FN * 512));
 }
