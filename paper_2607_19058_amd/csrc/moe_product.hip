@@ -192,11 +192,15 @@ __device__ __forceinline__ bool find_tile(const ProductArgs &a, int64_t tile, in
 // `to` + 16 i of LDS (`to` the same in every lane).
 // Written out because the compiler, which cannot tell the stage buffers apart, would wait for these loads
 // before every LDS read. It does not count them either: every use of the data comes after vm_wait() and a barrier.
+// m0 is a reserved register, about which naming it warns; the compiler sets it anew for each use of its own after it.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
 __device__ __forceinline__ void load_lds(const char *base, uint32_t offset, uint32_t to) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(__builtin_amdgcn_readfirstlane(to)),
                "v"(offset), "s"(base)
-               : "memory");
+               : "memory", "m0");
 }
+#pragma clang diagnostic pop
 // waits until at most N of this wave's loads are on their way
 template <int N>
 __device__ __forceinline__ void vm_wait() {

@@ -97,3 +97,22 @@ def test_early_reads_are_found():
     assert early_reads(body) == (4, ["v_accvgpr_read_b32 v1, a2"])
     del body[1]
     assert early_reads(body) == (4, [])
+
+
+def written_out():
+    """(file, statement) of every asm statement in the device sources."""
+    for f in sorted(os.listdir(build.CSRC)):
+        if f.endswith((".hip", ".h")):
+            for s in re.findall(r"\basm volatile\((.*?)\);", open(os.path.join(build.CSRC, f)).read(), flags=re.S):
+                yield f, s
+
+
+def test_written_registers_are_named():
+    """A fixed register that an asm statement writes (m0, which scalar code of the compiler's own may hold) is among its clobbers."""
+    seen = 0
+    for f, s in written_out():
+        text = "".join(re.findall(r'"((?:[^"\\]|\\.)*)"', s.split(":")[0]))
+        if re.search(r"\bs_mov_b32 m0\b", text):
+            assert '"m0"' in s.split(":")[-1], (f, s)
+            seen += 1
+    assert seen
