@@ -16,6 +16,8 @@ inline int bits_for(uint64_t x) {
   while (b < 64 && (x >> b) != 0) b++;
   return b < 1 ? 1 : b;
 }
+// Length of the round that begins at `base` of `total` in rounds of at most `most`. (base + most may pass 2^31.)
+constexpr int round_length(int base, int total, int most) { return total - base > most ? most : total - base; }
 inline size_t pad256(size_t x) { return (x + 255) / 256 * 256; }
 
 // How n keys of 0 .. keys (`keys` itself: none) are sorted, and where its scratch lies.

@@ -560,7 +560,7 @@ __global__ __launch_bounds__(256, FM * FN * KS >= 64 ? 1 : FM * FN == 8 ? 3 : 2)
 
   for (; base < K; base = end) {
     if (MODE == kWeights) {
-      end = base + kList < K ? base + kList : K;
+      end = base + round_length(base, K, kList);
       __syncthreads();   // the list of the round before is no longer read
       for (int i = tid; i < end - base; i += kThreads) {
         const int64_t p = t.first + base + i;
@@ -704,19 +704,20 @@ __global__ __launch_bounds__(256, 2) void any_kernel(ProductArgs a) {
   }
   // kSets stages are on their way into registers, set by set
   u32x4 ga[kSets][kPA], gb[kSets][kPB];
-  int base = 0, end = 0;   // kWeights: the places in the list
-  auto load = [&](auto SET, auto WHOLE, int k0) {
+  // Unsigned, as stages past the end of 2^31 - 1 places begin beyond it.
+  uint32_t base = 0, end = 0;   // kWeights: the places in the list
+  auto load = [&](auto SET, auto WHOLE, uint32_t k0) {
     const int64_t ob = MODE == kBackward ? k0 : k0 * a.ldw;
 #pragma unroll
     for (int i = 0; i < kPA; i++) {
-      const int left = end - k0 - ka[i];   // contraction values from this chunk on
+      const int left = (int)(end - k0) - ka[i];   // contraction values from this chunk on
       const bf16_t *p = pa[i] + (MODE != kWeights ? k0 : WHOLE || left > 0 ? list[k0 - base + ka[i]] * a.ldx : 0);
       if (WHOLE) ga[SET][i] = *reinterpret_cast<const u32x4_a2 *>(p);
       else ga[SET][i] = left > 0 ? load_chunk(p, MODE == kWeights ? na[i] : left) : u32x4{0, 0, 0, 0};
     }
 #pragma unroll
     for (int i = 0; i < kPB; i++) {
-      const int left = end - k0 - kb[i];
+      const int left = (int)(end - k0) - kb[i];
       if (WHOLE) gb[SET][i] = *reinterpret_cast<const u32x4_a2 *>(pb[i] + ob);
       else gb[SET][i] = left > 0 ? load_chunk(pb[i] + ob, MODE == kBackward ? left : nb[i]) : u32x4{0, 0, 0, 0};
     }
@@ -732,7 +733,7 @@ __global__ __launch_bounds__(256, 2) void any_kernel(ProductArgs a) {
   FragT<BN, FN> rb_t(tb, wc);
   int buf = 0;   // the buffer of the stage that is multiplied
   // one stage: the next one goes from SET to the other buffer, and the stage at `ahead` is sent for into SET
-  auto stage = [&](auto SET, auto WHOLE, int ahead) {
+  auto stage = [&](auto SET, auto WHOLE, uint32_t ahead) {
     __syncthreads();
     put_stage(SET, buf ^ 1);
     load(SET, WHOLE, ahead);
@@ -758,11 +759,11 @@ __global__ __launch_bounds__(256, 2) void any_kernel(ProductArgs a) {
   const std::integral_constant<int, kSets - 1> last_set;
   const std::true_type whole;
   const std::false_type any;
-  for (; base < K; base = end) {   // kWeights: rounds of the places in the list
-    end = MODE == kWeights && base + kList < K ? base + kList : K;
+  for (; base < (uint32_t)K; base = end) {   // kWeights: rounds of the places in the list
+    end = MODE == kWeights ? base + round_length((int)base, K, kList) : K;
     if (MODE == kWeights) {
       __syncthreads();
-      for (int i = tid; i < end - base; i += kThreads)
+      for (uint32_t i = tid; i < end - base; i += kThreads)
         list[i] = a.gather ? a.rows[t.first + base + i] / a.k : (int32_t)(t.first + base + i);
       __syncthreads();
     }
@@ -772,7 +773,7 @@ __global__ __launch_bounds__(256, 2) void any_kernel(ProductArgs a) {
     put_stage(set0, buf);
     load(set0, any, base + kSets * kBK);
     // a round of kSets stages; each sends for the stage kSets + 1 further on
-    auto round = [&](auto WHOLE, int k0) {
+    auto round = [&](auto WHOLE, uint32_t k0) {
       stage(set1, WHOLE, k0 + (kSets + 1) * kBK);
       if (WHOLE || k0 + kBK < end) {
         if (kSets == 3) stage(last_set, WHOLE, k0 + (kSets + 2) * kBK);
@@ -780,7 +781,7 @@ __global__ __launch_bounds__(256, 2) void any_kernel(ProductArgs a) {
       }
       if (kSets == 3 && (WHOLE || k0 + 2 * kBK < end)) stage(set0, WHOLE, k0 + (kSets + 3) * kBK);
     };
-    int k0 = base;
+    uint32_t k0 = base;
     if (inside)
       for (; k0 + (2 * kSets + 1) * kBK <= end; k0 += kSets * kBK) round(whole, k0);
     for (; k0 < end; k0 += kSets * kBK) round(any, k0);
