@@ -3,6 +3,8 @@
 Argument checks, output allocation and marshalling only; the work runs in the HIP library
 ``libskewadam.so``. Outputs (and the scratch of a call) are allocated with torch on the
 stream of the call. There is no fallback: without the built library every call raises.
+The backward passes are calls of their own and autograd does not follow them, so inputs that require a gradient are refused:
+call under ``torch.no_grad()``, or detach them.
 
 A layer of experts, forward and backward::
 
@@ -113,6 +115,15 @@ def _dtype_code(t, what):
     return F32 if t == torch.float32 else BF16
 
 
+def _no_autograd(*inputs):
+    import torch
+    if torch.is_grad_enabled():
+        for t in inputs:
+            if t is not None and t.requires_grad:
+                raise RuntimeError("autograd does not follow this call (its backward pass is a call of its own): use "
+                                   "torch.no_grad(), or detach inputs that require a gradient")
+
+
 def _tensor(t, what, dtypes, dims, device=None):
     """Type, device and rank of one tensor argument."""
     if t.dtype not in dtypes:
@@ -216,6 +227,7 @@ def route(logits, k, *, score="softmax", bias=None, groups=1, top_groups=None, g
     lowest index; a logit of -inf closes its expert, and places left over hold expert -1, weight 0.
     """
     import torch
+    _no_autograd(logits, bias)
     top_groups = groups if top_groups is None else top_groups
     d = _route_desc(logits, k, score, renormalize, scale, groups, top_groups, group_sum)
     if not 1 <= groups <= MAX_GROUPS or d.experts % groups:
@@ -239,6 +251,7 @@ def route(logits, k, *, score="softmax", bias=None, groups=1, top_groups=None, g
 def route_backward(logits, experts, dweights, *, score="softmax", renormalize=True, scale=1.0, stream=None):
     """The logits' gradient (T, E) in their type, from that of the weights and the choice of `route`."""
     import torch
+    _no_autograd(logits, dweights)
     _tensor(experts, "experts", (torch.int32,), 2, logits.device)
     d = _route_desc(logits, experts.shape[1], score, renormalize, scale)
     _dense(experts, "experts", (d.tokens, d.k))
@@ -318,6 +331,7 @@ def expert_matmul(x, w, plan, *, gather=False, transpose=False, scale=None, dtyp
     The result is bf16, or float32 with ``dtype``; rows past the last expert's are zero.
     """
     import torch
+    _no_autograd(x, w, scale)
     _tensor(x, "x", (torch.bfloat16,), 2)
     _tensor(w, "w", (torch.bfloat16,), 3, x.device)
     r = _plan_desc(plan, x.device)
@@ -349,6 +363,7 @@ def expert_matmul_grad(x, dy, plan, *, gather=False, out=None, stream=None):
     two bf16 numbers (2^-16 of a value is left out), in up to twice the time. ``out`` takes an existing
     tensor, such as the gradient that an optimizer was given."""
     import torch
+    _no_autograd(x, dy, out)
     _tensor(x, "x", (torch.bfloat16,), 2)
     _tensor(dy, "dy", (torch.bfloat16, torch.float32), 2, x.device)
     r = _plan_desc(plan, x.device)
@@ -383,6 +398,7 @@ def expert_combine(y, plan, weights=None, *, dtype=None, stream=None):
     """Rows back to tokens: (T, m), each the sum of its pairs' rows of ``y`` times ``weights`` float32 (T, k)
     (None: 1); zero for a token without experts. The result has y's type or ``dtype``."""
     import torch
+    _no_autograd(y, weights)
     _tensor(y, "y", (torch.bfloat16, torch.float32), 2)
     r = _plan_desc(plan, y.device)
     m = y.shape[1]
@@ -409,6 +425,7 @@ def expert_combine_backward(dout, y, plan, weights=None, *, dtype=None, stream=N
     import torch
     dtype = torch.float32 if dtype is None else dtype
     code = _dtype_code(dtype, "dtype")
+    _no_autograd(dout, y, weights)
     _tensor(dout, "dout", (torch.bfloat16,), 2)
     _tensor(y, "y", (torch.bfloat16, torch.float32), 2, dout.device)
     r = _plan_desc(plan, dout.device)
@@ -443,6 +460,7 @@ def embed(tokens, table, *, scale=1.0, stream=None):
     """``scale`` times the table's rows of ``tokens`` (int32 or int64 (T)): (T, D) in the table's type (bf16,
     float32). An id outside [0, V) is no token: a row of zeros."""
     import torch
+    _no_autograd(table)
     _tensor(table, "table", (torch.bfloat16, torch.float32), 2)
     size = _ids(tokens, table.device)
     (V, D), T = table.shape, tokens.shape[0]
@@ -463,6 +481,7 @@ def embed_grad(tokens, dout, vocab, *, scale=1.0, out=None, stream=None):
     """The table's gradient (V, D) in dout's type: ``scale`` times the sum of ``dout``'s rows of each id, zero for
     ids without tokens. ``out`` takes an existing tensor, such as the gradient that an optimizer was given."""
     import torch
+    _no_autograd(dout, out)
     _tensor(dout, "dout", (torch.bfloat16, torch.float32), 2)
     size = _ids(tokens, dout.device)
     T, D = dout.shape
