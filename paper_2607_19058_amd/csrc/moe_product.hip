@@ -353,7 +353,7 @@ __device__ __forceinline__ void store_tile(const ProductArgs &a, const Tile &t, 
     }
     return;
   }
-  float *y = static_cast<float *>(a.y) + (MODE == kWeights ? (int64_t)t.expert * a.slice : 0) + row0 * a.ldy + col0;
+  float *y = static_cast<float *>(a.y) + row0 * a.ldy + col0;   // (dW is bf16)
 #pragma unroll
   for (int i = 0; i < FM; i++) {
     if (row0 + i * 16 >= t.r1) break;
