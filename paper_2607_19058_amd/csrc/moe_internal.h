@@ -16,6 +16,9 @@ inline int bits_for(uint64_t x) {
   while (b < 64 && (x >> b) != 0) b++;
   return b < 1 ? 1 : b;
 }
+// bf16 rows whose byte offsets stay below 2^31, with a row to spare
+// (a single row may have any stride, whose products pass 2^63)
+constexpr bool short_rows(int64_t rows, int64_t ld) { return ld <= 0x7FFFFFFF / (2 * (rows + 1)); }
 // Length of the round that begins at `base` of `total` in rounds of at most `most`. (base + most may pass 2^31.)
 constexpr int round_length(int base, int total, int most) { return total - base > most ? most : total - base; }
 inline size_t pad256(size_t x) { return (x + 255) / 256 * 256; }

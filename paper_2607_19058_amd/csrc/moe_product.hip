@@ -947,8 +947,6 @@ ProductArgs args_of(const skew_rows &r, const skew_product_desc &p) {
 }
 
 constexpr int64_t kMaxTile = 256;   // result rows, or contraction rows, that a lane's offset spans
-// rows whose byte offsets stay below 2^31, with a row to spare
-bool short_rows(int64_t rows, int64_t ld) { return (rows + 1) * ld * 2 < (int64_t)1 << 31; }
 bool chunks(const void *p, int64_t ld) { return ((uintptr_t)p & 15) == 0 && ld % 8 == 0; }
 
 }  // namespace
