@@ -372,13 +372,14 @@ def expert_matmul_grad(x, dy, plan, *, gather=False, out=None, stream=None):
     n, m = x.shape[1], dy.shape[1]
     ldx = _rows_of(x, "x", r.tokens if gather else r.tokens * r.k, n)
     ldy = _rows_of(dy, "dy", r.tokens * r.k, m)
+    if out is not None:
+        _tensor(out, "out", (torch.bfloat16,), 3, x.device)
+        if tuple(out.shape[1:]) != (n, m):
+            raise ValueError(f"out must have shape {(r.experts, n, m)}, not {tuple(out.shape)}")
     s, here = _on(x.device, stream, x, dy, out, *plan)
     with here:
         if out is None:
             out = torch.empty((r.experts, n, m), dtype=torch.bfloat16, device=x.device)
-        _tensor(out, "out", (torch.bfloat16,), 3, x.device)
-        if tuple(out.shape[1:]) != (n, m):
-            raise ValueError(f"out must have shape {(r.experts, n, m)}, not {tuple(out.shape)}")
         ldw, step = _stack(out, "out", r.experts)
         p = ProductDesc(_ptr(x), _ptr(out), _ptr(dy), None, n, m, ldx, ldw, step, ldy, GATHER if gather else 0, BF16)
         L = _lib()
@@ -493,11 +494,12 @@ def embed_grad(tokens, dout, vocab, *, scale=1.0, out=None, stream=None):
         raise ValueError("scale must be finite")
     ldo, L, dev = _ld(dout, "dout"), _lib(), dout.device
     nbytes = _order_bytes(T, vocab, D)
+    if out is not None:
+        _tensor(out, "out", (dout.dtype,), 2, dev)
     s, here = _on(dev, stream, tokens, dout, out)
     with here:
         if out is None:
             out = torch.empty((vocab, D), dtype=dout.dtype, device=dev)
-        _tensor(out, "out", (dout.dtype,), 2, dev)
         ldt = _rows_of(out, "out", vocab, D)
         ws = _scratch(nbytes, dev)
         _check(L.skew_embed_grad(_ptr(tokens), size, T, _ptr(dout), ldo, out.data_ptr(), vocab, D, ldt,
