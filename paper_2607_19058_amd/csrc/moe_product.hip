@@ -807,7 +807,7 @@ __global__ __launch_bounds__(256) void join_kernel(ProductArgs a, const float *p
 // d's upper half, cut off; low, the rest, is exact before its own rounding). An expert's rows of high come before those of
 // low, so with the rows of x named twice the product of twice as many places is the gradient.
 //   offsets2[e] = 2 offsets[e];  place q of the 2 held: row rows2[q] of x and row q of d2.
-// Infinities and NaN are in high alone. 16 KB in and out a place of 2048 columns: bound by memory.
+// Infinities and NaN are in both. 16 KB in and out a place of 2048 columns: bound by memory; 4096 places 17 us (67 MB).
 __global__ __launch_bounds__(256) void split_kernel(ProductArgs a, const float *d, int64_t ldd, int32_t *offsets2,
                                                     int32_t *rows2, bf16_t *d2, int64_t ld2) {
   const int tid = threadIdx.x;
@@ -830,7 +830,8 @@ __global__ __launch_bounds__(256) void split_kernel(ProductArgs a, const float *
       for (int i = 0; i < 8; i++) {
         const bool finite = (__float_as_uint(v[i]) & 0x7F800000u) != 0x7F800000u;
         h[i] = finite ? __uint_as_float(__float_as_uint(v[i]) & 0xFFFF0000u) : v[i];
-        l[i] = finite ? v[i] - h[i] : 0.0f;
+        l[i] = finite ? v[i] - h[i] : v[i];
+        if (l[i] == 0.0f) l[i] = h[i] * 0x1p-24f;   // not 0 unless d is: an infinity of x times it would be NaN
       }
       store8(d2 + high * ld2 + col, a.m - col, h);
       store8(d2 + low * ld2 + col, a.m - col, l);

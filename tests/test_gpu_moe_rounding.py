@@ -98,3 +98,15 @@ def test_type_of_the_rows_and_no_tokens():
     closed = P.expert_rows(torch.full((5, 2), -1, dtype=torch.int32, device=DEV), 3)
     x, dy = torch.ones(10, 8, dtype=BF, device=DEV), torch.ones(10, 16, device=DEV)
     assert not P.expert_matmul_grad(x, dy, closed, out=torch.ones(3, 8, 16, dtype=BF, device=DEV)).any()
+
+
+def test_infinite_rows_stay_infinite():
+    """An infinity of x times a finite value, or an infinity, is an infinity, whether or not the value is a bf16 number."""
+    inf = float("inf")
+    x = torch.tensor([[inf, -inf, 1.0, 0.0, 2.0, -1.0, 0.5, 3.0]])
+    d = torch.tensor([[1.0, -1.0, 1 + 2.0**-9, -(1 + 2.0**-20), 2.0**-60, inf, -inf, 0.0]])
+    plan = P.expert_rows(torch.zeros(1, 1, dtype=torch.int32, device=DEV), 1)
+    got = P.expert_matmul_grad(x.to(BF).to(DEV), d.to(DEV), plan).cpu()[0].float()
+    want = (x.double().T @ d.double()).to(BF).float()
+    assert torch.equal(got.isnan(), want.isnan())
+    assert torch.equal(got[~want.isnan()], want[~want.isnan()])
