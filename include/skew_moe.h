@@ -11,8 +11,9 @@
  * allocates nothing, never synchronises, and can be captured in a HIP graph. Results are the
  * same bits on every run (no atomic adds of floats). Sums are float32; a result in bf16 is
  * rounded once. Row strides (ld*) are in elements. Pointers may have any alignment that their
- * element type allows; 16-byte-aligned rows are the fastest. A call whose launch the device cannot take (some 2^24
- * work-groups: as many tokens, or tiles of 64 x 128 results) returns SKEW_EHIP and leaves its outputs undefined.
+ * element type allows; 16-byte-aligned rows are the fastest. Workspaces are 16-byte-aligned at
+ * least. A call whose launch the device cannot take (some 2^24 work-groups: as many tokens, or tiles
+ * of 64 x 128 results) returns SKEW_EHIP and leaves its outputs undefined.
  */
 #ifndef SKEW_MOE_H
 #define SKEW_MOE_H

@@ -13,9 +13,11 @@
 // one result row, which it stores together.
 //
 // What bounds them: with some 300 rows an expert or fewer, the bytes of W (or of dW); with more, the matrix cores.
-// Measured: 1024 tokens, top 2 of 128 experts of 2048 x 8192, forward: 674 us, W at 6.0 TB/s (a copy: 4.9). 8 experts of
-// 4096 x 11008 with 2048 rows each, forward: 1290 us, 1.15 PFLOP/s (the library's product of that size: 1.25). 32 experts
-// of 8192 x 2048 with 128 uneven rows each: backward 356 us, weights 410 us (2.7 TB/s of dW).
+// Kernel times: 1024 tokens, top 2 of 128 experts of 2048 x 8192, forward: 673 us, W at 6.0 TB/s (a copy: 4.9, reads alone: 7.1). 8
+// experts of 4096 x 11008 with 2048 rows each, forward: 1306 to 1452 us, 1.02 to 1.13 PFLOP/s (the library's product of that size:
+// 1.25). 32 experts of 8192 x 2048 with 128 uneven rows each: backward 328 to 350 us; weights 386 to 410 us from bf16 rows (2.7 TB/s of
+// dW), 497 to 528 us and 17 us for the split from float32 rows. 512 uneven rows of 2048 x 8192 each: forward 725, backward 696, weights
+// 700 us (0.79 PFLOP/s), from float32 rows 1253.
 #include <type_traits>
 
 #include "moe_internal.h"
@@ -636,8 +638,10 @@ __global__ __launch_bounds__(256, FM * FN * KS >= 64 ? 1 : FM * FN == 8 ? 3 : 2)
 // the result is at least a tile wide, its last tile is moved back inside (its results are computed twice, from the same
 // numbers in the same order), so that all chunks but those at the end of the contraction are whole; else, and
 // there, chunks are loaded element by element. At 2-byte positions that are no 4-byte ones a 16-byte load takes four
-// times as long (from L2 9.5 TB/s, else 35). 16 experts of 2765 x 1031 with 563 rows each, forward: 136 us, 0.38 PFLOP/s;
-// with 2760 x 1032, through tile_kernel: 97 us.
+// times as long (from L2 9.5 TB/s, else 35). 16 experts of 2765 x 1031 with 563 rows each, forward: 133 us, 0.39 PFLOP/s;
+// with 2760 x 1032, through tile_kernel: 97 us. Calls: forward 145, backward 154, weights 146 us; 2760 x 1032: 113, 143, 116.
+// The 4 x 8 tiles are short of registers: the compiler spills 6 vector ones forward and 15 in the weights' kernel, outside
+// the main loops.
 template <int MODE, int FM, int FN, int kSets>
 __global__ __launch_bounds__(256, 2) void any_kernel(ProductArgs a) {
   constexpr int BM = 32 * FM, BN = 32 * FN, kThreads = 256;
@@ -858,6 +862,13 @@ int64_t tiles(ProductArgs &a, int64_t bm, int64_t bn) {
 //   128              258  199  257      251  225  266      339  402
 //   256              418  326  291      407  367  290      523  515
 //   512              752  594  515      728  671  516      737  709
+// With 256 x 256 the rows of an expert that do not fill a tile cost more. Forward, 32 experts, even rows of 256, 300, 340, 380: 128 x 256
+// 352, 413, 427, 445, 256 x 256 302, 479, 474, 471; uneven ones of the same mean: 402, 418, 456, 490 and 434, 481, 510, 538. So below 384
+// it pays for rows that fill its tiles alone (and for the 380 of 8 experts of 4096 x 11008: 394, 317). Backward and for weights the two
+// are mostly within 6% of each other there, either way.
+// any_kernel takes its 128 x 256 tiles from half as many on: 16 experts of 1031 x 5001, 125 rows each, forward 73 us (64 x 128: 70),
+// 8 of 2765 x 4101, 312 rows, 154 (184), 64 of 1031 x 2051, 94 rows, 142 (134); with uneven rows 76 (82), 138 (174), 170 (137).
+// The rule looks at the mean of the rows, which the host knows; with uneven ones it can be off by the likes of the last figure.
 // Where even tiles of 64 x 128 are few, several work-groups share a contraction and join_kernel adds their parts.
 struct Choice {
   int fm, fn, parts;
@@ -875,7 +886,9 @@ Choice choose(const ProductArgs &a) {
   const int64_t part_full = a.places / 64 + a.experts;   // row tiles with those that are not full
   const int64_t row_tiles = part_full < a.places ? part_full : a.places;
   if (row_tiles * ((cols + 255) / 256) >= kEnough) return {2, 8, 1};
-  // (below 2048 the join, 3 us, costs what the shorter contractions save)
+  // (below 2048 the join, 3 us, costs about what the shorter contractions save: contractions of 1024, one | shared, in us: one token's
+  // 2 x 8192 results 10.7 | 10.4, 2 x 1024 8.8 | 7.7, 64 tokens' 128 x 1024 9.3 | 10.2; of 512 6.8 | 7.8; of 1536 14.1 | 14.6, 11.5 | 8.2,
+  // 11.6 | 11.4)
   int64_t parts = K < 2048 ? 1 : kEnough / (row_tiles * ((cols + 127) / 128));
   if (parts > K / 256) parts = K / 256;
   return {2, 4, parts > 1 ? (int)parts : 1};
@@ -947,6 +960,9 @@ ProductArgs args_of(const skew_rows &r, const skew_product_desc &p) {
   return a;
 }
 
+// The direct loads' offsets of lanes have 32 bits. Where a call names rows of x all over (gathered ones, and every place of the
+// weights' gradient) they have to lie within 2^31 bytes; beyond, any_kernel takes it. 8 experts of 8192 x 2048 on either side of that
+// line (131000 and 131100 rows): gathered forward 3565 and 4055 us, forward 3247 and 3395 (the same kernel), gradient 3259 and 4553.
 constexpr int64_t kMaxTile = 256;   // result rows, or contraction rows, that a lane's offset spans
 bool chunks(const void *p, int64_t ld) { return ((uintptr_t)p & 15) == 0 && ld % 8 == 0; }
 

@@ -5,8 +5,9 @@
 // holds a value holds its lowest index. 16 lanes a token (up to 256 experts) keep the lane steps inside a
 // row of 16, where they are one instruction each; 64 lanes hold up to 1024 experts.
 // The chosen experts go to a few words of LDS; from there lane j of the token computes weight j.
-// The vector instructions bound it where tokens are many: 40001 tokens of 192 experts, 6 chosen from 3 of 6 groups, 24 us
-// (its bytes are 4), gradient 10 us; 8192 tokens, top 2 of 128, 4 us each way.
+// The vector instructions bound it where tokens are many: 40001 tokens of 192 experts, 6 chosen from 3 of 6 groups, 30 us
+// (its bytes are 4; 6 us of it are the scores' exponentials and divisions in full), gradient 10 us; 8192 tokens, top 2 of 128, 4 us
+// each way.
 #include "moe_internal.h"
 
 namespace moe {

@@ -1,8 +1,8 @@
 // moe_tokens.hip -- what moves whole token rows: the weighted sum of expert rows back to tokens and its
 // gradients, the embedding lookup and the gradient of its table. All are bound by memory.
-// Measured: combine of 9003 float32 rows of 1031 to 3001 tokens 9.4 us (4.6 TB/s); its gradients for 2048 tokens, top 2, 2048
-// columns 11 to 15 us (42 MB); lookup of 65537 rows of 1031 floats 92 us (540 MB read and written, rows met twice among
-// them); gradient of a 50304 x 2048 bf16 table from 8192 tokens 19 us for the cuts and 50 to 65 us for the rows (206 MB
+// Measured: combine of 9003 float32 rows of 1031 to 3001 tokens 9.2 us (4.6 TB/s); its gradients for 2048 tokens, top 2, 2048
+// columns 15 to 19 us (59 MB; with dy in bf16 11 to 15, 42 MB); lookup of 65537 rows of 1031 floats 92 us (540 MB read and written, rows met twice among
+// them); gradient of a 50304 x 2048 bf16 table from 8192 tokens 18 us for the cuts and 51 to 63 us for the rows (206 MB
 // written, 3.2 to 4.1 TB/s).
 #include "moe_internal.h"
 
@@ -99,7 +99,8 @@ __global__ __launch_bounds__(kThreads) void embed_kernel(const I *ids, int64_t n
 // holds of the ids that reach over its ends (the one it begins in and the one it ends in; where the two are the
 // same id it is one part) into `part`, 2 rows of float a cut. Then a work-group per kIds rows of the table finds
 // their places, and a wave per row and 64 pieces adds the row's tokens, or its parts in order, scales once and
-// rounds once.
+// rounds once. An id's parts are added one after another, so an id that many tokens have still takes longer, if 32 times
+// less so: 65537 tokens into 32003 x 1031 floats 232 us with Zipf's law, 427 with one id in half of them, 730 in all of them.
 constexpr int kRun = 32, kIds = 16;
 
 // the first sorted place in [lo, hi) whose key is at least v, else hi
