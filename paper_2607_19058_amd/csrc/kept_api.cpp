@@ -1,0 +1,109 @@
+// kept_api.cpp -- the C ABI declared in include/skew_kept.h: argument checks, then the launchers.
+#include <hip/hip_runtime_api.h>
+
+#include "moe_checks.h"
+#include "moe_internal.h"
+#include "kept_internal.h"
+
+using namespace moe;
+
+namespace {
+
+int64_t blocks_of(int64_t cols) { return (cols + SKEW_KEPT_BLOCK - 1) / SKEW_KEPT_BLOCK; }
+// (a work-group takes 128 blocks, and the device's grid some 2^24 work-groups)
+bool kept_ok(int64_t rows, int64_t cols) {
+  return rows >= 0 && cols_ok(cols) && rows <= kMaxPlaces / blocks_of(cols);
+}
+bool codes_ok(const int8_t *codes, const uint8_t *scales) {
+  return codes != nullptr && scales != nullptr && ((uintptr_t)codes & 15) == 0;
+}
+bool act_ok(const skew_act_desc *d) {
+  if (d == nullptr || !kept_ok(d->rows, d->cols) || !type_ok(d->in_dtype) || !type_ok(d->out_dtype)) return false;
+  if (d->kind < SKEW_ACT_RELU || d->kind > SKEW_ACT_GELU_TANH) return false;
+  if ((d->codes_g == nullptr) != (d->scales_g == nullptr) || (d->codes_u == nullptr) != (d->scales_u == nullptr)) return false;
+  return ((uintptr_t)d->codes_g & 15) == 0 && ((uintptr_t)d->codes_u & 15) == 0;
+}
+bool grad_kept_ok(const skew_rows *r, const skew_product_desc *p) {
+  if (p == nullptr || p->x != nullptr || !type_ok(p->out_dtype) || !cols_ok(p->n)) return false;
+  skew_product_desc q = *p;
+  q.ldx = 32 * blocks_of(p->n);
+  if (!product_ok(r, &q, true)) return false;
+  const int64_t places = r->tokens * r->k;
+  return kept_ok(p->flags & SKEW_GATHER ? r->tokens : places, p->n) && (p->out_dtype == SKEW_BF16 || places <= kMaxPlaces / 2);
+}
+// the restored rows, and what the product needs behind them
+size_t restored_bytes(const skew_rows *r, const skew_product_desc *p) {
+  return pad256((size_t)(p->flags & SKEW_GATHER ? r->tokens : r->tokens * r->k) * blocks_of(p->n) * 64);
+}
+skew_product_desc restored(const skew_product_desc *p, void *workspace) {
+  skew_product_desc q = *p;
+  q.x = workspace;
+  q.ldx = 32 * blocks_of(p->n);
+  return q;
+}
+
+}  // namespace
+
+extern "C" {
+
+int skew_keep8(const void *x, int32_t dtype, int64_t rows, int64_t cols, int64_t ldx, int8_t *codes, uint8_t *scales,
+               void *stream) {
+  if (!type_ok(dtype) || !kept_ok(rows, cols) || !ld_ok(ldx, cols, rows)) return SKEW_EINVAL;
+  if (rows == 0) return SKEW_OK;
+  if (x == nullptr || !codes_ok(codes, scales)) return SKEW_EINVAL;
+  return status(launch_keep8(x, dtype, rows, cols, ldx, codes, scales, stream));
+}
+
+int skew_restore8(const int8_t *codes, const uint8_t *scales, int64_t rows, int64_t cols, void *x, int32_t dtype,
+                  int64_t ldx, void *stream) {
+  if (!type_ok(dtype) || !kept_ok(rows, cols) || !ld_ok(ldx, cols, rows)) return SKEW_EINVAL;
+  if (rows == 0) return SKEW_OK;
+  if (x == nullptr || !codes_ok(codes, scales)) return SKEW_EINVAL;
+  return status(launch_restore8(codes, scales, rows, cols, x, dtype, ldx, stream));
+}
+
+int skew_expert_act(const skew_act_desc *d, void *stream) {
+  if (!act_ok(d) || !ld_ok(d->ldg, d->cols, d->rows) || !ld_ok(d->lda, d->cols, d->rows)) return SKEW_EINVAL;
+  if (d->codes_u != nullptr && (d->codes_g == nullptr || d->u == nullptr)) return SKEW_EINVAL;
+  if (d->u != nullptr && !ld_ok(d->ldu, d->cols, d->rows)) return SKEW_EINVAL;
+  if (d->rows == 0) return SKEW_OK;
+  if (d->g == nullptr || d->a == nullptr) return SKEW_EINVAL;
+  return status(launch_act(*d, stream));
+}
+
+int skew_expert_act_backward(const skew_act_desc *d, void *stream) {
+  if (!act_ok(d) || !ld_ok(d->ldda, d->cols, d->rows) || !ld_ok(d->lddg, d->cols, d->rows)) return SKEW_EINVAL;
+  if (d->a != nullptr && !ld_ok(d->lda, d->cols, d->rows)) return SKEW_EINVAL;
+  if (d->codes_u != nullptr && !ld_ok(d->lddu, d->cols, d->rows)) return SKEW_EINVAL;
+  if (d->rows == 0) return SKEW_OK;
+  if (d->da == nullptr || d->dg == nullptr || d->codes_g == nullptr) return SKEW_EINVAL;
+  if ((d->codes_u == nullptr) != (d->du == nullptr)) return SKEW_EINVAL;
+  return status(launch_act_backward(*d, stream));
+}
+
+int skew_expert_matmul_grad_kept_bytes(const skew_rows *r, const skew_product_desc *p, size_t *bytes) {
+  if (!grad_kept_ok(r, p) || bytes == nullptr) return SKEW_EINVAL;
+  *bytes = 0;
+  if (r->tokens > 0)
+    *bytes = restored_bytes(r, p) + (p->out_dtype == SKEW_F32 ? product_grad_f32_scratch(*r, restored(p, nullptr)) : 0);
+  return SKEW_OK;
+}
+
+int skew_expert_matmul_grad_kept(const skew_rows *r, const skew_product_desc *p, const int8_t *codes, const uint8_t *scales,
+                                 void *workspace, size_t workspace_bytes, void *stream) {
+  size_t need;
+  if (skew_expert_matmul_grad_kept_bytes(r, p, &need) != SKEW_OK || p->w == nullptr) return SKEW_EINVAL;
+  if (r->tokens == 0) return status(launch_product_grad(*r, *p, stream));   // (nothing but dW is touched)
+  if (p->y == nullptr || !codes_ok(codes, scales)) return SKEW_EINVAL;
+  if (workspace_bytes < need) return SKEW_ENOSPACE;
+  if (workspace == nullptr) return SKEW_EINVAL;
+  const int64_t rows = p->flags & SKEW_GATHER ? r->tokens : r->tokens * r->k;
+  const skew_product_desc q = restored(p, workspace);
+  // whole blocks: the columns past a row's end are 0, as their codes are
+  const int e = launch_restore8(codes, scales, rows, q.ldx, workspace, SKEW_BF16, q.ldx, stream);
+  if (e != (int)hipSuccess) return SKEW_EHIP;
+  char *rest = static_cast<char *>(workspace) + restored_bytes(r, p);
+  return status(p->out_dtype == SKEW_F32 ? launch_product_grad_f32(*r, q, rest, stream) : launch_product_grad(*r, q, stream));
+}
+
+}  // extern "C"

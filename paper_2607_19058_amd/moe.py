@@ -78,6 +78,16 @@ class ExpertRows(NamedTuple):
     slots: "torch.Tensor"     # noqa: F821
 
 
+class Kept8(NamedTuple):
+    """Rows in 8 bits (see `keep8`): blocks of 32 neighbours of a row share a power of two.
+
+    ``codes`` int8 (R, 32 B), B = ceil(cols / 32); ``scales`` uint8 (R, B): code times 2^(scale - 127), NaN for code -128.
+    """
+    codes: "torch.Tensor"     # noqa: F821
+    scales: "torch.Tensor"    # noqa: F821
+    cols: int
+
+
 _READY = None
 
 
@@ -361,8 +371,11 @@ def expert_matmul_grad(x, dy, plan, *, gather=False, out=None, stream=None):
     """The weights' gradient bf16 (E, n, m): each expert's sum of x's rows (one a place, or with ``gather`` one a
     token) times ``dy`` (T k, m), bf16 or float32; zero for an expert without rows. A float32 ``dy`` is taken as
     two bf16 numbers (2^-16 of a value is left out), in up to twice the time. ``out`` takes an existing
-    tensor, such as the gradient that an optimizer was given."""
+    tensor, such as the gradient that an optimizer was given. ``x`` may be rows kept in 8 bits (`Kept8`)."""
     import torch
+    if isinstance(x, Kept8):
+        from .kept import _matmul_grad_kept
+        return _matmul_grad_kept(x, dy, plan, gather, out, stream)
     _no_autograd(x, dy, out)
     _tensor(x, "x", (torch.bfloat16,), 2)
     _tensor(dy, "dy", (torch.bfloat16, torch.float32), 2, x.device)
