@@ -5,3 +5,4 @@ from .skewadam import (BACKBONE, EXPERT, ROUTER, TIERS, STATE_MOMENTUM, STATE_FA
 from .moe import (ExpertRows, Kept8, embed, embed_grad, expert_combine, expert_combine_backward,  # noqa: F401
                   expert_matmul, expert_matmul_grad, expert_rows, route, route_backward)
 from .kept import expert_act, expert_act_backward, keep8, restore8  # noqa: F401
+from .loss import head_loss, head_loss_backward  # noqa: F401

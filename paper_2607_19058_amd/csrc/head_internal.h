@@ -1,0 +1,76 @@
+// head_internal.h -- what the kernels of the head's loss share.
+#pragma once
+
+#include "../../include/skew_loss.h"
+#include "moe_internal.h"
+
+namespace moe {
+
+// A token as the gradients' kernels take it: the base-2 exponent of its sum, the logits' gradient's factors times the power
+// of two that G is kept with, and its target (-1: no token).
+struct HeadRow {
+  float l2, both, one;
+  int32_t target;
+};
+
+// One product of the head on the tiles of product_tiles.h. Operands are padded to chunks of 8 in both directions; rows, cols and n8, m8
+// say where the result ends and where its operands do.
+struct HeadProduct {
+  const void *a, *b;          // kForward: a rows, b [K x cols]; kBackward: b [cols x K]; kOuter: a [K x rows], b [K x cols]
+  int64_t lda, ldb;
+  int64_t rows, cols, K;      // of the result, and the contraction
+  int64_t pad_rows, pad_cols; // kOuter: a's columns; b's columns or rows
+};
+
+// Forward: of each row and each run of 128 (or 64, ...) columns that a wave has, the largest base-2 exponent and the sum
+// of the powers relative to it; the logit of the row's target.
+struct HeadForward {
+  float c;                    // scale log2(e)
+  const void *targets;
+  int32_t target_bytes;
+  int64_t vocab, col0;        // of the whole; the first column of this product
+  float2 *part;               // [rows x part_ld], runs of this product from part_at on
+  int64_t part_ld, part_at;
+  float *target_sum;          // [rows]: <x, w_y>
+};
+int head_parts(int mode, const HeadProduct &p);   // runs that a row's columns fall into
+int launch_head_forward(int mode, const HeadProduct &p, const HeadForward &f, void *stream);
+
+// Backward: G of this product's columns, float16 [rows x ldg].
+struct HeadGrad {
+  float c;
+  const HeadRow *row;
+  int64_t vocab, col0;
+  uint16_t *g;
+  int64_t ldg;
+};
+int launch_head_grad(int mode, const HeadProduct &p, const HeadGrad &g, void *stream);
+
+// result = 2^e (a b) + prev, of float16 operands. e is minus an exponent that G is kept with, plus those that the rows or columns of the other
+// operand are kept with (top: bits of their largest magnitudes).
+struct HeadResult {
+  void *y;
+  int64_t ldy;
+  int32_t y_dtype;
+  const float *prev;          // NULL, or float [rows x ldprev] that is added
+  int64_t ldprev;
+  const uint32_t *top, *coef; // per column, or per row; of G's coefficients
+  int32_t by_row;
+};
+size_t head_result_scratch(int mode, const HeadProduct &p);
+int launch_head_result(int mode, const HeadProduct &p, const HeadResult &r, char *ws, void *stream);
+
+// Exponents of what is kept in float16: a value whose largest magnitude has the bits `top` is kept times 2^-exponent, so
+// that the largest lies in [2^14, 2^15).
+constexpr int kHalfTop = 14;
+__host__ __device__ inline int half_exponent(uint32_t top) { return (int)(top >> 23) - 127 - kHalfTop; }
+
+// The calls of skew_loss.h, after their checks.
+size_t head_forward_scratch(const skew_head_desc &h);
+size_t head_backward_scratch(const skew_head_desc &h);
+int launch_fill_zero(void *dw, int64_t rows, int64_t cols, int64_t ld, void *stream);   // bf16
+int launch_head_loss(const skew_head_desc &h, float *loss, float *lse, char *ws, void *stream);
+int launch_head_loss_backward(const skew_head_desc &h, const float *lse, const float *dloss, const float *dlse, void *dx, int dx_dtype,
+                              int64_t lddx, void *dw, int64_t lddw, char *ws, void *stream);
+
+}  // namespace moe

@@ -1,0 +1,222 @@
+// head_logits.hip -- the head's logits on the matrix cores, taken from the sums' registers: their softmax sums, and
+// their gradient. No logit reaches memory.
+//
+// A lane of a finished tile holds rows lane % 16 of FM blocks and 4 FN of each row's columns. Forward it finds their largest, adds up powers of
+// two relative to it, and joins four lanes; a wave writes one pair for each row. Backward a logit becomes its gradient in
+// place, which leaves through LDS as float16. Per logit that is some 32 cycles of a SIMD (16 of them the exponential's), 8200 for a tile of
+// 256 x 256, beside its 64 K / 32 matrix instructions of 16.
+#include "head_internal.h"
+#include "product_tiles.h"
+
+namespace moe {
+namespace {
+
+__device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }   // (1 ulp; 0 below 2^-126)
+
+// The tile of a product without experts.
+template <int MODE, int BM, int BN>
+__device__ __forceinline__ bool take_plain(const ProductArgs &a, Tile *t) {
+  uint32_t tr, tc;
+  t->expert = 0;
+  t->first = 0;
+  t->r1 = a.places;
+  t->c1 = MODE == kBackward ? a.n : a.m;
+  t->K = (int)(MODE == kBackward ? a.m : a.n);
+  if (!patch_tile(a.in_patches, (uint32_t)a.row_tiles, ((uint32_t)t->c1 + BN - 1) / BN, &tr, &tc)) return false;
+  t->r0 = (int64_t)tr * BM;
+  t->c0 = (int64_t)tc * BN;
+  return true;
+}
+
+// The element of a lane's 4 FN values that is column `at` of the wave's columns, if the lane has it.
+template <int FN>
+__device__ __forceinline__ bool pick(const f32x4 (&acc)[FN], int at, float *v) {
+  const bool mine = at >= 0 && at < 16 * FN && ((at >> 2) & 3) == (int)((threadIdx.x & 63) >> 4);
+  if (__ballot(mine) == 0) return false;
+#pragma unroll
+  for (int j = 0; j < FN; j++)
+#pragma unroll
+    for (int q = 0; q < 4; q++)
+      if ((at >> 4) == j && (at & 3) == q) *v = acc[j][q];
+  return mine;
+}
+
+struct ForwardOp {
+  static constexpr bool kHalf = false;
+  HeadForward f;
+  template <int MODE, int BM, int BN>
+  __device__ __forceinline__ bool take(const ProductArgs &a, Tile *t) const {
+    return take_plain<MODE, BM, BN>(a, t);
+  }
+  template <int MODE, int FM, int FN>
+  __device__ __forceinline__ void finish(const ProductArgs &a, const Tile &t, int wr, int wc, const f32x4 (&acc)[FM][FN], char *) const {
+    const int lane = threadIdx.x & 63;
+    const int64_t col_w = t.c0 + wc, row_w = t.r0 + wr + (lane & 15);
+    const int64_t left = f.vocab - f.col0 - col_w;   // columns of the vocabulary from the wave's first on
+    const bool whole = left >= 16 * FN;
+    const int mine = (int)(left < 16 * FN ? left : 16 * FN) - (lane >> 4) * 4;
+#pragma unroll
+    for (int i = 0; i < FM; i++) {
+      const int64_t row = row_w + i * 16;
+      f32x4 v[FN];
+#pragma unroll
+      for (int j = 0; j < FN; j++) {
+        v[j] = acc[i][j];
+        if (!whole) {
+#pragma unroll
+          for (int q = 0; q < 4; q++)
+            if (j * 16 + q >= mine) v[j][q] = -INFINITY;
+        }
+      }
+      int64_t y = -1;
+      if (row < t.r1) y = f.target_bytes == 8 ? static_cast<const int64_t *>(f.targets)[row] : static_cast<const int32_t *>(f.targets)[row];
+      const int64_t at = y - f.col0 - col_w;
+      float z;
+      if (pick<FN>(v, y >= 0 && y < f.vocab && at >= 0 && at < 16 * FN ? (int)at : -1, &z)) f.target_sum[row] = z;
+      float m = v[0][0];
+#pragma unroll
+      for (int j = 0; j < FN; j++)
+#pragma unroll
+        for (int q = 0; q < 4; q++) m = fmaxf(m, v[j][q]);
+      m *= f.c;
+      const float base = m == -INFINITY ? 0.0f : m;   // (columns past the end alone)
+      float s = 0.0f;
+#pragma unroll
+      for (int j = 0; j < FN; j++)
+#pragma unroll
+        for (int q = 0; q < 4; q++) s += exp2_(__builtin_fmaf(v[j][q], f.c, -base));
+      const float m16 = fmaxf(m, __shfl_xor(m, 16)), top = fmaxf(m16, __shfl_xor(m16, 32));
+      s *= exp2_(m - (top == -INFINITY ? 0.0f : top));
+      s += __shfl_xor(s, 16);
+      s += __shfl_xor(s, 32);
+      if (lane < 16 && row < t.r1) f.part[row * f.part_ld + f.part_at + col_w / (16 * FN)] = make_float2(top, s);
+    }
+  }
+};
+
+struct GradOp {
+  static constexpr bool kHalf = false;
+  HeadGrad g;
+  template <int MODE, int BM, int BN>
+  __device__ __forceinline__ bool take(const ProductArgs &a, Tile *t) const {
+    return take_plain<MODE, BM, BN>(a, t);
+  }
+  template <int MODE, int FM, int FN>
+  __device__ __forceinline__ void finish(const ProductArgs &a, const Tile &t, int wr, int wc, const f32x4 (&acc)[FM][FN],
+                                         char *room) const {
+    typedef uint16_t __attribute__((may_alias)) u16;
+    const int lane = threadIdx.x & 63;
+    const int64_t col_w = t.c0 + wc, row_w = t.r0 + wr;
+    const int64_t left = g.vocab - g.col0 - col_w;
+    const bool whole = left >= 16 * FN;
+    const int mine = (int)(left < 16 * FN ? left : 16 * FN) - (lane >> 4) * 4;
+    auto half = [](float x) { return __builtin_bit_cast(uint16_t, (_Float16)x); };
+#pragma unroll
+    for (int i = 0; i < FM; i++) {
+      const int64_t row = row_w + i * 16 + (lane & 15);
+      HeadRow r = {0.0f, 0.0f, 0.0f, -1};
+      if (row < t.r1) r = g.row[row];
+      const bool token = r.target >= 0;
+#pragma unroll
+      for (int j = 0; j < FN; j++) {
+        uint16_t h[4];
+#pragma unroll
+        for (int q = 0; q < 4; q++) {
+          float v = r.both * exp2_(__builtin_fmaf(acc[i][j][q], g.c, -r.l2));
+          if (!whole && j * 16 + q >= mine) v = 0.0f;
+          h[q] = half(token ? v : 0.0f);   // (a row that is no token may hold NaN)
+        }
+        put_room<FN>(room, i, j, make_uint2(h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16));
+      }
+      const int64_t at = r.target - g.col0 - col_w;
+      const int k = token && at >= 0 && at < 16 * FN ? (int)at : -1;
+      float z;
+      if (pick<FN>(acc[i], k, &z)) {   // both p - one, where p is near 1: (both - one) p + one (p - 1)
+        const float d = __builtin_fmaf(z, g.c, -r.l2);
+        const float v = __builtin_fmaf(r.both - r.one, exp2_(d), r.one * expm1f(d * 0.6931471805599453f));
+        const int row16 = i * 16 + (lane & 15);
+        *reinterpret_cast<u16 *>(room + row16 * (FN * 32) + ((k >> 3) ^ (row16 & 7)) * 16 + (k & 7) * 2) = half(v);
+      }
+    }
+    store_room<FM, FN, true>(room, g.g + row_w * g.ldg + col_w, g.ldg, t.r1 - row_w, t.c1 - col_w);
+  }
+};
+
+template <int MODE, int FM, int FN, int NS, int KS, class Op>
+__global__ __launch_bounds__(256, per_unit(FM, FN, KS)) void logits_kernel(ProductArgs a, Op op) {
+  tile_body<MODE, FM, FN, NS, KS>(a, op);
+}
+
+int tile_rows(int s) { return s == 0 ? 256 : s == 1 ? 128 : 64; }
+int tile_cols(int s) { return s == 3 ? 128 : 256; }
+
+// Which tile: the one whose rounds over the chip take the least time.
+int choose_logits(int mode, const HeadProduct &p) {
+  // a round of tiles of 256 x 256, 128 x 256, 64 x 256 and 64 x 128 with their work-groups on every compute unit takes this, relatively
+  const double round[4] = {1.0, mode == kBackward ? 0.58 : 1.15, 0.73, 0.68};
+  const int slots[4] = {256, mode == kBackward ? 256 : 512, 512, 768};
+  int best = 0;
+  double least = 1e300;
+  for (int s = 0; s < 4; s++) {
+    const int64_t n = ((p.rows + tile_rows(s) - 1) / tile_rows(s)) * ((p.cols + tile_cols(s) - 1) / tile_cols(s));
+    const double t = (double)((n + slots[s] - 1) / slots[s]) * round[s];
+    if (t < least) {
+      least = t;
+      best = s;
+    }
+  }
+  return best;
+}
+
+ProductArgs args_of(const HeadProduct &p, int mode, int tile) {
+  ProductArgs a = {};
+  a.x = static_cast<const bf16_t *>(p.a);
+  a.w = static_cast<const bf16_t *>(p.b);
+  a.ldx = p.lda;
+  a.ldw = p.ldb;
+  a.places = p.rows;
+  a.n = mode == kBackward ? p.pad_cols : p.K;
+  a.m = mode == kBackward ? p.K : p.pad_cols;
+  a.k = 1;
+  a.experts = 1;
+  a.row_tiles = (p.rows + tile_rows(tile) - 1) / tile_rows(tile);
+  a.in_patches = patches(a.row_tiles, (p.pad_cols + tile_cols(tile) - 1) / tile_cols(tile)) >= kMinPatches;
+  return a;
+}
+
+template <class Op, int MODE, int FM, int FN, int NS, int KS>
+int launch_one(const HeadProduct &p, const Op &op, int tile, void *stream) {
+  const ProductArgs a = args_of(p, MODE, tile);
+  const int64_t grid = patch_grid(a.row_tiles, (p.pad_cols + 32 * FN - 1) / (32 * FN), a.in_patches);
+  if (grid > 0x7FFFFFFF) return (int)hipErrorInvalidConfiguration;
+  logits_kernel<MODE, FM, FN, NS, KS, Op><<<(unsigned)grid, 256, 0, static_cast<hipStream_t>(stream)>>>(a, op);
+  return (int)hipGetLastError();
+}
+template <class Op, int MODE>
+int launch_mode(const HeadProduct &p, const Op &op, void *stream) {
+  constexpr int S = MODE == kBackward ? 2 : 1;
+  const int tile = choose_logits(MODE, p);
+  switch (tile) {
+    case 0: return launch_one<Op, MODE, 8, 8, 4 / S, S>(p, op, tile, stream);
+    case 1: return launch_one<Op, MODE, 4, 8, 3, S>(p, op, tile, stream);
+    case 2: return launch_one<Op, MODE, 2, 8, 4 / S, S>(p, op, tile, stream);
+    default: return launch_one<Op, MODE, 2, 4, 4 / S, S>(p, op, tile, stream);
+  }
+}
+
+}  // namespace
+
+int head_parts(int mode, const HeadProduct &p) {
+  const int cols = tile_cols(choose_logits(mode, p));
+  return (int)((p.cols + cols - 1) / cols) * 2;
+}
+int launch_head_forward(int mode, const HeadProduct &p, const HeadForward &f, void *stream) {
+  const ForwardOp op = {f};
+  return mode == kBackward ? launch_mode<ForwardOp, kBackward>(p, op, stream) : launch_mode<ForwardOp, kForward>(p, op, stream);
+}
+int launch_head_grad(int mode, const HeadProduct &p, const HeadGrad &g, void *stream) {
+  const GradOp op = {g};
+  return mode == kBackward ? launch_mode<GradOp, kBackward>(p, op, stream) : launch_mode<GradOp, kForward>(p, op, stream);
+}
+
+}  // namespace moe

@@ -1,0 +1,439 @@
+// head_loss.hip -- the head's loss: the order of its products, and the small kernels around them.
+//
+//   forward   logits' tiles -> a pair (largest, sum) for each row and run of columns -> loss and lse
+//   backward  x and, piece by piece of the vocabulary, w to float16 beside powers of two; logits' tiles again -> G of the piece
+//             (float16) -> dx += G w^T, the piece of dw = x^T G
+//
+// G is rounded before the products that it enters. In bf16 that would be an error of the size of the results' own rounding; in float16,
+// which the matrix cores take at the same rate, it is an eighth. That needs float16 x and w: w is converted piece by
+// piece (a pass of its bytes, twice read and once written), x once.
+#include <algorithm>
+
+#include "head_internal.h"
+
+namespace moe {
+namespace {
+
+enum { kForward = 0, kBackward = 1, kOuter = 3 };   // as in product_tiles.h
+constexpr int kThreads = 256;
+
+__device__ __forceinline__ int64_t id_at(const void *ids, int bytes, int64_t i) {
+  return bytes == 8 ? static_cast<const int64_t *>(ids)[i] : static_cast<const int32_t *>(ids)[i];
+}
+__device__ __forceinline__ bool is_token(const skew_head_desc &h, int64_t t) {
+  const int64_t y = id_at(h.targets, h.target_bytes, t);
+  return y >= 0 && y < h.vocab;
+}
+__device__ __forceinline__ uint32_t finite_bits(float x) {
+  const uint32_t m = __float_as_uint(x) & 0x7FFFFFFFu;
+  return m < 0x7F800000u ? m : 0u;
+}
+
+__global__ __launch_bounds__(kThreads) void zero_kernel(uint32_t *p, int n) {
+  const int i = blockIdx.x * kThreads + threadIdx.x;
+  if (i < n) p[i] = 0;
+}
+
+__global__ __launch_bounds__(kThreads) void fill_zero_kernel(bf16_t *p, int64_t rows, int64_t cols, int64_t ld) {
+  const Chunks c(rows, (cols + 7) / 8, kThreads);
+  const Place at = c.at(0);
+  const float v[8] = {};
+  if (at.there) store8(p + at.row * ld + at.col, cols - at.col, v);
+}
+
+// loss and lse of a row from its pairs: a wave a row.
+__global__ __launch_bounds__(kThreads) void loss_kernel(skew_head_desc h, float c, const float2 *part, int64_t ld, int parts,
+                                                        const float *target_sum, float *loss, float *lse) {
+  const int64_t t = (int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63;
+  if (t >= h.tokens) return;
+  float m = -INFINITY, s = 0.0f;
+  for (int i = lane; i < parts; i += 64) {
+    const float2 p = part[t * ld + i];
+    const float top = fmaxf(m, p.x), base = top == -INFINITY ? 0.0f : top;   // (a run past the end has -inf and 0)
+    s = s * __builtin_amdgcn_exp2f(m - base) + p.y * __builtin_amdgcn_exp2f(p.x - base);
+    m = top;
+  }
+  for (int o = 32; o > 0; o >>= 1) {
+    const float m2 = __shfl_xor(m, o), s2 = __shfl_xor(s, o), top = fmaxf(m, m2), base = top == -INFINITY ? 0.0f : top;
+    s = s * __builtin_amdgcn_exp2f(m - base) + s2 * __builtin_amdgcn_exp2f(m2 - base);
+    m = top;
+  }
+  if (lane == 0) {
+    const bool token = is_token(h, t);
+    const double all = ((double)m + log2((double)s)) * ((double)h.scale / (double)c);
+    lse[t] = token ? (float)all : 0.0f;
+    loss[t] = token ? (float)(all - (double)h.scale * (double)target_sum[t]) : 0.0f;
+  }
+}
+
+// Largest magnitudes, as bits, of the columns of `rows` x cols values (those of tokens, where h is given): top has to be zero before.
+// A work-group takes 256 columns of 128 rows, a thread 8 columns of every eighth row.
+constexpr int kTopRows = 128;
+__global__ __launch_bounds__(kThreads) void column_top_kernel(const bf16_t *x, int64_t ld, int64_t rows, int64_t cols, skew_head_desc h,
+                                                              int masked, uint32_t *top) {
+  __shared__ uint32_t held[kThreads][9];
+  const int64_t strips = (cols + 255) / 256, strip = blockIdx.x % strips, row0 = blockIdx.x / strips * kTopRows;
+  const int lane = threadIdx.x & 31;
+  const int64_t col = strip * 256 + lane * 8;
+  uint32_t m[8] = {};
+#pragma unroll 4
+  for (int i = threadIdx.x >> 5; i < kTopRows; i += 8) {
+    const int64_t row = row0 + i;
+    if (row >= rows || col >= cols || (masked && !is_token(h, row))) continue;
+    float v[8];
+    load8(x + row * ld + col, cols - col, v);
+#pragma unroll
+    for (int q = 0; q < 8; q++) m[q] = max(m[q], finite_bits(v[q]));
+  }
+#pragma unroll
+  for (int q = 0; q < 8; q++) held[threadIdx.x][q] = m[q];
+  __syncthreads();
+  const int c = threadIdx.x;   // a thread a column
+  uint32_t all = 0;
+  for (int i = 0; i < 8; i++) all = max(all, held[i * 32 + c / 8][c % 8]);
+  if (strip * 256 + c < cols && all) atomicMax(top + strip * 256 + c, all);
+}
+
+// The factors of G's rows: their largest sum, as bits (zero before).
+__device__ __forceinline__ void factors(const skew_head_desc &h, const float *dloss, const float *dlse, int64_t t, float *both, float *one) {
+  *one = h.scale * dloss[t];
+  *both = dlse ? h.scale * (dloss[t] + dlse[t]) : *one;
+}
+__global__ __launch_bounds__(kThreads) void factor_top_kernel(skew_head_desc h, const float *dloss, const float *dlse, uint32_t *top) {
+  __shared__ uint32_t held[kThreads];
+  uint32_t m = 0;
+  for (int64_t t = (int64_t)blockIdx.x * kThreads + threadIdx.x; t < h.tokens; t += (int64_t)gridDim.x * kThreads)
+    if (is_token(h, t)) {
+      float both, one;
+      factors(h, dloss, dlse, t, &both, &one);
+      m = max(m, finite_bits(fabsf(both) + fabsf(one)));
+    }
+  held[threadIdx.x] = m;
+  for (int o = kThreads / 2; o > 0; o >>= 1) {
+    __syncthreads();
+    if (threadIdx.x < o) held[threadIdx.x] = max(held[threadIdx.x], held[threadIdx.x + o]);
+  }
+  if (threadIdx.x == 0 && held[0]) atomicMax(top, held[0]);
+}
+__global__ __launch_bounds__(kThreads) void rows_kernel(skew_head_desc h, float c, const float *lse, const float *dloss, const float *dlse,
+                                                        const uint32_t *top, HeadRow *row) {
+  const int64_t t = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+  if (t >= h.tokens) return;
+  HeadRow r = {0.0f, 0.0f, 0.0f, -1};
+  if (is_token(h, t)) {
+    factors(h, dloss, dlse, t, &r.both, &r.one);
+    const int e = half_exponent(*top);
+    r.both = __builtin_ldexpf(r.both, -e);
+    r.one = __builtin_ldexpf(r.one, -e);
+    r.l2 = (float)((double)lse[t] * ((double)c / (double)h.scale));
+    r.target = (int32_t)id_at(h.targets, h.target_bytes, t);
+  }
+  row[t] = r;
+}
+
+__device__ __forceinline__ void store_half8(uint16_t *p, const float *v, const int *e) {
+  u32x4 u;
+#pragma unroll
+  for (int i = 0; i < 4; i++) {
+    const uint16_t a = __builtin_bit_cast(uint16_t, (_Float16)__builtin_ldexpf(v[2 * i], -e[2 * i]));
+    const uint16_t b = __builtin_bit_cast(uint16_t, (_Float16)__builtin_ldexpf(v[2 * i + 1], -e[2 * i + 1]));
+    u[i] = a | (uint32_t)b << 16;
+  }
+  *reinterpret_cast<u32x4 *>(p) = u;
+}
+
+// Values to whole rows of whole chunks (rows8 x cols8, zeros past rows and cols): float16 beside their columns' powers of two (half),
+// and as they are (copy). Rows that are no token are zeros where h is given.
+struct Padded {
+  const bf16_t *x;
+  int64_t ld, rows, cols, rows8, cols8;
+  uint16_t *half;
+  bf16_t *copy;
+  const uint32_t *top;
+  int masked;
+};
+__global__ __launch_bounds__(kThreads) void pad_kernel(Padded p, skew_head_desc h) {
+  const Chunks c(p.rows8, p.cols8 / 8, kThreads);
+  const Place at = c.at(0);
+  if (!at.there) return;
+  float v[8] = {};
+  if (at.row < p.rows && (!p.masked || is_token(h, at.row))) load8(p.x + at.row * p.ld + at.col, p.cols - at.col, v);
+  const int64_t to = at.row * p.cols8 + at.col;
+  if (p.half) {
+    int e[8];
+#pragma unroll
+    for (int q = 0; q < 8; q++) e[q] = half_exponent(at.col + q < p.cols ? p.top[at.col + q] : 0);
+    store_half8(p.half + to, v, e);
+  }
+  if (p.copy) store8(p.copy + to, 8, v);
+}
+// The same beside the rows' powers of two, whose largest magnitudes it finds: a work-group a row.
+__global__ __launch_bounds__(kThreads) void pad_rows_kernel(Padded p, uint32_t *top) {
+  __shared__ uint32_t held[kThreads];
+  const int64_t row = blockIdx.x;
+  const bf16_t *x = p.x + row * p.ld;
+  uint32_t m = 0;
+  if (row < p.rows) {
+#pragma unroll 4
+    for (int64_t col = threadIdx.x * 8; col < p.cols; col += kThreads * 8) {
+      float v[8];
+      load8(x + col, p.cols - col, v);
+#pragma unroll
+      for (int q = 0; q < 8; q++) m = max(m, finite_bits(v[q]));
+    }
+  }
+  held[threadIdx.x] = m;
+  for (int o = kThreads / 2; o > 0; o >>= 1) {
+    __syncthreads();
+    if (threadIdx.x < o) held[threadIdx.x] = max(held[threadIdx.x], held[threadIdx.x + o]);
+  }
+  __syncthreads();
+  const uint32_t all = held[0];
+  if (threadIdx.x == 0) top[row] = all;
+  int e[8];
+#pragma unroll
+  for (int q = 0; q < 8; q++) e[q] = half_exponent(all);
+#pragma unroll 4
+  for (int64_t col = threadIdx.x * 8; col < p.cols8; col += kThreads * 8) {
+    float v[8] = {};
+    if (row < p.rows) load8(x + col, p.cols - col, v);
+    store_half8(p.half + row * p.cols8 + col, v, e);
+    if (p.copy) store8(p.copy + row * p.cols8 + col, 8, v);
+  }
+}
+
+int64_t up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
+bool chunks(const void *p, int64_t ld) { return ((uintptr_t)p & 15) == 0 && ld % 8 == 0; }
+bool tied(const skew_head_desc &h) { return (h.flags & SKEW_TRANSPOSE) != 0; }
+
+// What is the same in both calls: which operands the tiles take as they are, and pieces of the vocabulary (of kPieceStep columns,
+// the last one of what is left).
+constexpr int64_t kTileRows = 256, kPieceStep = 256, kMaxPiece = 1 << 21;
+constexpr int64_t kPieceBytes = (int64_t)512 << 20;   // of G, and of a copy of w
+constexpr int64_t kRun = 16384;                       // rows of a forward launch, whose pairs are held
+struct HeadPlan {
+  bool x_as_is, w_as_is;
+  int64_t d8, v8, piece, run;
+};
+HeadPlan head_plan(const skew_head_desc &h, bool backward) {
+  HeadPlan p;
+  p.d8 = up(h.d, 8);
+  p.v8 = up(h.vocab, 8);
+  p.x_as_is = chunks(h.x, h.ldx) && h.d % 8 == 0 && short_rows(kTileRows, h.ldx);
+  p.w_as_is = chunks(h.w, h.ldw) && h.d % 8 == 0 && h.vocab % 8 == 0 && short_rows(kTileRows, h.ldw);
+  p.run = std::min(h.tokens, kRun);
+  if (!backward && p.w_as_is) {
+    p.piece = h.vocab;
+  } else {
+    const int64_t wide = std::max(p.d8, backward ? h.tokens : 0);   // rows of G, columns of w
+    int64_t most = std::min(std::max(kPieceBytes / (2 * wide), kPieceStep), kMaxPiece);
+    const int64_t n = (h.vocab + most - 1) / most;
+    p.piece = std::min(up((h.vocab + n - 1) / n, kPieceStep), p.v8);
+  }
+  return p;
+}
+int64_t pieces(const skew_head_desc &h, const HeadPlan &p) { return (h.vocab + p.piece - 1) / p.piece; }
+int64_t piece_cols(const skew_head_desc &h, const HeadPlan &p, int64_t v0) { return std::min(p.piece, h.vocab - v0); }
+
+// w from word v0 on, as it is
+const bf16_t *words(const skew_head_desc &h, int64_t v0) {
+  return static_cast<const bf16_t *>(h.w) + (tied(h) ? v0 * h.ldw : v0);
+}
+// x w of rows `rows` and the piece at v0 of `cols` words: from (a, lda) and w or its copy
+HeadProduct logits_of(const skew_head_desc &h, const HeadPlan &p, const void *a, int64_t lda, int64_t rows, int64_t v0, const void *copy) {
+  const int64_t cols = piece_cols(h, p, v0), cols8 = up(cols, 8);
+  HeadProduct q = {a, copy ? copy : words(h, v0), lda, copy ? (tied(h) ? p.d8 : cols8) : h.ldw, rows, cols, p.d8, 0, cols8};
+  return q;
+}
+// (shapes alone)
+int mode_of(const skew_head_desc &h) { return tied(h) ? kBackward : kForward; }
+
+int launch_pad(const Padded &p, const skew_head_desc &h, hipStream_t s) {
+  const int64_t grid = (p.rows8 * (p.cols8 / 8) + kThreads - 1) / kThreads;
+  if (grid > 0x7FFFFFFF) return (int)hipErrorInvalidConfiguration;
+  pad_kernel<<<(unsigned)grid, kThreads, 0, s>>>(p, h);
+  return (int)hipGetLastError();
+}
+// the piece of w at v0, padded
+Padded piece_of(const skew_head_desc &h, const HeadPlan &p, int64_t v0, uint16_t *half, bf16_t *copy, const uint32_t *top) {
+  const int64_t cols = piece_cols(h, p, v0), cols8 = up(cols, 8);
+  if (tied(h)) return {words(h, v0), h.ldw, cols, h.d, cols8, p.d8, half, copy, top, 0};
+  return {words(h, v0), h.ldw, h.d, cols, p.d8, cols8, half, copy, top, 0};
+}
+int launch_column_top(const bf16_t *x, int64_t ld, int64_t rows, int64_t cols, const skew_head_desc &h, bool masked, uint32_t *top,
+                      hipStream_t s) {
+  const int64_t grid = ((cols + 255) / 256) * ((rows + kTopRows - 1) / kTopRows);
+  if (grid > 0x7FFFFFFF) return (int)hipErrorInvalidConfiguration;
+  column_top_kernel<<<(unsigned)grid, kThreads, 0, s>>>(x, ld, rows, cols, h, masked, top);
+  return (int)hipGetLastError();
+}
+
+// a region of the workspace
+struct Regions {
+  size_t at = 0;
+  size_t take(size_t bytes) {
+    const size_t here = at;
+    at += pad256(bytes);
+    return here;
+  }
+};
+
+struct ForwardPlan : HeadPlan {
+  int64_t part_ld;
+  size_t part, sum, x, w, bytes;
+};
+ForwardPlan forward_plan(const skew_head_desc &h) {
+  ForwardPlan f;
+  static_cast<HeadPlan &>(f) = head_plan(h, false);
+  // rows of the last run may be fewer, and their tiles narrower
+  f.part_ld = 0;
+  const int64_t last = h.tokens % f.run ? h.tokens % f.run : f.run;
+  for (const int64_t rows : {f.run, last}) {
+    int64_t ld = 0;
+    for (int64_t v0 = 0; v0 < h.vocab; v0 += f.piece) ld += head_parts(mode_of(h), logits_of(h, f, nullptr, 0, rows, v0, nullptr));
+    f.part_ld = std::max(f.part_ld, ld);
+  }
+  Regions r;
+  f.part = r.take((size_t)f.run * f.part_ld * sizeof(float2));
+  f.sum = r.take((size_t)f.run * 4);
+  f.x = f.x_as_is ? 0 : r.take((size_t)f.run * f.d8 * 2);
+  f.w = f.w_as_is ? 0 : r.take((size_t)up(f.piece, 8) * f.d8 * 2);
+  f.bytes = r.at;
+  return f;
+}
+
+struct BackwardPlan : HeadPlan {
+  size_t tops, row, x16, x, w16, w, g, dx, rest, bytes;
+  int64_t ldg;
+};
+// the three products of a piece
+HeadProduct dx_of(const skew_head_desc &h, const BackwardPlan &b, const void *g, const void *w16, int64_t v0) {
+  const int64_t cols8 = up(piece_cols(h, b, v0), 8);
+  return {g, w16, b.ldg, tied(h) ? b.d8 : cols8, h.tokens, h.d, cols8, 0, b.d8};
+}
+HeadProduct dw_of(const skew_head_desc &h, const BackwardPlan &b, const void *x16, const void *g, int64_t v0) {
+  const int64_t cols = piece_cols(h, b, v0), cols8 = up(cols, 8);
+  if (tied(h)) return {g, x16, b.ldg, b.d8, cols, h.d, h.tokens, cols8, b.d8};
+  return {x16, g, b.d8, b.ldg, h.d, cols, h.tokens, b.d8, cols8};
+}
+int dx_mode(const skew_head_desc &h) { return tied(h) ? kForward : kBackward; }
+
+BackwardPlan backward_plan(const skew_head_desc &h) {
+  BackwardPlan b;
+  static_cast<HeadPlan &>(b) = head_plan(h, true);
+  b.ldg = up(b.piece, 8);
+  const size_t x = (size_t)h.tokens * b.d8 * 2, w = (size_t)b.ldg * b.d8 * 2;
+  Regions r;
+  b.tops = r.take((size_t)(1 + 2 * b.d8) * 4);   // of G's factors, of x's columns, of w's
+  b.row = r.take((size_t)h.tokens * sizeof(HeadRow));
+  b.x16 = r.take(x);
+  b.x = b.x_as_is ? 0 : r.take(x);
+  b.w16 = r.take(w);
+  b.w = b.w_as_is ? 0 : r.take(w);
+  b.g = r.take((size_t)h.tokens * b.ldg * 2);
+  b.dx = pieces(h, b) > 1 ? r.take((size_t)h.tokens * b.d8 * 4) : 0;
+  size_t rest = 0;
+  for (int64_t v0 = 0; v0 < h.vocab; v0 += b.piece) {
+    rest = std::max(rest, head_result_scratch(dx_mode(h), dx_of(h, b, nullptr, nullptr, v0)));
+    rest = std::max(rest, head_result_scratch(kOuter, dw_of(h, b, nullptr, nullptr, v0)));
+  }
+  b.rest = r.take(rest);
+  b.bytes = r.at;
+  return b;
+}
+
+float log2_scale(const skew_head_desc &h) { return (float)((double)h.scale * 1.4426950408889634); }
+
+}  // namespace
+
+size_t head_forward_scratch(const skew_head_desc &h) { return forward_plan(h).bytes; }
+size_t head_backward_scratch(const skew_head_desc &h) { return backward_plan(h).bytes; }
+
+int launch_fill_zero(void *dw, int64_t rows, int64_t cols, int64_t ld, void *stream) {
+  const int64_t grid = (rows * ((cols + 7) / 8) + kThreads - 1) / kThreads;
+  if (grid > 0x7FFFFFFF) return (int)hipErrorInvalidConfiguration;
+  fill_zero_kernel<<<(unsigned)grid, kThreads, 0, static_cast<hipStream_t>(stream)>>>(static_cast<bf16_t *>(dw), rows, cols, ld);
+  return (int)hipGetLastError();
+}
+
+#define TRY(call)                             \
+  do {                                        \
+    const int e_ = (call);                    \
+    if (e_ != (int)hipSuccess) return e_;     \
+  } while (0)
+
+int launch_head_loss(const skew_head_desc &h, float *loss, float *lse, char *ws, void *stream) {
+  const ForwardPlan f = forward_plan(h);
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  const float c = log2_scale(h);
+  float2 *part = reinterpret_cast<float2 *>(ws + f.part);
+  float *sum = reinterpret_cast<float *>(ws + f.sum);
+  bf16_t *x_copy = reinterpret_cast<bf16_t *>(ws + f.x), *w_copy = reinterpret_cast<bf16_t *>(ws + f.w);
+  for (int64_t t0 = 0; t0 < h.tokens; t0 += f.run) {
+    skew_head_desc r = h;   // this run's rows
+    r.tokens = std::min(f.run, h.tokens - t0);
+    r.x = static_cast<const bf16_t *>(h.x) + t0 * h.ldx;
+    r.targets = static_cast<const char *>(h.targets) + t0 * h.target_bytes;
+    if (!f.x_as_is)
+      TRY(launch_pad({static_cast<const bf16_t *>(r.x), h.ldx, r.tokens, h.d, r.tokens, f.d8, nullptr, x_copy, nullptr, 0}, r, s));
+    int64_t at = 0;
+    for (int64_t v0 = 0; v0 < h.vocab; v0 += f.piece) {
+      if (!f.w_as_is) TRY(launch_pad(piece_of(h, f, v0, nullptr, w_copy, nullptr), r, s));
+      const HeadProduct p = logits_of(h, f, f.x_as_is ? r.x : x_copy, f.x_as_is ? h.ldx : f.d8, r.tokens, v0, f.w_as_is ? nullptr : w_copy);
+      TRY(launch_head_forward(mode_of(h), p, {c, r.targets, h.target_bytes, h.vocab, v0, part, f.part_ld, at, sum}, stream));
+      at += head_parts(mode_of(h), p);
+    }
+    loss_kernel<<<(unsigned)((r.tokens + 3) / 4), kThreads, 0, s>>>(r, c, part, f.part_ld, (int)at, sum, loss + t0, lse + t0);
+    TRY((int)hipGetLastError());
+  }
+  return (int)hipSuccess;
+}
+
+int launch_head_loss_backward(const skew_head_desc &h, const float *lse, const float *dloss, const float *dlse, void *dx, int dx_dtype,
+                              int64_t lddx, void *dw, int64_t lddw, char *ws, void *stream) {
+  const BackwardPlan b = backward_plan(h);
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  const float c = log2_scale(h);
+  uint32_t *coef = reinterpret_cast<uint32_t *>(ws + b.tops), *x_top = coef + 1, *w_top = x_top + b.d8;
+  HeadRow *row = reinterpret_cast<HeadRow *>(ws + b.row);
+  uint16_t *x16 = reinterpret_cast<uint16_t *>(ws + b.x16), *w16 = reinterpret_cast<uint16_t *>(ws + b.w16),
+           *g = reinterpret_cast<uint16_t *>(ws + b.g);
+  bf16_t *x_copy = b.x_as_is ? nullptr : reinterpret_cast<bf16_t *>(ws + b.x), *w_copy = b.w_as_is ? nullptr : reinterpret_cast<bf16_t *>(ws + b.w);
+  float *dx_sum = reinterpret_cast<float *>(ws + b.dx);
+  const bf16_t *x = static_cast<const bf16_t *>(h.x);
+  const int tops = (int)(1 + 2 * b.d8);
+  zero_kernel<<<(tops + kThreads - 1) / kThreads, kThreads, 0, s>>>(coef, tops);
+  TRY((int)hipGetLastError());
+  TRY(launch_column_top(x, h.ldx, h.tokens, h.d, h, true, x_top, s));
+  const int64_t groups = (h.tokens + kThreads - 1) / kThreads;
+  factor_top_kernel<<<(unsigned)std::min(groups, (int64_t)64), kThreads, 0, s>>>(h, dloss, dlse, coef);
+  TRY((int)hipGetLastError());
+  rows_kernel<<<(unsigned)groups, kThreads, 0, s>>>(h, c, lse, dloss, dlse, coef, row);
+  TRY((int)hipGetLastError());
+  TRY(launch_pad({x, h.ldx, h.tokens, h.d, h.tokens, b.d8, x16, x_copy, x_top, 1}, h, s));
+  for (int64_t v0 = 0; v0 < h.vocab; v0 += b.piece) {
+    const Padded p = piece_of(h, b, v0, w16, w_copy, w_top);
+    const bool first = v0 == 0, last = v0 + b.piece >= h.vocab;
+    if (tied(h)) {
+      if (!first) {
+        zero_kernel<<<(unsigned)((b.d8 + kThreads - 1) / kThreads), kThreads, 0, s>>>(w_top, (int)b.d8);
+        TRY((int)hipGetLastError());
+      }
+      TRY(launch_column_top(p.x, p.ld, p.rows, p.cols, h, false, w_top, s));
+      TRY(launch_pad(p, h, s));
+    } else {
+      pad_rows_kernel<<<(unsigned)p.rows8, kThreads, 0, s>>>(p, w_top);
+      TRY((int)hipGetLastError());
+    }
+    TRY(launch_head_grad(mode_of(h), logits_of(h, b, b.x_as_is ? h.x : x_copy, b.x_as_is ? h.ldx : b.d8, h.tokens, v0, w_copy),
+                         {c, row, h.vocab, v0, g, b.ldg}, stream));
+    HeadResult to_dx = {last ? dx : dx_sum, last ? lddx : b.d8, last ? dx_dtype : SKEW_F32, first ? nullptr : dx_sum, b.d8, w_top, coef, 0};
+    TRY(launch_head_result(dx_mode(h), dx_of(h, b, g, w16, v0), to_dx, ws + b.rest, stream));
+    bf16_t *to = static_cast<bf16_t *>(dw) + (tied(h) ? v0 * lddw : v0);
+    TRY(launch_head_result(kOuter, dw_of(h, b, x16, g, v0), {to, lddw, SKEW_BF16, nullptr, 0, x_top, coef, !tied(h)}, ws + b.rest, stream));
+  }
+  return (int)hipSuccess;
+}
+
+}  // namespace moe

@@ -1,0 +1,188 @@
+// head_products.hip -- the gradients of the head's rows and weights: products of float16 operands on the matrix cores.
+#include "head_internal.h"
+#include "product_tiles.h"
+
+namespace moe {
+namespace {
+
+struct ResultOp {
+  static constexpr bool kHalf = true;
+  HeadResult r;
+  int64_t rows, cols;
+  template <int MODE, int BM, int BN>
+  __device__ __forceinline__ bool take(const ProductArgs &a, Tile *t) const {
+    uint32_t tr, tc;
+    t->expert = 0;
+    t->first = 0;
+    t->r1 = MODE == kOuter ? a.n : a.places;
+    t->c1 = MODE == kBackward ? a.n : a.m;
+    t->K = (int)(MODE == kOuter ? a.places : MODE == kBackward ? a.m : a.n);
+    if (!patch_tile(a.in_patches, (uint32_t)a.row_tiles, ((uint32_t)t->c1 + BN - 1) / BN, &tr, &tc)) return false;
+    t->r0 = (int64_t)tr * BM;
+    t->c0 = (int64_t)tc * BN;
+    return true;
+  }
+  template <int MODE, int FM, int FN>
+  __device__ __forceinline__ void finish(const ProductArgs &a, const Tile &t, int wr, int wc, const f32x4 (&acc)[FM][FN],
+                                         char *room) const {
+    const int lane = threadIdx.x & 63;
+    const int64_t row_w = t.r0 + wr, col_w = t.c0 + wc, row0 = row_w + (lane & 15), col0 = col_w + (lane >> 4) * 4;
+    if (a.part) {   // the sums themselves, for join_kernel
+      float *y = static_cast<float *>(a.y) + (int64_t)blockIdx.y * rows * a.ldy + row0 * a.ldy + col0;
+#pragma unroll
+      for (int i = 0; i < FM; i++) {
+        if (row0 + i * 16 >= rows) break;
+#pragma unroll
+        for (int j = 0; j < FN; j++)
+          if (col0 + j * 16 < cols) *reinterpret_cast<f32x4 *>(y + i * 16 * a.ldy + j * 16) = acc[i][j];   // (ldy: whole fours)
+      }
+      return;
+    }
+    const int coef = half_exponent(*r.coef);
+    auto power = [&](int64_t at, int64_t end) { return at < end ? half_exponent(r.top[at]) + coef : 0; };
+    int ec[FN][4];
+    if (!r.by_row) {
+#pragma unroll
+      for (int j = 0; j < FN; j++)
+#pragma unroll
+        for (int q = 0; q < 4; q++) ec[j][q] = power(col0 + j * 16 + q, cols);
+    }
+    const bool f32 = r.y_dtype == SKEW_F32;
+#pragma unroll
+    for (int i = 0; i < FM; i++) {
+      const int64_t row = row0 + i * 16;
+      const int er = r.by_row ? power(row, rows) : 0;
+#pragma unroll
+      for (int j = 0; j < FN; j++) {
+        const int64_t n = row < rows ? cols - col0 - j * 16 : 0;
+        f32x4 v;
+#pragma unroll
+        for (int q = 0; q < 4; q++) v[q] = __builtin_ldexpf(acc[i][j][q], r.by_row ? er : ec[j][q]);
+        if (r.prev && n > 0) {   // (rows of whole fours)
+          v += *reinterpret_cast<const f32x4 *>(r.prev + row * r.ldprev + col0 + j * 16);
+        }
+        if (!f32) {
+          put_room<FN>(room, i, j, make_uint2(pack2(v[0], v[1]), pack2(v[2], v[3])));
+        } else {
+          float *y = static_cast<float *>(r.y) + row * r.ldy + col0 + j * 16;
+          if (n >= 4) {
+            *reinterpret_cast<f32x4_a4 *>(y) = v;
+          } else {
+#pragma unroll
+            for (int q = 0; q < 3; q++)
+              if (q < n) y[q] = v[q];
+          }
+        }
+      }
+    }
+    if (!f32) store_room<FM, FN, false>(room, static_cast<uint16_t *>(r.y) + row_w * r.ldy + col_w, r.ldy, rows - row_w, cols - col_w);
+  }
+};
+
+template <int MODE, int FM, int FN, int NS, int KS>
+__global__ __launch_bounds__(256, per_unit(FM, FN, KS)) void result_kernel(ProductArgs a, ResultOp op) {
+  tile_body<MODE, FM, FN, NS, KS>(a, op);
+}
+
+// Sums the parts of a shared contraction, in order, and finishes them as ResultOp does.
+__global__ __launch_bounds__(256) void join_kernel(HeadResult r, int64_t rows, int64_t cols, const float *part, int parts, int64_t ld) {
+  const Chunks c(rows, (cols + 7) / 8, 256);
+  const Place p = c.at(0);
+  if (!p.there) return;
+  float v[8] = {};
+  for (int i = 0; i < parts; i++) {
+    const float *y = part + ((int64_t)i * rows + p.row) * ld + p.col;
+#pragma unroll
+    for (int q = 0; q < 8; q++) v[q] += y[q];
+  }
+  const int64_t n = cols - p.col;
+  const int coef = half_exponent(*r.coef);
+#pragma unroll
+  for (int q = 0; q < 8; q++) {
+    if (q < n) v[q] = __builtin_ldexpf(v[q], coef + half_exponent(r.top[r.by_row ? p.row : p.col + q]));
+    if (r.prev && q < n) v[q] += r.prev[p.row * r.ldprev + p.col + q];
+  }
+  if (r.y_dtype == SKEW_F32) store8(static_cast<float *>(r.y) + p.row * r.ldy + p.col, n, v);
+  else store8(static_cast<bf16_t *>(r.y) + p.row * r.ldy + p.col, n, v);
+}
+
+// Which tile, and how many work-groups share a contraction.
+struct Choice {
+  int tile, parts;
+};
+int tile_rows(int s) { return s == 0 ? 256 : s == 1 ? 128 : 64; }
+int tile_cols(int s) { return s == 2 ? 128 : 256; }
+Choice choose_result(int mode, const HeadProduct &p) {
+  const double round[3] = {1.0, mode == kBackward ? 0.58 : 1.15, 0.68};
+  const int slots[3] = {256, mode == kBackward ? 256 : 512, 768};
+  Choice best = {0, 1};
+  double least = 1e300;
+  for (int s = 0; s < 3; s++) {
+    const int64_t n = ((p.rows + tile_rows(s) - 1) / tile_rows(s)) * ((p.cols + tile_cols(s) - 1) / tile_cols(s));
+    int64_t parts = slots[s] / n;
+    if (parts > p.K / 512) parts = p.K / 512;
+    if (parts < 1) parts = 1;
+    if (parts > 64) parts = 64;
+    const double t = (double)((n * parts + slots[s] - 1) / slots[s]) * round[s] * ((double)p.K / parts + 256);
+    if (t < least) {
+      least = t;
+      best = {s, (int)parts};
+    }
+  }
+  return best;
+}
+int64_t part_ld(int64_t cols) { return (cols + 7) / 8 * 8; }
+
+template <int MODE, int FM, int FN, int NS, int KS>
+int launch_one(const HeadProduct &p, const HeadResult &r, Choice c, char *ws, void *stream) {
+  ProductArgs a = {};
+  a.x = static_cast<const bf16_t *>(p.a);   // (float16 bits)
+  a.w = static_cast<const bf16_t *>(p.b);
+  a.ldx = p.lda;
+  a.ldw = p.ldb;
+  a.k = 1;
+  a.experts = 1;
+  a.places = MODE == kOuter ? p.K : p.rows;
+  a.n = MODE == kOuter ? p.pad_rows : MODE == kBackward ? p.pad_cols : p.K;
+  a.m = MODE == kBackward ? p.K : p.pad_cols;
+  a.row_tiles = (p.rows + 32 * FM - 1) / (32 * FM);
+  const int64_t cols = (p.pad_cols + 32 * FN - 1) / (32 * FN);
+  a.in_patches = patches(a.row_tiles, cols) >= kMinPatches;
+  int parts = 1;
+  if (c.parts > 1) {
+    a.part = (int32_t)(((p.K + c.parts - 1) / c.parts + 63) / 64 * 64);
+    parts = (int)((p.K + a.part - 1) / a.part);
+    a.y = ws;
+    a.ldy = part_ld(p.cols);
+  }
+  const int64_t grid = patch_grid(a.row_tiles, cols, a.in_patches);
+  if (grid > 0x7FFFFFFF) return (int)hipErrorInvalidConfiguration;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  result_kernel<MODE, FM, FN, NS, KS><<<dim3((unsigned)grid, parts), 256, 0, s>>>(a, ResultOp{r, p.rows, p.cols});
+  const int e = (int)hipGetLastError();
+  if (e != (int)hipSuccess || c.parts == 1) return e;
+  join_kernel<<<(unsigned)((p.rows * (part_ld(p.cols) / 8) + 255) / 256), 256, 0, s>>>(r, p.rows, p.cols, reinterpret_cast<float *>(ws), parts,
+                                                                                     a.ldy);
+  return (int)hipGetLastError();
+}
+template <int MODE>
+int launch_mode(const HeadProduct &p, const HeadResult &r, char *ws, void *stream) {
+  constexpr int S = MODE == kBackward ? 2 : 1;
+  const Choice c = choose_result(MODE, p);
+  if (c.tile == 0) return launch_one<MODE, 8, 8, 4 / S, S>(p, r, c, ws, stream);
+  if (c.tile == 1) return launch_one<MODE, 4, 8, 3, S>(p, r, c, ws, stream);
+  return launch_one<MODE, 2, 4, 4 / S, S>(p, r, c, ws, stream);
+}
+
+}  // namespace
+
+size_t head_result_scratch(int mode, const HeadProduct &p) {
+  const Choice c = choose_result(mode, p);
+  return c.parts > 1 ? pad256((size_t)c.parts * (size_t)p.rows * (size_t)part_ld(p.cols) * 4) : 0;
+}
+int launch_head_result(int mode, const HeadProduct &p, const HeadResult &r, char *ws, void *stream) {
+  if (mode == kOuter) return launch_mode<kOuter>(p, r, ws, stream);
+  return mode == kBackward ? launch_mode<kBackward>(p, r, ws, stream) : launch_mode<kForward>(p, r, ws, stream);
+}
+
+}  // namespace moe

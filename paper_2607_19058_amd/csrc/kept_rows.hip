@@ -15,27 +15,6 @@ namespace {
 constexpr int kThreads = 256, kUnroll = 2;   // chunks of a thread
 constexpr int kTile = kThreads * kUnroll;    // chunks of a work-group
 
-// Where a work-group's chunk q is: rows are cut into `per` chunks (a multiple of 4).
-struct Place {
-  int64_t row;
-  int64_t col;
-  bool there;
-};
-struct Chunks {
-  int64_t row0, rows;
-  uint32_t first, per;
-  __device__ __forceinline__ Chunks(int64_t rows_, int64_t cols) : rows(rows_) {
-    per = (uint32_t)((cols + 31) / 32) * 4;
-    const int64_t at = (int64_t)blockIdx.x * kTile;
-    row0 = at / per;
-    first = (uint32_t)(at - row0 * per);
-  }
-  __device__ __forceinline__ Place at(int i) const {
-    const uint32_t t = first + threadIdx.x + i * kThreads, r = t / per;
-    return {row0 + r, (int64_t)(t - r * per) * 8, row0 + r < rows};
-  }
-};
-
 template <int kPerm>   // the value of another of four neighbouring lanes
 __device__ __forceinline__ uint32_t quad(uint32_t x) {
   return (uint32_t)__builtin_amdgcn_mov_dpp((int)x, kPerm, 0xF, 0xF, true);
@@ -78,6 +57,9 @@ __device__ __forceinline__ void restore(uint2 codes, uint32_t b, float *v) {
   }
 }
 
+// Chunks of a row in whole blocks.
+__host__ __device__ inline int64_t chunks_of(int64_t cols) { return (cols + 31) / 32 * 4; }
+
 // The place of a chunk's codes and of its block's byte.
 __device__ __forceinline__ void put_kept(const Chunks &c, const Place &p, uint2 codes, uint32_t b, int8_t *at, uint8_t *scales) {
   const int64_t chunk = p.row * c.per + p.col / 8;
@@ -96,7 +78,7 @@ __device__ __forceinline__ KeptChunk get_kept(const Chunks &c, const Place &p, c
 template <class T>
 __global__ __launch_bounds__(kThreads) void keep_kernel(const T *x, int64_t rows, int64_t cols, int64_t ldx, int8_t *codes,
                                                         uint8_t *scales) {
-  const Chunks c(rows, cols);
+  const Chunks c(rows, chunks_of(cols), kTile);
   float v[kUnroll][8];
   Place p[kUnroll];
 #pragma unroll
@@ -115,7 +97,7 @@ __global__ __launch_bounds__(kThreads) void keep_kernel(const T *x, int64_t rows
 template <class T>
 __global__ __launch_bounds__(kThreads) void restore_kernel(const int8_t *codes, const uint8_t *scales, int64_t rows, int64_t cols,
                                                            T *x, int64_t ldx) {
-  const Chunks c(rows, cols);
+  const Chunks c(rows, chunks_of(cols), kTile);
   Place p[kUnroll];
   KeptChunk k[kUnroll];
 #pragma unroll
@@ -152,7 +134,7 @@ __device__ __forceinline__ void act(float g, float *f, float *df) {
 
 template <class T, class O, int KIND>
 __global__ __launch_bounds__(kThreads) void act_kernel(skew_act_desc d) {
-  const Chunks c(d.rows, d.cols);
+  const Chunks c(d.rows, chunks_of(d.cols), kTile);
   float g[kUnroll][8], u[kUnroll][8];
   Place p[kUnroll];
 #pragma unroll
@@ -187,7 +169,7 @@ __global__ __launch_bounds__(kThreads) void act_kernel(skew_act_desc d) {
 
 template <class T, class O, int KIND>
 __global__ __launch_bounds__(kThreads) void act_backward_kernel(skew_act_desc d) {
-  const Chunks c(d.rows, d.cols);
+  const Chunks c(d.rows, chunks_of(d.cols), kTile);
   float da[kUnroll][8];
   Place p[kUnroll];
   KeptChunk kg[kUnroll], ku[kUnroll];
@@ -222,7 +204,7 @@ __global__ __launch_bounds__(kThreads) void act_backward_kernel(skew_act_desc d)
 }
 
 int64_t groups(int64_t rows, int64_t cols) {
-  return (rows * ((cols + 31) / 32 * 4) + kTile - 1) / kTile;
+  return (rows * chunks_of(cols) + kTile - 1) / kTile;
 }
 
 // calls f with null pointers of the element types of in and out

@@ -172,5 +172,26 @@ __device__ __forceinline__ void store_vec(float *p, int64_t n, const float *v) {
   }
 }
 
+// Rows cut into `per` chunks of 8 values (per < 2^31 - 2^16), chunks of all rows in order, `tile` of them a work-group, given to
+// its threads in turn.
+struct Place {
+  int64_t row, col;
+  bool there;
+};
+struct Chunks {
+  int64_t row0, rows;
+  uint32_t first, per;
+  __device__ __forceinline__ Chunks(int64_t rows_, int64_t per_, int tile) : rows(rows_), per((uint32_t)per_) {
+    const int64_t at = (int64_t)blockIdx.x * tile;
+    row0 = at / per;
+    first = (uint32_t)(at - row0 * per);
+  }
+  // chunk i of this thread
+  __device__ __forceinline__ Place at(int i) const {
+    const uint32_t t = first + threadIdx.x + i * blockDim.x, r = t / per;
+    return {row0 + r, (int64_t)(t - r * per) * 8, row0 + r < rows};
+  }
+};
+
 }  // namespace moe
 #endif

@@ -4,13 +4,7 @@
 //   backward  y[p] = s_p a_p W[e]^T      contraction over m: contiguous in both
 //   weights   dW[e] = sum_p a_p^T d_p    contraction over an expert's places: contiguous in neither
 //
-// A work-group computes one tile of one expert's result. Operand tiles go through LDS in the order they
-// have in memory; a lane of the matrix instruction needs 8 neighbours along the contraction, which are
-// one 16-byte LDS read where memory is contiguous in it, and two transposing LDS reads (4 rows by 16 columns
-// to 4 neighbours per lane) where it is not. 16-byte chunks are placed in LDS with their index xor-ed with bits of
-// their row, so that the lanes of one LDS access fall into different banks.
-// The matrix instruction is called with W's side first: a lane then holds 4 neighbouring columns of
-// one result row, which it stores together.
+// A work-group computes one tile of one expert's result (product_tiles.h).
 //
 // What bounds them: with some 300 rows an expert or fewer, the bytes of W (or of dW); with more, the matrix cores.
 // Kernel times: 1024 tokens, top 2 of 128 experts of 2048 x 8192, forward: 673 us, W at 6.0 TB/s (a copy: 4.9, reads alone: 7.1). 8
@@ -18,106 +12,10 @@
 // 1.25). 32 experts of 8192 x 2048 with 128 uneven rows each: backward 328 to 350 us; weights 386 to 410 us from bf16 rows (2.7 TB/s of
 // dW), 497 to 528 us and 17 us for the split from float32 rows. 512 uneven rows of 2048 x 8192 each: forward 725, backward 696, weights
 // 700 us (0.79 PFLOP/s), from float32 rows 1253.
-#include <type_traits>
-
-#include "moe_internal.h"
+#include "product_tiles.h"
 
 namespace moe {
 namespace {
-
-enum { kForward = 0, kBackward = 1, kWeights = 2 };
-
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef short s16x4 __attribute__((ext_vector_type(4)));
-
-struct ProductArgs {
-  const bf16_t *x;
-  const bf16_t *w;     // the weights; kWeights: d
-  void *y;             // kWeights: dW
-  const float *scale;
-  const int32_t *offsets, *rows;
-  int64_t ldx, ldw, slice, ldy;   // kWeights: ldw is d's row stride, ldy and slice are dW's
-  int64_t n, m, places;           // n x m weights
-  int32_t k, experts, gather, f32;
-  int32_t direct;                 // 16-byte rows in both operands (and in a bf16 result), lengths that are multiples of 8
-  int32_t wide;                   // 4 neighbouring results can be stored together
-  int64_t row_tiles;              // forward, backward: tiles of rows in the grid
-  int32_t in_patches;             // how tiles are given out (patch_tile)
-  int32_t part;                   // forward, backward: contraction length of a work-group (a multiple of its stages)
-};
-
-constexpr int kBK = 32;   // contraction length of a step: one matrix instruction's
-
-// ---- LDS tiles ------------------------------------------------------------------------------
-// Contiguous in the contraction: rows of KS steps of kBK values, 4 KS chunks of 8. A 16-byte read takes two
-// cycles of 16 lanes each: rows 0-3 and 12-15 at one chunk with rows 4-11 at the next one, and the other way about.
-// KS = 1: 4 rows are as long as the banks; with the rows' groups of 4 xor-ed by 0, 2, 3, 1 the lanes fall into different banks
-// (with 0, 1, 2, 3 a third of the reads' cycles were conflicts). KS = 2: 2 rows are, and the row does it.
-template <int KS>
-__device__ __forceinline__ int swizzle_k(int row) {
-  return KS == 1 ? (((row >> 2) ^ (row >> 3)) & 1) << 1 | ((row >> 3) & 1) : row & 7;
-}
-// Contiguous along the result: kBK rows of W values (W / 8 chunks). A transposing read takes two
-// neighbouring chunks of 4 rows in each of 4 lane groups, which are 8 rows apart.
-template <int W>
-__device__ __forceinline__ int swizzle_t(int row) {
-  return (W >= 128 ? (row & 3) | ((row >> 1) & 4) : ((row >> 1) & 1) | ((row >> 2) & 2)) << 1;
-}
-
-__device__ __forceinline__ uint32_t lds_offset(const void *p) {
-  typedef __attribute__((address_space(3))) const void lds;
-  return (uint32_t)(uintptr_t)(lds *)p;
-}
-template <class V>
-__device__ __forceinline__ const __attribute__((address_space(3))) V *lds_at(uint32_t byte) {
-  return (const __attribute__((address_space(3))) V *)(uintptr_t)byte;
-}
-
-// A wave's fragments: 8 neighbours along the contraction (8 (lane / 16) .. + 7) of each of 16 result rows (lane % 16).
-// get(buf, i): rows r0 + 16 i .. of the buffer `buf` bytes on. Contiguous in the contraction: fragments are a
-// constant apart, as the xor takes bits of the row below 16.
-template <int KS>
-struct FragK {
-  uint32_t at[KS];
-  __device__ __forceinline__ FragK(const u32x4 *tile, int r0) {
-    const int lane = threadIdx.x & 63, row = lane & 15;
-#pragma unroll
-    for (int k = 0; k < KS; k++)
-      at[k] = lds_offset(tile) + (r0 + row) * (64 * KS) + ((k * 4 + (lane >> 4)) ^ swizzle_k<KS>(row)) * 16;
-  }
-  __device__ __forceinline__ bf16x8 get(int step, int i) const {
-    return __builtin_bit_cast(bf16x8, *lds_at<u32x4>(at[step] + i * 1024 * KS));
-  }
-  __device__ __forceinline__ void move(int32_t bytes) {
-#pragma unroll
-    for (int k = 0; k < KS; k++) at[k] += bytes;
-  }
-};
-// Contiguous along the result: fragments are 16 columns apart, which the xor mixes with the row.
-template <int B, int F>
-struct FragT {
-  uint32_t at[F];
-  __device__ __forceinline__ FragT(const u32x4 *tile, int c0) {
-    const int lane = threadIdx.x & 63, i = lane & 15;
-    const int row = (lane >> 4) * 8 + (i >> 2), chunk = c0 / 8 + ((i & 3) >> 1);
-#pragma unroll
-    for (int f = 0; f < F; f++)
-      at[f] = lds_offset(tile) + row * (B * 2) + ((chunk + 2 * f) ^ swizzle_t<B>(row)) * 16 + (i & 1) * 8;
-  }
-  __device__ __forceinline__ bf16x8 get(int step, int f) const {
-    typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-    struct {
-      s16x4 lo, hi;   // rows row .. + 3 and, with the same xor, row + 4 .. + 7
-    } v;
-    v.lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(uintptr_t)(at[f] + step * kBK * B * 2));
-    v.hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(uintptr_t)(at[f] + (step * kBK + 4) * B * 2));
-    return __builtin_bit_cast(bf16x8, v);
-  }
-  __device__ __forceinline__ void move(int32_t bytes) {
-#pragma unroll
-    for (int f = 0; f < F; f++) at[f] += bytes;
-  }
-};
 
 // 8 values at p, of which the first n exist (n <= 0: none)
 __device__ __forceinline__ u32x4 load_chunk(const bf16_t *p, int64_t n) {
@@ -190,83 +88,6 @@ __device__ __forceinline__ bool find_tile(const ProductArgs &a, int64_t tile, in
   return false;
 }
 
-// 16 bytes a lane from global memory (a scalar base and the lane's byte offset) to LDS: lane i of the wave to byte
-// `to` + 16 i of LDS (`to` the same in every lane).
-// Written out because the compiler, which cannot tell the stage buffers apart, would wait for these loads
-// before every LDS read. It does not count them either: every use of the data comes after vm_wait() and a barrier.
-// m0 is a reserved register, about which naming it warns; the compiler sets it anew for each use of its own after it.
-#pragma clang diagnostic push
-#pragma clang diagnostic ignored "-Winline-asm"
-__device__ __forceinline__ void load_lds(const char *base, uint32_t offset, uint32_t to) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(__builtin_amdgcn_readfirstlane(to)),
-               "v"(offset), "s"(base)
-               : "memory", "m0");
-}
-#pragma clang diagnostic pop
-// waits until at most N of this wave's loads are on their way
-template <int N>
-__device__ __forceinline__ void vm_wait() {
-  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
-}
-__device__ __forceinline__ uint32_t lds_address(const void *p) { return __builtin_amdgcn_readfirstlane(lds_offset(p)); }
-
-// a value that is the same in every lane, as a scalar
-__device__ __forceinline__ int64_t scalar(int64_t x) {
-  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)x), hi = __builtin_amdgcn_readfirstlane((uint32_t)(x >> 32));
-  return (int64_t)((uint64_t)hi << 32 | lo);
-}
-__device__ __forceinline__ const char *scalar(const char *p) {
-  return reinterpret_cast<const char *>(scalar((int64_t)(uintptr_t)p));
-}
-
-// Which tile a work-group takes. Work-groups go to the 8 dies in turn (id % 8), and each die has its own L2, so
-// patches of kPatchR x kPatchC tiles (one for each of a die's 32 compute units) go to the dies in turn: a
-// patch's tiles share their operands' rows and columns in one L2. patch_tile: false where the patch passes the edge.
-// Fewer patches than kMinPatches would leave dies idle: then single tiles go to the dies in turn.
-constexpr int kDies = 8, kPatchR = 4, kPatchC = 8, kMinPatches = 4 * kDies;
-inline int64_t patches(int64_t rows, int64_t cols) {
-  return ((rows + kPatchR - 1) / kPatchR) * ((cols + kPatchC - 1) / kPatchC);
-}
-inline int64_t patch_grid(int64_t rows, int64_t cols, bool in_patches) {
-  return in_patches ? (patches(rows, cols) + kDies - 1) / kDies * kDies * (kPatchR * kPatchC) : rows * cols;
-}
-__device__ __forceinline__ bool patch_tile(bool in_patches, uint32_t rows, uint32_t cols, uint32_t *row, uint32_t *col) {
-  if (!in_patches) {
-    *row = blockIdx.x / cols;
-    *col = blockIdx.x - *row * cols;
-    return true;
-  }
-  const uint32_t i = blockIdx.x / kDies, in = i % (kPatchR * kPatchC);
-  const uint32_t patch = i / (kPatchR * kPatchC) * kDies + blockIdx.x % kDies, pc = (cols + kPatchC - 1) / kPatchC;
-  const uint32_t pr = patch / pc;
-  *row = pr * kPatchR + in % kPatchR;
-  *col = (patch - pr * pc) * kPatchC + in / kPatchR;
-  return *row < rows && *col < cols;
-}
-
-// acc += the product of two fragments (result rows along the second). IN_A: the sums stay in the accumulation
-// registers, which the compiler, left to itself, copies to others and back when they are 256 of a lane's 512.
-// It does not know the written-out instruction's latency: the sums go through mfma_done() before they are read.
-template <bool IN_A>
-__device__ __forceinline__ void mfma(f32x4 &acc, bf16x8 b, bf16x8 a) {
-  if (IN_A) asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(acc) : "v"(b), "v"(a));
-  else acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b, a, acc, 0, 0, 0);
-}
-template <int FM, int FN>
-__device__ __forceinline__ void mfma_done(f32x4 (&acc)[FM][FN]) {
-  asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
-#pragma unroll
-  for (int i = 0; i < FM; i++)
-#pragma unroll
-    for (int j = 0; j < FN; j++) asm volatile("" : "+a"(acc[i][j]));   // what reads them depends on this, which stays behind the wait
-}
-
-// What a tiled work-group computes: rows [r0, r1) and columns [c0, c1) of the result of one expert, contraction length K;
-// kWeights: places first .. first + K - 1.
-struct Tile {
-  int expert, K;
-  int64_t r0, r1, c0, c1, first;
-};
 template <int MODE, int BM, int BN>
 __device__ __forceinline__ bool take_tile(const ProductArgs &a, Tile *t) {
   uint32_t tr, tc;   // (the grid has fewer than 2^31 tiles)
@@ -295,8 +116,7 @@ __device__ __forceinline__ bool take_tile(const ProductArgs &a, Tile *t) {
 
 // Stores a wave's FM x FN blocks of 16 x 16 results from row wr and column wc of the tile. A lane holds row
 // lane % 16 of each block and its columns 4 (lane / 16) .. + 3.
-// bf16 results go through `room` (FM FN 512 bytes of LDS of this wave's own), so that a row's 32 FN bytes leave
-// together: 8-byte stores of 16 rows at once reached 3.1 TB/s on a gradient that is all output.
+// bf16 results go through `room`.
 template <int MODE, int FM, int FN, bool CHUNKS>
 __device__ __forceinline__ void store_tile(const ProductArgs &a, const Tile &t, int wr, int wc, const f32x4 (&acc)[FM][FN],
                                            char *room) {
@@ -311,48 +131,16 @@ __device__ __forceinline__ void store_tile(const ProductArgs &a, const Tile &t, 
       if (row0 + i * 16 < t.r1) s[i] = a.scale[a.rows[row0 + i * 16]];
   }
   if (MODE == kWeights || !a.f32) {
-    constexpr int kChunks = 2 * FN;   // of a row, placed with their index xor-ed with the row
 #pragma unroll
     for (int i = 0; i < FM; i++)
 #pragma unroll
       for (int j = 0; j < FN; j++) {
-        const int row = i * 16 + (lane & 15), c = 2 * j + (lane >> 5);
         const f32x4 v = s[i] * acc[i][j];
-        *reinterpret_cast<uint2 *>(room + row * (kChunks * 16) + (c ^ (row & 7)) * 16 + (lane >> 4 & 1) * 8) =
-            make_uint2(pack2(v[0], v[1]), pack2(v[2], v[3]));
+        put_room<FN>(room, i, j, make_uint2(pack2(v[0], v[1]), pack2(v[2], v[3])));
       }
-    __builtin_amdgcn_wave_barrier();
-    constexpr int kRows = 64 / kChunks;   // rows of one store
-    const int c = lane % kChunks, row_in = lane / kChunks;
-    const int64_t col = t.c0 + wc + c * 8, left = t.r1 - (t.r0 + wr);
-    const int rows = left < 16 * FM ? (int)left : 16 * FM, n = (int)(t.c1 - col < 8 ? t.c1 - col : 8);   // of the wave's; of the lane's 8 columns
-    bf16_t *y = static_cast<bf16_t *>(a.y) + (MODE == kWeights ? (int64_t)t.expert * a.slice : 0) +
-                (t.r0 + wr + row_in) * a.ldy + col;
-    const int64_t step = kRows * a.ldy;
-    auto read = [&](int i) {
-      const int row = i * kRows + row_in;
-      return *reinterpret_cast<const u32x4 *>(room + row * (kChunks * 16) + (c ^ (row & 7)) * 16);
-    };
-    if (CHUNKS) {   // not a case of the loop below: its reads wait for each other, and its code is in the registers' way
-#pragma unroll
-      for (int i = 0; i < 16 * FM / kRows; i++, y += step) {
-        const u32x4 v = read(i);
-        if (i * kRows + row_in < rows && n > 0) *reinterpret_cast<u32x4 *>(y) = v;
-      }
-      return;
-    }
-#pragma unroll
-    for (int i = 0; i < 16 * FM / kRows; i++, y += step) {
-      const u32x4 v = read(i);
-      if (i * kRows + row_in >= rows || n <= 0) continue;
-      if (n == 8) {
-        *reinterpret_cast<u32x4_a2 *>(y) = v;
-      } else {
-#pragma unroll
-        for (int e = 0; e < 7; e++)
-          if (e < n) y[e].v = (uint16_t)(v[e >> 1] >> (16 * (e & 1)));
-      }
-    }
+    const int64_t row = t.r0 + wr, col = t.c0 + wc;
+    store_room<FM, FN, CHUNKS>(room, static_cast<uint16_t *>(a.y) + (MODE == kWeights ? (int64_t)t.expert * a.slice : 0) +
+                               row * a.ldy + col, a.ldy, t.r1 - row, t.c1 - col);
     return;
   }
   float *y = static_cast<float *>(a.y) + row0 * a.ldy + col0;   // (dW is bf16)
@@ -375,262 +163,23 @@ __device__ __forceinline__ void store_tile(const ProductArgs &a, const Tile &t, 
   }
 }
 
-// ---- tiles whose chunks go from memory to LDS without registers ---------------------------------
-// For rows at 16-byte positions and lengths that are multiples of 8, so that a chunk is inside its row or outside.
-// Tiles of 32 FM x 32 FN results, 4 waves, each FM x FN matrix instructions a stage; NS LDS buffers of a stage.
-// A stage is KS steps. While a wave multiplies one step from registers it reads the next one from LDS into other registers
-// and sends for a stage further on, one load or fragment after every few matrix instructions. A load's address is a
-// scalar, which moves from stage to stage, plus a lane's 32-bit offset, which stays.
-// Rows and columns past the edge of the result repeat the last one inside and are not stored; past the end of the
-// contraction both operands are zero, so nothing there meets a NaN.
-constexpr int kList = 1024;   // places whose rows kWeights looks up at once
+// The experts' products on those tiles.
+struct ExpertOp {
+  static constexpr bool kHalf = false;
+  template <int MODE, int BM, int BN>
+  __device__ __forceinline__ bool take(const ProductArgs &a, Tile *t) const {
+    return take_tile<MODE, BM, BN>(a, t);
+  }
+  template <int MODE, int FM, int FN>
+  __device__ __forceinline__ void finish(ProductArgs a, const Tile &t, int wr, int wc, const f32x4 (&acc)[FM][FN], char *room) const {
+    if (MODE != kWeights && a.part) a.y = static_cast<float *>(a.y) + (int64_t)blockIdx.y * a.places * a.ldy;
+    store_tile<MODE, FM, FN, true>(a, t, wr, wc, acc, room);
+  }
+};
 
 template <int MODE, int FM, int FN, int NS, int KS>
-__global__ __launch_bounds__(256, FM * FN * KS >= 64 ? 1 : FM * FN == 8 ? 3 : 2) void tile_kernel(ProductArgs a) {
-  constexpr int BM = 32 * FM, BN = 32 * FN, BK = KS * kBK, kThreads = 256;
-  constexpr int kCA = BM * BK / 8, kCB = BN * BK / 8, kPA = kCA / kThreads, kPB = kCB / kThreads;   // chunks of a stage
-  constexpr int kBytesA = kCA * 16, kBytesB = kCB * 16, kLoads = kPA + kPB;
-  constexpr bool kInA = FM * FN == 64;
-  constexpr int kAhead = KS == 1 ? NS - 1 : NS;   // a stage of two steps is sent for when its buffer's second step was read
-  static_assert(FM * FN * 512 * 4 <= NS * (kBytesA + kBytesB), "room for the results");
-  static_assert(kPA * kThreads == kCA && kPB * kThreads == kCB, "whole chunks per thread");
-  __shared__ u32x4 lds[NS * (kCA + kCB) + (MODE == kWeights ? kList / 4 : 0)];
-  u32x4 *const ta = lds, *const tb = lds + NS * kCA;
-  uint32_t *const list = reinterpret_cast<uint32_t *>(tb + NS * kCB);   // byte offsets of x's rows
-  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int wr = (wave >> 1) * (BM / 2), wc = (wave & 1) * (BN / 2);
-  Tile t;
-  if (!take_tile<MODE, BM, BN>(a, &t)) return;
-  int K = t.K;
-
-  f32x4 acc[FM][FN];
-#pragma unroll
-  for (int i = 0; i < FM; i++)
-#pragma unroll
-    for (int j = 0; j < FN; j++) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-
-  // Slot i of this thread is chunk q = tid + i kThreads of a stage's tile in LDS. A tile that is contiguous in the
-  // contraction holds result row q / (4 KS) and chunk (q % (4 KS)) ^ swizzle there; one that is not holds contraction row
-  // q / (tile width / 8) likewise. ka, kb: the slot's contraction index in its stage; oa, ob: its byte offset from xa, xb, where
-  // the next stage that is sent for begins (kWeights: oa without the row of x).
-  const char *xa = reinterpret_cast<const char *>(a.x), *xb = reinterpret_cast<const char *>(a.w);
-  int64_t step_a = 0, step_b;
-  if (MODE == kWeights) {
-    xb += 2 * t.first * a.ldw;
-  } else {
-    xb += 2 * (int64_t)(K ? t.expert : 0) * a.slice;
-    if (!a.gather) xa += 2 * t.r0 * a.ldx;
-    step_a = 2 * BK;
-  }
-  step_b = MODE == kBackward ? 2 * BK : 2 * BK * a.ldw;
-  if (MODE != kWeights && a.part) {   // this work-group's part of a contraction that several share
-    const int k0 = (int)blockIdx.y * a.part;
-    K = K - k0 < a.part ? (K > k0 ? K - k0 : 0) : a.part;
-    if (K > 0) {
-      xa += k0 / BK * step_a;
-      xb += k0 / BK * step_b;
-    }
-  }
-  if (MODE == kBackward) xb += 2 * t.c0 * a.ldw;
-  xa = scalar(xa);
-  xb = scalar(xb);
-  step_b = scalar(step_b);
-  uint32_t oa[kPA], ob[kPB];
-  int ka[kPA], kb[kPB];
-#pragma unroll
-  for (int i = 0; i < kPA; i++) {
-    const int q = tid + i * kThreads;
-    if (MODE == kWeights) {
-      const int row = q / (BM / 8), c = (q % (BM / 8)) ^ swizzle_t<BM>(row);
-      ka[i] = row;
-      oa[i] = (uint32_t)(2 * (t.r0 + c * 8 < t.r1 ? t.r0 + c * 8 : t.r1 - 8));
-    } else {
-      const int row = q / (4 * KS), c = (q % (4 * KS)) ^ swizzle_k<KS>(row);
-      const int r = t.r0 + row < t.r1 ? row : (int)(t.r1 - 1 - t.r0);
-      ka[i] = c * 8;
-      oa[i] = (uint32_t)((K > 0 && a.gather ? (int64_t)(a.rows[t.r0 + r] / a.k) : r) * a.ldx + c * 8) * 2;
-    }
-  }
-#pragma unroll
-  for (int i = 0; i < kPB; i++) {
-    const int q = tid + i * kThreads;
-    if (MODE == kBackward) {
-      const int row = q / (4 * KS), c = (q % (4 * KS)) ^ swizzle_k<KS>(row);
-      kb[i] = c * 8;
-      ob[i] = (uint32_t)((t.c0 + row < t.c1 ? row : t.c1 - 1 - t.c0) * a.ldw + c * 8) * 2;
-    } else {
-      const int row = q / (BN / 8), c = (q % (BN / 8)) ^ swizzle_t<BN>(row);
-      kb[i] = row;
-      ob[i] = (uint32_t)(row * a.ldw + (t.c0 + c * 8 < t.c1 ? t.c0 + c * 8 : t.c1 - 8)) * 2;
-    }
-  }
-  // W's rows in the contraction are a power of two apart in most models, so that tiles at the same place of their rows ask the
-  // same memory channels: the tiles of a row of tiles begin at different stages and go round.
-  int turn = -1, sent_at = 0;
-  if (MODE == kBackward && K % BK == 0 && K > 0) {
-    turn = K / BK;
-    sent_at = __builtin_amdgcn_readfirstlane((int)((t.c0 / BN * 3 + t.expert) % turn));
-    xa += sent_at * step_a;
-    xb += sent_at * step_b;
-  }
-  const uint32_t la = lds_address(ta + wave * 64), lb = lds_address(tb + wave * 64);
-
-  int reading = 0, sending = 0;   // buffers of the stages that are read, and sent for, next
-  int base = 0, end = K;   // the contraction [base, end) of this round (kWeights: the places in the list)
-  uint32_t row_next[kPA];   // kWeights: the rows of x of the next stage that is sent for
-  auto look_up = [&](int stage) {
-    if (MODE == kWeights) {
-#pragma unroll
-      for (int i = 0; i < kPA; i++) row_next[i] = list[(stage * BK + ka[i]) & (kList - 1)];
-    }
-  };
-  // load i of a stage: the slots of a, then those of b
-  auto send = [&](int i) {
-    if (i < kPA) load_lds(xa, oa[i < kPA ? i : 0] + (MODE == kWeights ? row_next[i < kPA ? i : 0] : 0),
-                          la + sending * kBytesA + i * kThreads * 16);
-    else load_lds(xb, ob[i < kPA ? 0 : i - kPA], lb + sending * kBytesB + (i - kPA) * kThreads * 16);
-  };
-  auto sent_all = [&]() {
-    xa += step_a;
-    xb += step_b;
-    sending = sending + 1 == NS ? 0 : sending + 1;
-    if (MODE == kBackward && ++sent_at == turn) {   // round the end of the contraction
-      xa -= turn * step_a;
-      xb -= turn * step_b;
-      sent_at = 0;
-    }
-  };
-  // the same for any stage, also one that the contraction ends in
-  auto send_stage = [&](int stage) {
-    const int left = end - base - stage * BK;
-    look_up(stage);
-    if (left >= BK) {
-#pragma unroll
-      for (int i = 0; i < kLoads; i++) send(i);
-    } else {
-#pragma unroll
-      for (int i = 0; i < kLoads; i++) {
-        const bool is_a = i < kPA;
-        const int sl = is_a ? i : i - kPA;
-        if ((is_a ? ka[is_a ? sl : 0] : kb[is_a ? 0 : sl]) < left) send(i);
-        else if (is_a) ta[sending * kCA + tid + sl * kThreads] = u32x4{0, 0, 0, 0};
-        else tb[sending * kCB + tid + sl * kThreads] = u32x4{0, 0, 0, 0};
-      }
-    }
-    sent_all();
-  };
-
-  // this lane's fragments, in the buffer of the stage that is read next
-  FragK<KS> ra_k(ta, wr), rb_k(tb, wc);
-  FragT<BM, FM> ra_t(ta, wr);
-  FragT<BN, FN> rb_t(tb, wc);
-  bf16x8 fa[2][FM], fb[2][FN];
-  auto read_a = [&](int k, int i, bf16x8 *d) { d[i] = MODE == kWeights ? ra_t.get(k, i) : ra_k.get(k, i); };
-  auto read_b = [&](int k, int i, bf16x8 *d) { d[i] = MODE == kBackward ? rb_k.get(k, i) : rb_t.get(k, i); };
-  auto advance = [&]() {
-    const bool wrap = reading + 1 == NS;
-    const int32_t by_a = wrap ? -(NS - 1) * kBytesA : kBytesA, by_b = wrap ? -(NS - 1) * kBytesB : kBytesB;
-    if (MODE == kWeights) ra_t.move(by_a);
-    else ra_k.move(by_a);
-    if (MODE == kBackward) rb_k.move(by_b);
-    else rb_t.move(by_b);
-    reading = wrap ? 0 : reading + 1;
-  };
-  // multiply fragments X; NEXT: read step k of the stage that is read next into the others; MORE: send for a
-  // stage. The loads come first.
-  auto step = [&](auto X, auto NEXT, auto MORE, int k) {
-    constexpr int x = X, y = 1 - x, kDo = (MORE ? kLoads : 0) + (NEXT ? FM + FN : 0);
-    auto due = [](int m) { return m >= FM * FN - 2 ? kDo : m * kDo / (FM * FN - 2); };   // how many come before instruction m
-#pragma unroll
-    for (int m = 0; m < FM * FN; m++) {
-      mfma<kInA>(acc[m / FN][m % FN], fb[x][m % FN], fa[x][m / FN]);
-#pragma unroll
-      for (int d = due(m); d < due(m + 1); d++) {
-        const int r = d - (MORE ? kLoads : 0);
-        if (r < 0) send(d);
-        else if (r < FM) read_a(k, r, fa[y]);
-        else read_b(k, r - FM, fb[y]);
-      }
-    }
-    if (MORE) sent_all();
-    if (NEXT && k == KS - 1) advance();
-  };
-  const std::integral_constant<int, 0> even;
-  const std::integral_constant<int, 1> odd;
-  const std::true_type yes;
-  const std::false_type no;
-
-  for (; base < K; base = end) {
-    if (MODE == kWeights) {
-      end = base + round_length(base, K, kList);
-      __syncthreads();   // the list of the round before is no longer read
-      for (int i = tid; i < end - base; i += kThreads) {
-        const int64_t p = t.first + base + i;
-        list[i] = (uint32_t)((a.gather ? (int64_t)(a.rows[p] / a.k) : p) * a.ldx * 2);
-      }
-      __syncthreads();
-    }
-    const int S = (end - base + BK - 1) / BK;
-    for (int i = 0; i < kAhead && i < S; i++) send_stage(i);
-    // of the stages that were sent for, all but `n` have arrived in every wave
-    auto meet = [&](bool whole, auto n) {
-      if (whole) vm_wait<n * kLoads>();
-      else vm_wait<0>();   // the last stage may have sent for less than kLoads loads
-      __syncthreads();
-    };
-    const std::integral_constant<int, kAhead - 1> one;    // one stage is there
-    const std::integral_constant<int, kAhead - 2> two;
-    meet(S > kAhead, one);
-#pragma unroll
-    for (int i = 0; i < FM; i++) read_a(0, i, fa[0]);
-#pragma unroll
-    for (int i = 0; i < FN; i++) read_b(0, i, fb[0]);
-    if (KS == 1) advance();
-    int s = 0;
-    if constexpr (KS == 1) {
-      // Before stage s: stage s + 1 is there, and the buffer of stage s + kAhead is no longer read.
-      look_up(kAhead);
-      for (; s + kAhead + 2 < S; s += 2) {    // sends for stages s + kAhead and s + kAhead + 1, which are whole
-        meet(true, two);
-        step(even, yes, yes, 0);
-        look_up(s + kAhead + 1);
-        meet(true, two);
-        step(odd, yes, yes, 0);
-        look_up(s + kAhead + 2);
-      }
-      for (; s + 1 < S; s += 2) {
-        meet(s + kAhead < S, two);
-        if (s + kAhead < S) send_stage(s + kAhead);
-        step(even, yes, no, 0);
-        meet(s + kAhead + 1 < S, two);
-        if (s + kAhead + 1 < S) send_stage(s + kAhead + 1);
-        step(odd, yes, no, 0);   // at the end of an even number of stages this reads what is not used
-      }
-      if (s < S) step(even, no, no, 0);
-    } else {
-      // Between a stage's steps: stage s + 1 is there, and the buffer of stage s, the one of s + kAhead, is no longer read.
-      auto first_step = [&]() {
-        step(even, yes, no, 1);
-      };
-      for (; s + kAhead + 1 < S; s++) {   // sends for stage s + kAhead, which is whole
-        first_step();
-        meet(true, two);
-        step(odd, yes, yes, 0);
-      }
-      for (; s < S; s++) {
-        first_step();
-        meet(s + kAhead < S, two);
-        if (s + kAhead < S) send_stage(s + kAhead);
-        step(odd, yes, no, 0);   // of the last stage: reads what is not used
-      }
-    }
-    if (kInA) mfma_done(acc);   // here, not after the loop: where a contraction may be empty, the sums are copied on the loop's way out
-    // the next round, if any, starts in the buffer that is sent for next
-    while (reading != sending) advance();
-    __syncthreads();   // the buffers are no longer read
-  }
-  if (MODE != kWeights && a.part) a.y = static_cast<float *>(a.y) + (int64_t)blockIdx.y * a.places * a.ldy;
-  store_tile<MODE, FM, FN, true>(a, t, wr, wc, acc, reinterpret_cast<char *>(lds) + wave * (FM * FN * 512));
+__global__ __launch_bounds__(256, per_unit(FM, FN, KS)) void tile_kernel(ProductArgs a) {
+  tile_body<MODE, FM, FN, NS, KS>(a, ExpertOp());
 }
 
 // ---- tiles of any shape ---------------------------------------------------------------------
