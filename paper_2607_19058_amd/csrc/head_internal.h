@@ -22,6 +22,31 @@ struct HeadProduct {
   int64_t pad_rows, pad_cols; // kOuter: a's columns; b's columns or rows
 };
 
+// Tiles of the head's products, and about how long they take (us, contraction 2048): `full` a round with work-groups on all slots of the
+// chip, `lone` one with a work-group on each compute unit at most. Both grow with the contraction. Measured with each tile forced:
+//   logits of 4096 rows, 16384 words of width 2048 (forward | tied): 226 231 286 339 | 223 261 287 310;  of 1024 rows and 1152 words: 56 46
+//   30 26 | 57 47 33 28.  Rows' gradient, 4096 x 4096 from 4096 words (untied, tied): 127 142 - 164, 117 123 - 181, weights' 122 122 - 183
+struct HeadTile {
+  int rows, cols, slots;
+  double full, lone;
+};
+constexpr int kHeadTiles = 4;
+inline HeadTile head_tile(bool backward, int i) {
+  static const HeadTile tiles[2][kHeadTiles] = {{{256, 256, 256, 54, 54}, {128, 256, 512, 58, 40}, {64, 256, 512, 36, 24}, {64, 128, 768, 33, 20}},
+                                                {{256, 256, 256, 56, 56}, {128, 256, 512, 70, 46}, {64, 256, 512, 36, 25}, {64, 128, 768, 32, 21}}};
+  return tiles[backward ? 1 : 0][i];
+}
+inline int64_t head_count(const HeadTile &t, int64_t rows, int64_t cols) {
+  return ((rows + t.rows - 1) / t.rows) * ((cols + t.cols - 1) / t.cols);
+}
+// of n tiles with contractions of K, and their launch
+inline double head_time(const HeadTile &t, int64_t n, int64_t K) {
+  constexpr int64_t kUnits = 256;
+  const int64_t left = n % t.slots;
+  const double more = left > kUnits ? (double)(left - kUnits) / (t.slots - kUnits) : 0.0;
+  return ((double)(n / t.slots) * t.full + (left ? t.lone + (t.full - t.lone) * more : 0.0)) * (double)(K + 128) / 2176 + 4;
+}
+
 // Forward: of each row and each run of 128 (or 64, ...) columns that a wave has, the largest base-2 exponent and the sum
 // of the powers relative to it; the logit of the row's target.
 struct HeadForward {
@@ -35,6 +60,12 @@ struct HeadForward {
 };
 int head_parts(int mode, const HeadProduct &p);   // runs that a row's columns fall into
 int launch_head_forward(int mode, const HeadProduct &p, const HeadForward &f, void *stream);
+
+// The same for up to 64 rows, whose product is bound by b's bytes: any position and alignment, K and cols as they are (no padding). One
+// pair a row and work-group.
+constexpr int64_t kFewRows = 64;
+int64_t head_few_parts(int mode, const HeadProduct &p);
+int launch_head_few(int mode, const HeadProduct &p, const HeadForward &f, void *stream);
 
 // Backward: G of this product's columns, float16 [rows x ldg].
 struct HeadGrad {

@@ -16,13 +16,14 @@ __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(
 // The tile of a product without experts.
 template <int MODE, int BM, int BN>
 __device__ __forceinline__ bool take_plain(const ProductArgs &a, Tile *t) {
-  uint32_t tr, tc;
+  uint32_t tr, tc, part;
   t->expert = 0;
   t->first = 0;
+  t->part = 0;
   t->r1 = a.places;
   t->c1 = MODE == kBackward ? a.n : a.m;
   t->K = (int)(MODE == kBackward ? a.m : a.n);
-  if (!patch_tile(a.in_patches, (uint32_t)a.row_tiles, ((uint32_t)t->c1 + BN - 1) / BN, &tr, &tc)) return false;
+  if (!plain_tile((uint32_t)a.row_tiles, ((uint32_t)t->c1 + BN - 1) / BN, 1, &tr, &tc, &part)) return false;
   t->r0 = (int64_t)tr * BM;
   t->c0 = (int64_t)tc * BN;
   return true;
@@ -147,25 +148,47 @@ __global__ __launch_bounds__(256, per_unit(FM, FN, KS)) void logits_kernel(Produ
   tile_body<MODE, FM, FN, NS, KS>(a, op);
 }
 
-int tile_rows(int s) { return s == 0 ? 256 : s == 1 ? 128 : 64; }
-int tile_cols(int s) { return s == 3 ? 128 : 256; }
+constexpr int64_t kMostGroups = 1 << 24;
 
-// Which tile: the one whose rounds over the chip take the least time.
-int choose_logits(int mode, const HeadProduct &p) {
-  // a round of tiles of 256 x 256, 128 x 256, 64 x 256 and 64 x 128 with their work-groups on every compute unit takes this, relatively
-  const double round[4] = {1.0, mode == kBackward ? 0.58 : 1.15, 0.73, 0.68};
-  const int slots[4] = {256, mode == kBackward ? 256 : 512, 512, 768};
-  int best = 0;
+// Which tile: the one that takes the least time. Where the last round of large tiles would be nearly empty, the columns past the whole
+// rounds (first to last) get tiles of their own.
+struct Choice {
+  int tile;
+  int64_t first;   // columns that `tile` takes; the rest has `rest`
+  int rest;
+};
+double best_of(int mode, int64_t rows, int64_t cols, int64_t K, int *tile) {
   double least = 1e300;
-  for (int s = 0; s < 4; s++) {
-    const int64_t n = ((p.rows + tile_rows(s) - 1) / tile_rows(s)) * ((p.cols + tile_cols(s) - 1) / tile_cols(s));
-    const double t = (double)((n + slots[s] - 1) / slots[s]) * round[s];
-    if (t < least) {
-      least = t;
-      best = s;
+  for (int i = 0; i < kHeadTiles; i++) {
+    const HeadTile t = head_tile(mode == kBackward, i);
+    const double time = head_time(t, head_count(t, rows, cols), K);
+    if (time < least) {
+      least = time;
+      *tile = i;
     }
   }
-  return best;
+  return least;
+}
+Choice choose_logits(int mode, const HeadProduct &p) {
+  Choice c = {0, p.cols, 0};
+  const double all = best_of(mode, p.rows, p.cols, p.K, &c.tile);
+  const HeadTile large = head_tile(mode == kBackward, 0);
+  const int64_t down = (p.rows + large.rows - 1) / large.rows;
+  const int64_t first = head_count(large, p.rows, p.cols) / large.slots * large.slots / down * large.cols;
+  if (first > 0 && first < p.cols) {
+    int rest;
+    const double time = head_time(large, first / large.cols * down, p.K) + best_of(mode, p.rows, p.cols - first, p.K, &rest);
+    if (time < 0.97 * all) c = {0, first, rest};
+  }
+  return c;
+}
+// The columns of a product from `at` on, `cols` of them (at: a multiple of every tile's).
+HeadProduct columns(int mode, const HeadProduct &p, int64_t at, int64_t cols) {
+  HeadProduct q = p;
+  q.b = static_cast<const bf16_t *>(p.b) + (mode == kBackward ? at * p.ldb : at);
+  q.cols = cols;
+  q.pad_cols = at + cols == p.cols ? p.pad_cols - at : cols;
+  return q;
 }
 
 ProductArgs args_of(const HeadProduct &p, int mode, int tile) {
@@ -179,36 +202,58 @@ ProductArgs args_of(const HeadProduct &p, int mode, int tile) {
   a.m = mode == kBackward ? p.K : p.pad_cols;
   a.k = 1;
   a.experts = 1;
-  a.row_tiles = (p.rows + tile_rows(tile) - 1) / tile_rows(tile);
-  a.in_patches = patches(a.row_tiles, (p.pad_cols + tile_cols(tile) - 1) / tile_cols(tile)) >= kMinPatches;
+  a.row_tiles = (p.rows + head_tile(mode == kBackward, tile).rows - 1) / head_tile(mode == kBackward, tile).rows;
   return a;
 }
 
 template <class Op, int MODE, int FM, int FN, int NS, int KS>
 int launch_one(const HeadProduct &p, const Op &op, int tile, void *stream) {
   const ProductArgs a = args_of(p, MODE, tile);
-  const int64_t grid = patch_grid(a.row_tiles, (p.pad_cols + 32 * FN - 1) / (32 * FN), a.in_patches);
-  if (grid > 0x7FFFFFFF) return (int)hipErrorInvalidConfiguration;
+  const int64_t grid = plain_grid(a.row_tiles * ((p.pad_cols + 32 * FN - 1) / (32 * FN)));
+  if (grid > kMostGroups) return (int)hipErrorInvalidConfiguration;
   logits_kernel<MODE, FM, FN, NS, KS, Op><<<(unsigned)grid, 256, 0, static_cast<hipStream_t>(stream)>>>(a, op);
   return (int)hipGetLastError();
 }
 template <class Op, int MODE>
-int launch_mode(const HeadProduct &p, const Op &op, void *stream) {
+int launch_tiles(const HeadProduct &p, const Op &op, int tile, void *stream) {
   constexpr int S = MODE == kBackward ? 2 : 1;
-  const int tile = choose_logits(MODE, p);
   switch (tile) {
     case 0: return launch_one<Op, MODE, 8, 8, 4 / S, S>(p, op, tile, stream);
-    case 1: return launch_one<Op, MODE, 4, 8, 3, S>(p, op, tile, stream);
+    case 1: return launch_one<Op, MODE, 4, 8, 3, 1>(p, op, tile, stream);
     case 2: return launch_one<Op, MODE, 2, 8, 4 / S, S>(p, op, tile, stream);
     default: return launch_one<Op, MODE, 2, 4, 4 / S, S>(p, op, tile, stream);
   }
+}
+int runs(int mode, int tile, int64_t cols) {   // of a wave's columns
+  const int w = head_tile(mode == kBackward, tile).cols;
+  return (int)((cols + w - 1) / w) * 2;
+}
+ForwardOp shifted(const ForwardOp &op, int mode, const Choice &c) {
+  ForwardOp o = op;
+  o.f.col0 += c.first;
+  o.f.part_at += runs(mode, c.tile, c.first);
+  return o;
+}
+GradOp shifted(const GradOp &op, int, const Choice &c) {
+  GradOp o = op;
+  o.g.col0 += c.first;
+  o.g.g += c.first;
+  return o;
+}
+template <class Op, int MODE>
+int launch_mode(const HeadProduct &p, const Op &op, void *stream) {
+  const Choice c = choose_logits(MODE, p);
+  if (c.first == p.cols) return launch_tiles<Op, MODE>(p, op, c.tile, stream);
+  const int e = launch_tiles<Op, MODE>(columns(MODE, p, 0, c.first), op, c.tile, stream);
+  if (e != (int)hipSuccess) return e;
+  return launch_tiles<Op, MODE>(columns(MODE, p, c.first, p.cols - c.first), shifted(op, MODE, c), c.rest, stream);
 }
 
 }  // namespace
 
 int head_parts(int mode, const HeadProduct &p) {
-  const int cols = tile_cols(choose_logits(mode, p));
-  return (int)((p.cols + cols - 1) / cols) * 2;
+  const Choice c = choose_logits(mode, p);
+  return runs(mode, c.tile, c.first) + (c.first < p.cols ? runs(mode, c.rest, p.cols - c.first) : 0);
 }
 int launch_head_forward(int mode, const HeadProduct &p, const HeadForward &f, void *stream) {
   const ForwardOp op = {f};

@@ -279,17 +279,24 @@ struct Regions {
   }
 };
 
+// x w as they are
+HeadProduct whole_of(const skew_head_desc &h) { return {h.x, h.w, h.ldx, h.ldw, h.tokens, h.vocab, h.d, 0, h.vocab}; }
+
 struct ForwardPlan : HeadPlan {
+  bool few;
   int64_t part_ld;
   size_t part, sum, x, w, bytes;
 };
 ForwardPlan forward_plan(const skew_head_desc &h) {
   ForwardPlan f;
   static_cast<HeadPlan &>(f) = head_plan(h, false);
+  f.few = h.tokens <= kFewRows;
+  if (f.few) f.x_as_is = f.w_as_is = true;   // (whatever their alignment)
   // rows of the last run may be fewer, and their tiles narrower
-  f.part_ld = 0;
+  f.part_ld = f.few ? head_few_parts(mode_of(h), whole_of(h)) : 0;
   const int64_t last = h.tokens % f.run ? h.tokens % f.run : f.run;
   for (const int64_t rows : {f.run, last}) {
+    if (f.few) break;
     int64_t ld = 0;
     for (int64_t v0 = 0; v0 < h.vocab; v0 += f.piece) ld += head_parts(mode_of(h), logits_of(h, f, nullptr, 0, rows, v0, nullptr));
     f.part_ld = std::max(f.part_ld, ld);
@@ -370,6 +377,11 @@ int launch_head_loss(const skew_head_desc &h, float *loss, float *lse, char *ws,
   float2 *part = reinterpret_cast<float2 *>(ws + f.part);
   float *sum = reinterpret_cast<float *>(ws + f.sum);
   bf16_t *x_copy = reinterpret_cast<bf16_t *>(ws + f.x), *w_copy = reinterpret_cast<bf16_t *>(ws + f.w);
+  if (f.few) {
+    TRY(launch_head_few(mode_of(h), whole_of(h), {c, h.targets, h.target_bytes, h.vocab, 0, part, f.part_ld, 0, sum}, stream));
+    loss_kernel<<<(unsigned)((h.tokens + 3) / 4), kThreads, 0, s>>>(h, c, part, f.part_ld, (int)f.part_ld, sum, loss, lse);
+    return (int)hipGetLastError();
+  }
   for (int64_t t0 = 0; t0 < h.tokens; t0 += f.run) {
     skew_head_desc r = h;   // this run's rows
     r.tokens = std::min(f.run, h.tokens - t0);

@@ -9,15 +9,17 @@ struct ResultOp {
   static constexpr bool kHalf = true;
   HeadResult r;
   int64_t rows, cols;
+  int32_t parts;
   template <int MODE, int BM, int BN>
   __device__ __forceinline__ bool take(const ProductArgs &a, Tile *t) const {
-    uint32_t tr, tc;
+    uint32_t tr, tc, part;
     t->expert = 0;
     t->first = 0;
     t->r1 = MODE == kOuter ? a.n : a.places;
     t->c1 = MODE == kBackward ? a.n : a.m;
     t->K = (int)(MODE == kOuter ? a.places : MODE == kBackward ? a.m : a.n);
-    if (!patch_tile(a.in_patches, (uint32_t)a.row_tiles, ((uint32_t)t->c1 + BN - 1) / BN, &tr, &tc)) return false;
+    if (!plain_tile((uint32_t)a.row_tiles, ((uint32_t)t->c1 + BN - 1) / BN, (uint32_t)parts, &tr, &tc, &part)) return false;
+    t->part = (int)part;
     t->r0 = (int64_t)tr * BM;
     t->c0 = (int64_t)tc * BN;
     return true;
@@ -28,7 +30,7 @@ struct ResultOp {
     const int lane = threadIdx.x & 63;
     const int64_t row_w = t.r0 + wr, col_w = t.c0 + wc, row0 = row_w + (lane & 15), col0 = col_w + (lane >> 4) * 4;
     if (a.part) {   // the sums themselves, for join_kernel
-      float *y = static_cast<float *>(a.y) + (int64_t)blockIdx.y * rows * a.ldy + row0 * a.ldy + col0;
+      float *y = static_cast<float *>(a.y) + (int64_t)t.part * rows * a.ldy + row0 * a.ldy + col0;
 #pragma unroll
       for (int i = 0; i < FM; i++) {
         if (row0 + i * 16 >= rows) break;
@@ -106,30 +108,73 @@ __global__ __launch_bounds__(256) void join_kernel(HeadResult r, int64_t rows, i
   else store8(static_cast<bf16_t *>(r.y) + p.row * r.ldy + p.col, n, v);
 }
 
-// Which tile, and how many work-groups share a contraction.
+constexpr int64_t kMostGroups = 1 << 24;
+
+// Which tile, and how many work-groups share a contraction (their parts go through memory, and join_kernel adds them up: a launch, and
+// the bytes at some 4 TB/s).
 struct Choice {
   int tile, parts;
 };
-int tile_rows(int s) { return s == 0 ? 256 : s == 1 ? 128 : 64; }
-int tile_cols(int s) { return s == 2 ? 128 : 256; }
-Choice choose_result(int mode, const HeadProduct &p) {
-  const double round[3] = {1.0, mode == kBackward ? 0.58 : 1.15, 0.68};
-  const int slots[3] = {256, mode == kBackward ? 256 : 512, 768};
-  Choice best = {0, 1};
+double best_of(int mode, int64_t rows, int64_t cols, int64_t K, Choice *c) {
   double least = 1e300;
-  for (int s = 0; s < 3; s++) {
-    const int64_t n = ((p.rows + tile_rows(s) - 1) / tile_rows(s)) * ((p.cols + tile_cols(s) - 1) / tile_cols(s));
-    int64_t parts = slots[s] / n;
-    if (parts > p.K / 512) parts = p.K / 512;
-    if (parts < 1) parts = 1;
-    if (parts > 64) parts = 64;
-    const double t = (double)((n * parts + slots[s] - 1) / slots[s]) * round[s] * ((double)p.K / parts + 256);
-    if (t < least) {
-      least = t;
-      best = {s, (int)parts};
+  for (const int tile : {0, 1, 3}) {
+    const HeadTile t = head_tile(mode == kBackward, tile);
+    const int64_t n = head_count(t, rows, cols);
+    for (const int parts : {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 48, 64}) {
+      if (parts > 1 && (K / parts < 128 || n * parts > 2 * t.slots)) break;
+      const double time = head_time(t, n * parts, K / parts) + (parts > 1 ? 4 + (double)parts * rows * cols * 4 * 2 / 4e6 : 0);
+      if (time < least) {
+        least = time;
+        *c = {tile, parts};
+      }
     }
   }
-  return best;
+  return least;
+}
+// Where the last round of large tiles would be nearly empty, or the last row or column of them, what lies past the whole ones is
+// a product of its own.
+struct Plan {
+  Choice main, rest;
+  int64_t rows, cols;   // of main
+};
+Plan plan_result(int mode, const HeadProduct &p) {
+  Plan s = {{0, 1}, {0, 0}, p.rows, p.cols};
+  double least = 0.97 * best_of(mode, p.rows, p.cols, p.K, &s.main);
+  const HeadTile t = head_tile(mode == kBackward, 0);
+  const int64_t down = (p.rows + t.rows - 1) / t.rows, across = (p.cols + t.cols - 1) / t.cols, whole = down * across / t.slots * t.slots;
+  auto cut = [&](int64_t rows, int64_t cols) {   // (one of them all)
+    if (rows == 0 || cols == 0 || (rows >= p.rows && cols >= p.cols)) return;
+    Plan c = {{0, 1}, {0, 1}, rows, cols};
+    const double time = best_of(mode, rows, cols, p.K, &c.main) +
+                        best_of(mode, rows < p.rows ? p.rows - rows : rows, rows < p.rows ? cols : p.cols - cols, p.K, &c.rest);
+    if (time < least) {
+      least = time;
+      s = c;
+    }
+  };
+  cut(whole / across * t.rows, p.cols);
+  cut(p.rows, whole / down * t.cols);
+  cut(p.rows / t.rows * t.rows, p.cols);
+  cut(p.rows, p.cols / t.cols * t.cols);
+  return s;
+}
+// The part of a product from (row, col) on, and of its result.
+HeadProduct part_of(int mode, const HeadProduct &p, int64_t row, int64_t col, int64_t rows, int64_t cols) {
+  HeadProduct q = p;
+  q.a = static_cast<const bf16_t *>(p.a) + (mode == kOuter ? row : row * p.lda);
+  q.b = static_cast<const bf16_t *>(p.b) + (mode == kBackward ? col * p.ldb : col);
+  q.rows = rows;
+  q.cols = cols;
+  q.pad_rows = row + rows == p.rows ? p.pad_rows - row : rows;
+  q.pad_cols = col + cols == p.cols ? p.pad_cols - col : cols;
+  return q;
+}
+HeadResult result_of(const HeadResult &r, int64_t row, int64_t col) {
+  HeadResult q = r;
+  q.y = static_cast<char *>(r.y) + (row * r.ldy + col) * (r.y_dtype == SKEW_F32 ? 4 : 2);
+  if (r.prev) q.prev = r.prev + row * r.ldprev + col;
+  q.top = r.top + (r.by_row ? row : col);
+  return q;
 }
 int64_t part_ld(int64_t cols) { return (cols + 7) / 8 * 8; }
 
@@ -147,7 +192,6 @@ int launch_one(const HeadProduct &p, const HeadResult &r, Choice c, char *ws, vo
   a.m = MODE == kBackward ? p.K : p.pad_cols;
   a.row_tiles = (p.rows + 32 * FM - 1) / (32 * FM);
   const int64_t cols = (p.pad_cols + 32 * FN - 1) / (32 * FN);
-  a.in_patches = patches(a.row_tiles, cols) >= kMinPatches;
   int parts = 1;
   if (c.parts > 1) {
     a.part = (int32_t)(((p.K + c.parts - 1) / c.parts + 63) / 64 * 64);
@@ -155,10 +199,10 @@ int launch_one(const HeadProduct &p, const HeadResult &r, Choice c, char *ws, vo
     a.y = ws;
     a.ldy = part_ld(p.cols);
   }
-  const int64_t grid = patch_grid(a.row_tiles, cols, a.in_patches);
-  if (grid > 0x7FFFFFFF) return (int)hipErrorInvalidConfiguration;
+  const int64_t grid = plain_grid(a.row_tiles * cols * parts);
+  if (grid > kMostGroups) return (int)hipErrorInvalidConfiguration;
   hipStream_t s = static_cast<hipStream_t>(stream);
-  result_kernel<MODE, FM, FN, NS, KS><<<dim3((unsigned)grid, parts), 256, 0, s>>>(a, ResultOp{r, p.rows, p.cols});
+  result_kernel<MODE, FM, FN, NS, KS><<<(unsigned)grid, 256, 0, s>>>(a, ResultOp{r, p.rows, p.cols, parts});
   const int e = (int)hipGetLastError();
   if (e != (int)hipSuccess || c.parts == 1) return e;
   join_kernel<<<(unsigned)((p.rows * (part_ld(p.cols) / 8) + 255) / 256), 256, 0, s>>>(r, p.rows, p.cols, reinterpret_cast<float *>(ws), parts,
@@ -166,19 +210,33 @@ int launch_one(const HeadProduct &p, const HeadResult &r, Choice c, char *ws, vo
   return (int)hipGetLastError();
 }
 template <int MODE>
-int launch_mode(const HeadProduct &p, const HeadResult &r, char *ws, void *stream) {
+int launch_choice(const HeadProduct &p, const HeadResult &r, Choice c, char *ws, void *stream) {
   constexpr int S = MODE == kBackward ? 2 : 1;
-  const Choice c = choose_result(MODE, p);
   if (c.tile == 0) return launch_one<MODE, 8, 8, 4 / S, S>(p, r, c, ws, stream);
-  if (c.tile == 1) return launch_one<MODE, 4, 8, 3, S>(p, r, c, ws, stream);
+  if (c.tile == 1) return launch_one<MODE, 4, 8, 3, 1>(p, r, c, ws, stream);
   return launch_one<MODE, 2, 4, 4 / S, S>(p, r, c, ws, stream);
+}
+template <int MODE>
+int launch_mode(const HeadProduct &p, const HeadResult &r, char *ws, void *stream) {
+  const Plan s = plan_result(MODE, p);
+  if (s.rest.parts == 0) return launch_choice<MODE>(p, r, s.main, ws, stream);
+  const int e = launch_choice<MODE>(part_of(MODE, p, 0, 0, s.rows, s.cols), r, s.main, ws, stream);
+  if (e != (int)hipSuccess) return e;
+  const int64_t row = s.rows < p.rows ? s.rows : 0, col = s.rows < p.rows ? 0 : s.cols;
+  return launch_choice<MODE>(part_of(MODE, p, row, col, p.rows - row, p.cols - col), result_of(r, row, col), s.rest, ws, stream);
+}
+size_t scratch_of(const Choice &c, int64_t rows, int64_t cols) {
+  return c.parts > 1 ? pad256((size_t)c.parts * (size_t)rows * (size_t)part_ld(cols) * 4) : 0;
 }
 
 }  // namespace
 
 size_t head_result_scratch(int mode, const HeadProduct &p) {
-  const Choice c = choose_result(mode, p);
-  return c.parts > 1 ? pad256((size_t)c.parts * (size_t)p.rows * (size_t)part_ld(p.cols) * 4) : 0;
+  const Plan s = plan_result(mode, p);
+  const size_t main = scratch_of(s.main, s.rows, s.cols);
+  if (s.rest.parts == 0) return main;
+  const size_t rest = scratch_of(s.rest, s.rows < p.rows ? p.rows - s.rows : p.rows, s.rows < p.rows ? p.cols : p.cols - s.cols);
+  return main > rest ? main : rest;
 }
 int launch_head_result(int mode, const HeadProduct &p, const HeadResult &r, char *ws, void *stream) {
   if (mode == kOuter) return launch_mode<kOuter>(p, r, ws, stream);

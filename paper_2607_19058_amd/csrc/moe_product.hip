@@ -17,19 +17,6 @@
 namespace moe {
 namespace {
 
-// 8 values at p, of which the first n exist (n <= 0: none)
-__device__ __forceinline__ u32x4 load_chunk(const bf16_t *p, int64_t n) {
-  u32x4 u = {0, 0, 0, 0};
-  if (n >= 8) {
-    u = *reinterpret_cast<const u32x4_a2 *>(p);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 7; i++)
-      if (i < n) u[i >> 1] |= (uint32_t)p[i].v << (16 * (i & 1));
-  }
-  return u;
-}
-
 // 4 neighbouring results at element `at`, of which the first n exist
 __device__ __forceinline__ void store4(const ProductArgs &a, int64_t at, int64_t n, f32x4 v) {
   if (a.f32) {
@@ -92,6 +79,7 @@ template <int MODE, int BM, int BN>
 __device__ __forceinline__ bool take_tile(const ProductArgs &a, Tile *t) {
   uint32_t tr, tc;   // (the grid has fewer than 2^31 tiles)
   t->first = 0;
+  t->part = blockIdx.y;
   t->c1 = MODE == kBackward ? a.n : a.m;
   const uint32_t cols = ((uint32_t)t->c1 + BN - 1) / BN;
   if (MODE == kWeights) {
