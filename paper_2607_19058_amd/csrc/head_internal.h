@@ -61,11 +61,11 @@ struct HeadForward {
 int head_parts(int mode, const HeadProduct &p);   // runs that a row's columns fall into
 int launch_head_forward(int mode, const HeadProduct &p, const HeadForward &f, void *stream);
 
-// The same for up to 64 rows, whose product is bound by b's bytes: any position and alignment, K and cols as they are (no padding). One
-// pair a row and work-group.
-constexpr int64_t kFewRows = 64;
-int64_t head_few_parts(int mode, const HeadProduct &p);
-int launch_head_few(int mode, const HeadProduct &p, const HeadForward &f, void *stream);
+// The same (kForward) for up to 16 rows: any position and alignment, K and cols as they are (no padding); 32 rows of b lie within 2^31
+// bytes. One pair a row and work-group.
+constexpr int64_t kFewRows = 16;
+int64_t head_few_parts(int64_t cols);
+int launch_head_few(const HeadProduct &p, const HeadForward &f, void *stream);
 
 // Backward: G of this product's columns, float16 [rows x ldg].
 struct HeadGrad {

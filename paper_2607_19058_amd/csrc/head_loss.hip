@@ -16,6 +16,7 @@ namespace {
 
 enum { kForward = 0, kBackward = 1, kOuter = 3 };   // as in product_tiles.h
 constexpr int kThreads = 256;
+constexpr int64_t kMostGroups = 1 << 24;   // of a launch
 
 __device__ __forceinline__ int64_t id_at(const void *ids, int bytes, int64_t i) {
   return bytes == 8 ? static_cast<const int64_t *>(ids)[i] : static_cast<const int32_t *>(ids)[i];
@@ -41,50 +42,109 @@ __global__ __launch_bounds__(kThreads) void fill_zero_kernel(bf16_t *p, int64_t 
   if (at.there) store8(p + at.row * ld + at.col, cols - at.col, v);
 }
 
-// loss and lse of a row from its pairs: a wave a row.
+// loss and lse of a row from its pairs: W waves a row.
+struct Pair {
+  float m, s;   // s 2^m
+};
+__device__ __forceinline__ Pair joined(Pair a, Pair b) {
+  const float top = fmaxf(a.m, b.m), base = top == -INFINITY ? 0.0f : top;   // (a run past the end has -inf and 0)
+  return {top, a.s * __builtin_amdgcn_exp2f(a.m - base) + b.s * __builtin_amdgcn_exp2f(b.m - base)};
+}
+template <int W>
 __global__ __launch_bounds__(kThreads) void loss_kernel(skew_head_desc h, float c, const float2 *part, int64_t ld, int parts,
                                                         const float *target_sum, float *loss, float *lse) {
-  const int64_t t = (int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6);
-  const int lane = threadIdx.x & 63;
-  if (t >= h.tokens) return;
-  float m = -INFINITY, s = 0.0f;
-  for (int i = lane; i < parts; i += 64) {
-    const float2 p = part[t * ld + i];
-    const float top = fmaxf(m, p.x), base = top == -INFINITY ? 0.0f : top;   // (a run past the end has -inf and 0)
-    s = s * __builtin_amdgcn_exp2f(m - base) + p.y * __builtin_amdgcn_exp2f(p.x - base);
-    m = top;
+  constexpr int kRowsHere = kThreads / 64 / W;
+  __shared__ Pair held[kThreads / 64];
+  const int wave = threadIdx.x >> 6, in = threadIdx.x % (64 * W);
+  const int64_t t = (int64_t)blockIdx.x * kRowsHere + wave / W;
+  Pair p = {-INFINITY, 0.0f};
+  if (t < h.tokens) {
+#pragma unroll 4
+    for (int i = in; i < parts; i += 64 * W) {
+      const float2 q = part[t * ld + i];
+      p = joined(p, {q.x, q.y});
+    }
   }
-  for (int o = 32; o > 0; o >>= 1) {
-    const float m2 = __shfl_xor(m, o), s2 = __shfl_xor(s, o), top = fmaxf(m, m2), base = top == -INFINITY ? 0.0f : top;
-    s = s * __builtin_amdgcn_exp2f(m - base) + s2 * __builtin_amdgcn_exp2f(m2 - base);
-    m = top;
+  for (int o = 32; o > 0; o >>= 1) p = joined(p, {__shfl_xor(p.m, o), __shfl_xor(p.s, o)});
+  if (W > 1) {
+    if ((threadIdx.x & 63) == 0) held[wave] = p;
+    __syncthreads();
+    p = held[wave / W * W];
+#pragma unroll
+    for (int i = 1; i < W; i++) p = joined(p, held[wave / W * W + i]);
   }
-  if (lane == 0) {
+  if (in == 0 && t < h.tokens) {
     const bool token = is_token(h, t);
-    const double all = ((double)m + log2((double)s)) * ((double)h.scale / (double)c);
+    const double all = ((double)p.m + log2((double)p.s)) * ((double)h.scale / (double)c);
     lse[t] = token ? (float)all : 0.0f;
     loss[t] = token ? (float)(all - (double)h.scale * (double)target_sum[t]) : 0.0f;
   }
 }
+int launch_loss(const skew_head_desc &h, float c, const float2 *part, int64_t ld, int parts, const float *target_sum, float *loss, float *lse,
+                hipStream_t s) {
+  if (h.tokens <= 64) loss_kernel<4><<<(unsigned)h.tokens, kThreads, 0, s>>>(h, c, part, ld, parts, target_sum, loss, lse);
+  else loss_kernel<1><<<(unsigned)((h.tokens + 3) / 4), kThreads, 0, s>>>(h, c, part, ld, parts, target_sum, loss, lse);
+  return (int)hipGetLastError();
+}
 
-// Largest magnitudes, as bits, of the columns of `rows` x cols values (those of tokens, where h is given): top has to be zero before.
-// A work-group takes 256 columns of 128 rows, a thread 8 columns of every eighth row.
-constexpr int kTopRows = 128;
-__global__ __launch_bounds__(kThreads) void column_top_kernel(const bf16_t *x, int64_t ld, int64_t rows, int64_t cols, skew_head_desc h,
-                                                              int masked, uint32_t *top) {
+// The factors of G's rows.
+__device__ __forceinline__ void factors(const skew_head_desc &h, const float *dloss, const float *dlse, int64_t t, float *both, float *one) {
+  *one = h.scale * dloss[t];
+  *both = dlse ? h.scale * (dloss[t] + dlse[t]) : *one;
+}
+struct Factors {
+  const float *lse, *dloss, *dlse;
+  uint32_t *top;    // bits of their largest sum
+  HeadRow *row;
+  float c;
+};
+
+// The largest m of a work-group's threads, in every one of them.
+__device__ __forceinline__ uint32_t largest(uint32_t m) {
+  __shared__ uint32_t held[kThreads / 64];
+  for (int o = 32; o > 0; o >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, o));
+  if ((threadIdx.x & 63) == 0) held[threadIdx.x >> 6] = m;
+  __syncthreads();
+  return max(max(held[0], held[1]), max(held[2], held[3]));
+}
+
+// Largest magnitudes, as bits, of the columns of `rows` x cols values: top has to be zero before. A work-group takes 256 columns of
+// 8 `each` rows, a thread 8 columns of every eighth row. With `masked` rows that are no token are left out, and the work-groups past
+// those of x find the largest of G's factors.
+struct Tops {
+  const bf16_t *x;
+  int64_t ld, rows, cols;
+  uint32_t *top;
+  int32_t each, masked;
+  int64_t groups;
+};
+__global__ __launch_bounds__(kThreads) void top_kernel(Tops p, skew_head_desc h, Factors f) {
+  if (blockIdx.x >= p.groups) {
+    uint32_t m = 0;
+    const int64_t step = (int64_t)(gridDim.x - p.groups) * kThreads;
+    for (int64_t t = (blockIdx.x - p.groups) * kThreads + threadIdx.x; t < h.tokens; t += step)
+      if (is_token(h, t)) {
+        float both, one;
+        factors(h, f.dloss, f.dlse, t, &both, &one);
+        m = max(m, finite_bits(fabsf(both) + fabsf(one)));
+      }
+    m = largest(m);
+    if (threadIdx.x == 0 && m) atomicMax(f.top, m);
+    return;
+  }
   __shared__ uint32_t held[kThreads][9];
-  const int64_t strips = (cols + 255) / 256, strip = blockIdx.x % strips, row0 = blockIdx.x / strips * kTopRows;
-  const int lane = threadIdx.x & 31;
-  const int64_t col = strip * 256 + lane * 8;
+  const int64_t strips = (p.cols + 255) / 256, strip = blockIdx.x % strips, row0 = blockIdx.x / strips * (8 * p.each);
+  const int64_t col = strip * 256 + (threadIdx.x & 31) * 8;
   uint32_t m[8] = {};
 #pragma unroll 4
-  for (int i = threadIdx.x >> 5; i < kTopRows; i += 8) {
-    const int64_t row = row0 + i;
-    if (row >= rows || col >= cols || (masked && !is_token(h, row))) continue;
+  for (int i = 0; i < p.each; i++) {
+    const int64_t row = row0 + i * 8 + (threadIdx.x >> 5);
+    if (row >= p.rows || col >= p.cols) continue;
+    const bool token = !p.masked || is_token(h, row);
     float v[8];
-    load8(x + row * ld + col, cols - col, v);
+    load8(p.x + row * p.ld + col, p.cols - col, v);   // (whether it is a token's or not: the loads go together)
 #pragma unroll
-    for (int q = 0; q < 8; q++) m[q] = max(m[q], finite_bits(v[q]));
+    for (int q = 0; q < 8; q++) m[q] = max(m[q], token ? finite_bits(v[q]) : 0u);
   }
 #pragma unroll
   for (int q = 0; q < 8; q++) held[threadIdx.x][q] = m[q];
@@ -92,59 +152,24 @@ __global__ __launch_bounds__(kThreads) void column_top_kernel(const bf16_t *x, i
   const int c = threadIdx.x;   // a thread a column
   uint32_t all = 0;
   for (int i = 0; i < 8; i++) all = max(all, held[i * 32 + c / 8][c % 8]);
-  if (strip * 256 + c < cols && all) atomicMax(top + strip * 256 + c, all);
+  if (strip * 256 + c < p.cols && all) atomicMax(p.top + strip * 256 + c, all);   // (an old value looked up first: 37 -> 66 us for 103 M values)
 }
 
-// The factors of G's rows: their largest sum, as bits (zero before).
-__device__ __forceinline__ void factors(const skew_head_desc &h, const float *dloss, const float *dlse, int64_t t, float *both, float *one) {
-  *one = h.scale * dloss[t];
-  *both = dlse ? h.scale * (dloss[t] + dlse[t]) : *one;
-}
-__global__ __launch_bounds__(kThreads) void factor_top_kernel(skew_head_desc h, const float *dloss, const float *dlse, uint32_t *top) {
-  __shared__ uint32_t held[kThreads];
-  uint32_t m = 0;
-  for (int64_t t = (int64_t)blockIdx.x * kThreads + threadIdx.x; t < h.tokens; t += (int64_t)gridDim.x * kThreads)
-    if (is_token(h, t)) {
-      float both, one;
-      factors(h, dloss, dlse, t, &both, &one);
-      m = max(m, finite_bits(fabsf(both) + fabsf(one)));
-    }
-  held[threadIdx.x] = m;
-  for (int o = kThreads / 2; o > 0; o >>= 1) {
-    __syncthreads();
-    if (threadIdx.x < o) held[threadIdx.x] = max(held[threadIdx.x], held[threadIdx.x + o]);
-  }
-  if (threadIdx.x == 0 && held[0]) atomicMax(top, held[0]);
-}
-__global__ __launch_bounds__(kThreads) void rows_kernel(skew_head_desc h, float c, const float *lse, const float *dloss, const float *dlse,
-                                                        const uint32_t *top, HeadRow *row) {
-  const int64_t t = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-  if (t >= h.tokens) return;
-  HeadRow r = {0.0f, 0.0f, 0.0f, -1};
-  if (is_token(h, t)) {
-    factors(h, dloss, dlse, t, &r.both, &r.one);
-    const int e = half_exponent(*top);
-    r.both = __builtin_ldexpf(r.both, -e);
-    r.one = __builtin_ldexpf(r.one, -e);
-    r.l2 = (float)((double)lse[t] * ((double)c / (double)h.scale));
-    r.target = (int32_t)id_at(h.targets, h.target_bytes, t);
-  }
-  row[t] = r;
-}
-
-__device__ __forceinline__ void store_half8(uint16_t *p, const float *v, const int *e) {
+// 8 bf16 values to float16 times 2^-e
+__device__ __forceinline__ u32x4 to_half8(u32x4 v, const int *e) {
   u32x4 u;
 #pragma unroll
   for (int i = 0; i < 4; i++) {
-    const uint16_t a = __builtin_bit_cast(uint16_t, (_Float16)__builtin_ldexpf(v[2 * i], -e[2 * i]));
-    const uint16_t b = __builtin_bit_cast(uint16_t, (_Float16)__builtin_ldexpf(v[2 * i + 1], -e[2 * i + 1]));
-    u[i] = a | (uint32_t)b << 16;
+    const float a = __builtin_ldexpf(__uint_as_float(v[i] << 16), -e[2 * i]);
+    const float b = __builtin_ldexpf(__uint_as_float(v[i] & 0xFFFF0000u), -e[2 * i + 1]);
+    u[i] = __builtin_bit_cast(uint16_t, (_Float16)a) | (uint32_t)__builtin_bit_cast(uint16_t, (_Float16)b) << 16;
   }
-  *reinterpret_cast<u32x4 *>(p) = u;
+  return u;
 }
 
 // Values to whole rows of whole chunks (rows8 x cols8, zeros past rows and cols): float16 beside their columns' powers of two (half),
-// and as they are (copy). Rows that are no token are zeros where h is given.
+// and as they are (copy). A thread takes one chunk of columns, whose powers it loads once, of kPadRows rows. With `masked` rows that
+// are no token are zeros, and the work-groups past those of x make the rows' HeadRow.
 struct Padded {
   const bf16_t *x;
   int64_t ld, rows, cols, rows8, cols8;
@@ -152,54 +177,75 @@ struct Padded {
   bf16_t *copy;
   const uint32_t *top;
   int masked;
+  int64_t groups;
 };
-__global__ __launch_bounds__(kThreads) void pad_kernel(Padded p, skew_head_desc h) {
-  const Chunks c(p.rows8, p.cols8 / 8, kThreads);
-  const Place at = c.at(0);
-  if (!at.there) return;
-  float v[8] = {};
-  if (at.row < p.rows && (!p.masked || is_token(h, at.row))) load8(p.x + at.row * p.ld + at.col, p.cols - at.col, v);
-  const int64_t to = at.row * p.cols8 + at.col;
-  if (p.half) {
-    int e[8];
-#pragma unroll
-    for (int q = 0; q < 8; q++) e[q] = half_exponent(at.col + q < p.cols ? p.top[at.col + q] : 0);
-    store_half8(p.half + to, v, e);
+constexpr int kPadRows = 8;
+__host__ __device__ inline int64_t pad_wide(int64_t cols8) { return cols8 / 8 < kThreads ? cols8 / 8 : kThreads; }   // chunks side by side
+__global__ __launch_bounds__(kThreads) void pad_kernel(Padded p, skew_head_desc h, Factors f) {
+  if (blockIdx.x >= p.groups) {
+    const int64_t t = (blockIdx.x - p.groups) * kThreads + threadIdx.x;
+    if (t >= h.tokens) return;
+    HeadRow r = {0.0f, 0.0f, 0.0f, -1};
+    if (is_token(h, t)) {
+      factors(h, f.dloss, f.dlse, t, &r.both, &r.one);
+      const int e = half_exponent(*f.top);
+      r.both = __builtin_ldexpf(r.both, -e);
+      r.one = __builtin_ldexpf(r.one, -e);
+      r.l2 = (float)((double)f.lse[t] * ((double)f.c / (double)h.scale));
+      r.target = (int32_t)id_at(h.targets, h.target_bytes, t);
+    }
+    f.row[t] = r;
+    return;
   }
-  if (p.copy) store8(p.copy + to, 8, v);
+  const uint32_t wide = (uint32_t)pad_wide(p.cols8), side = kThreads / wide, at = threadIdx.x / wide;
+  const int64_t strips = (p.cols8 / 8 + kThreads - 1) / kThreads, strip = blockIdx.x % strips;
+  const int64_t col = (strip * kThreads + threadIdx.x - at * wide) * 8, row0 = blockIdx.x / strips * (side * kPadRows) + at;
+  if (at >= side || col >= p.cols8) return;
+  u32x4 v[kPadRows];
+  bool token[kPadRows];
+#pragma unroll
+  for (int i = 0; i < kPadRows; i++) {
+    const int64_t row = row0 + (int64_t)i * side;
+    v[i] = load_chunk(p.x + row * p.ld + col, row < p.rows ? p.cols - col : 0);
+    token[i] = !p.masked || (row < p.rows && is_token(h, row));
+  }
+#pragma unroll
+  for (int i = 0; i < kPadRows; i++)
+    if (!token[i]) v[i] = u32x4{0, 0, 0, 0};
+  int e[8];
+#pragma unroll
+  for (int q = 0; q < 8; q++) e[q] = p.half && col + q < p.cols ? half_exponent(p.top[col + q]) : 0;
+#pragma unroll
+  for (int i = 0; i < kPadRows; i++) {
+    const int64_t row = row0 + (int64_t)i * side, to = row * p.cols8 + col;
+    if (row >= p.rows8) break;
+    if (p.half) *reinterpret_cast<u32x4 *>(p.half + to) = to_half8(v[i], e);
+    if (p.copy) *reinterpret_cast<u32x4 *>(p.copy + to) = v[i];
+  }
 }
 // The same beside the rows' powers of two, whose largest magnitudes it finds: a work-group a row.
 __global__ __launch_bounds__(kThreads) void pad_rows_kernel(Padded p, uint32_t *top) {
-  __shared__ uint32_t held[kThreads];
   const int64_t row = blockIdx.x;
   const bf16_t *x = p.x + row * p.ld;
+  const int64_t cols = row < p.rows ? p.cols : 0;
   uint32_t m = 0;
-  if (row < p.rows) {
 #pragma unroll 4
-    for (int64_t col = threadIdx.x * 8; col < p.cols; col += kThreads * 8) {
-      float v[8];
-      load8(x + col, p.cols - col, v);
+  for (int64_t col = threadIdx.x * 8; col < cols; col += kThreads * 8) {
+    float v[8];
+    load8(x + col, cols - col, v);
 #pragma unroll
-      for (int q = 0; q < 8; q++) m = max(m, finite_bits(v[q]));
-    }
+    for (int q = 0; q < 8; q++) m = max(m, finite_bits(v[q]));
   }
-  held[threadIdx.x] = m;
-  for (int o = kThreads / 2; o > 0; o >>= 1) {
-    __syncthreads();
-    if (threadIdx.x < o) held[threadIdx.x] = max(held[threadIdx.x], held[threadIdx.x + o]);
-  }
-  __syncthreads();
-  const uint32_t all = held[0];
-  if (threadIdx.x == 0) top[row] = all;
+  m = largest(m);
+  if (threadIdx.x == 0) top[row] = m;
   int e[8];
 #pragma unroll
-  for (int q = 0; q < 8; q++) e[q] = half_exponent(all);
+  for (int q = 0; q < 8; q++) e[q] = half_exponent(m);
 #pragma unroll 4
   for (int64_t col = threadIdx.x * 8; col < p.cols8; col += kThreads * 8) {
-    float v[8] = {};
-    if (row < p.rows) load8(x + col, p.cols - col, v);
-    store_half8(p.half + row * p.cols8 + col, v, e);
-    if (p.copy) store8(p.copy + row * p.cols8 + col, 8, v);
+    const u32x4 v = load_chunk(x + col, cols - col);
+    *reinterpret_cast<u32x4 *>(p.half + row * p.cols8 + col) = to_half8(v, e);
+    if (p.copy) *reinterpret_cast<u32x4 *>(p.copy + row * p.cols8 + col) = v;
   }
 }
 
@@ -221,7 +267,7 @@ HeadPlan head_plan(const skew_head_desc &h, bool backward) {
   p.d8 = up(h.d, 8);
   p.v8 = up(h.vocab, 8);
   p.x_as_is = chunks(h.x, h.ldx) && h.d % 8 == 0 && short_rows(kTileRows, h.ldx);
-  p.w_as_is = chunks(h.w, h.ldw) && h.d % 8 == 0 && h.vocab % 8 == 0 && short_rows(kTileRows, h.ldw);
+  p.w_as_is = chunks(h.w, h.ldw) && h.d % 8 == 0 && (tied(h) || h.vocab % 8 == 0) && short_rows(kTileRows, h.ldw);
   p.run = std::min(h.tokens, kRun);
   if (!backward && p.w_as_is) {
     p.piece = h.vocab;
@@ -242,30 +288,37 @@ const bf16_t *words(const skew_head_desc &h, int64_t v0) {
 }
 // x w of rows `rows` and the piece at v0 of `cols` words: from (a, lda) and w or its copy
 HeadProduct logits_of(const skew_head_desc &h, const HeadPlan &p, const void *a, int64_t lda, int64_t rows, int64_t v0, const void *copy) {
-  const int64_t cols = piece_cols(h, p, v0), cols8 = up(cols, 8);
+  const int64_t cols = piece_cols(h, p, v0), cols8 = tied(h) && !copy ? cols : up(cols, 8);   // (words in rows need no padding)
   HeadProduct q = {a, copy ? copy : words(h, v0), lda, copy ? (tied(h) ? p.d8 : cols8) : h.ldw, rows, cols, p.d8, 0, cols8};
   return q;
 }
 // (shapes alone)
 int mode_of(const skew_head_desc &h) { return tied(h) ? kBackward : kForward; }
 
-int launch_pad(const Padded &p, const skew_head_desc &h, hipStream_t s) {
-  const int64_t grid = (p.rows8 * (p.cols8 / 8) + kThreads - 1) / kThreads;
-  if (grid > 0x7FFFFFFF) return (int)hipErrorInvalidConfiguration;
-  pad_kernel<<<(unsigned)grid, kThreads, 0, s>>>(p, h);
+// f: also the rows of G (p.x are the tokens' rows)
+int launch_pad(Padded p, const skew_head_desc &h, const Factors *f, hipStream_t s) {
+  const int64_t strips = (p.cols8 / 8 + kThreads - 1) / kThreads, side = kThreads / pad_wide(p.cols8) * kPadRows;
+  p.groups = strips * ((p.rows8 + side - 1) / side);
+  const int64_t grid = p.groups + (f ? (h.tokens + kThreads - 1) / kThreads : 0);
+  if (grid > kMostGroups) return (int)hipErrorInvalidConfiguration;
+  pad_kernel<<<(unsigned)grid, kThreads, 0, s>>>(p, h, f ? *f : Factors{});
   return (int)hipGetLastError();
 }
 // the piece of w at v0, padded
 Padded piece_of(const skew_head_desc &h, const HeadPlan &p, int64_t v0, uint16_t *half, bf16_t *copy, const uint32_t *top) {
   const int64_t cols = piece_cols(h, p, v0), cols8 = up(cols, 8);
-  if (tied(h)) return {words(h, v0), h.ldw, cols, h.d, cols8, p.d8, half, copy, top, 0};
-  return {words(h, v0), h.ldw, h.d, cols, p.d8, cols8, half, copy, top, 0};
+  if (tied(h)) return {words(h, v0), h.ldw, cols, h.d, cols8, p.d8, half, copy, top, 0, 0};
+  return {words(h, v0), h.ldw, h.d, cols, p.d8, cols8, half, copy, top, 0, 0};
 }
-int launch_column_top(const bf16_t *x, int64_t ld, int64_t rows, int64_t cols, const skew_head_desc &h, bool masked, uint32_t *top,
-                      hipStream_t s) {
-  const int64_t grid = ((cols + 255) / 256) * ((rows + kTopRows - 1) / kTopRows);
-  if (grid > 0x7FFFFFFF) return (int)hipErrorInvalidConfiguration;
-  column_top_kernel<<<(unsigned)grid, kThreads, 0, s>>>(x, ld, rows, cols, h, masked, top);
+// f: also the largest of G's factors
+int launch_tops(const bf16_t *x, int64_t ld, int64_t rows, int64_t cols, uint32_t *top, const skew_head_desc &h, const Factors *f,
+                hipStream_t s) {
+  const int64_t strips = (cols + 255) / 256;
+  const int each = strips * ((rows + 127) / 128) >= 512 ? 16 : 4;   // rows of a thread
+  Tops p = {x, ld, rows, cols, top, each, f != nullptr, strips * ((rows + 8 * each - 1) / (8 * each))};
+  const int64_t more = f ? std::min((h.tokens + kThreads - 1) / kThreads, (int64_t)64) : 0;
+  if (p.groups + more > kMostGroups) return (int)hipErrorInvalidConfiguration;
+  top_kernel<<<(unsigned)(p.groups + more), kThreads, 0, s>>>(p, h, f ? *f : Factors{});
   return (int)hipGetLastError();
 }
 
@@ -290,10 +343,12 @@ struct ForwardPlan : HeadPlan {
 ForwardPlan forward_plan(const skew_head_desc &h) {
   ForwardPlan f;
   static_cast<HeadPlan &>(f) = head_plan(h, false);
-  f.few = h.tokens <= kFewRows;
+  // One row and words at odd positions, in pieces copied for the tiles | as they are (us): width 2048, 8001 words 34 | 46, 16001 47 | 44,
+  // 24001 59 | 52, 50257 117 | 77; width 512, 50257 36 | 26; width 4096, 16001 79 | 78.
+  f.few = !f.w_as_is && !tied(h) && h.tokens <= kFewRows && h.vocab >= 16384 && (h.d == 1 || short_rows(kTileRows, h.ldw));
   if (f.few) f.x_as_is = f.w_as_is = true;   // (whatever their alignment)
   // rows of the last run may be fewer, and their tiles narrower
-  f.part_ld = f.few ? head_few_parts(mode_of(h), whole_of(h)) : 0;
+  f.part_ld = f.few ? head_few_parts(h.vocab) : 0;
   const int64_t last = h.tokens % f.run ? h.tokens % f.run : f.run;
   for (const int64_t rows : {f.run, last}) {
     if (f.few) break;
@@ -359,7 +414,7 @@ size_t head_backward_scratch(const skew_head_desc &h) { return backward_plan(h).
 
 int launch_fill_zero(void *dw, int64_t rows, int64_t cols, int64_t ld, void *stream) {
   const int64_t grid = (rows * ((cols + 7) / 8) + kThreads - 1) / kThreads;
-  if (grid > 0x7FFFFFFF) return (int)hipErrorInvalidConfiguration;
+  if (grid > kMostGroups) return (int)hipErrorInvalidConfiguration;
   fill_zero_kernel<<<(unsigned)grid, kThreads, 0, static_cast<hipStream_t>(stream)>>>(static_cast<bf16_t *>(dw), rows, cols, ld);
   return (int)hipGetLastError();
 }
@@ -378,9 +433,8 @@ int launch_head_loss(const skew_head_desc &h, float *loss, float *lse, char *ws,
   float *sum = reinterpret_cast<float *>(ws + f.sum);
   bf16_t *x_copy = reinterpret_cast<bf16_t *>(ws + f.x), *w_copy = reinterpret_cast<bf16_t *>(ws + f.w);
   if (f.few) {
-    TRY(launch_head_few(mode_of(h), whole_of(h), {c, h.targets, h.target_bytes, h.vocab, 0, part, f.part_ld, 0, sum}, stream));
-    loss_kernel<<<(unsigned)((h.tokens + 3) / 4), kThreads, 0, s>>>(h, c, part, f.part_ld, (int)f.part_ld, sum, loss, lse);
-    return (int)hipGetLastError();
+    TRY(launch_head_few(whole_of(h), {c, h.targets, h.target_bytes, h.vocab, 0, part, f.part_ld, 0, sum}, stream));
+    return launch_loss(h, c, part, f.part_ld, (int)f.part_ld, sum, loss, lse, s);
   }
   for (int64_t t0 = 0; t0 < h.tokens; t0 += f.run) {
     skew_head_desc r = h;   // this run's rows
@@ -388,16 +442,15 @@ int launch_head_loss(const skew_head_desc &h, float *loss, float *lse, char *ws,
     r.x = static_cast<const bf16_t *>(h.x) + t0 * h.ldx;
     r.targets = static_cast<const char *>(h.targets) + t0 * h.target_bytes;
     if (!f.x_as_is)
-      TRY(launch_pad({static_cast<const bf16_t *>(r.x), h.ldx, r.tokens, h.d, r.tokens, f.d8, nullptr, x_copy, nullptr, 0}, r, s));
+      TRY(launch_pad({static_cast<const bf16_t *>(r.x), h.ldx, r.tokens, h.d, r.tokens, f.d8, nullptr, x_copy, nullptr, 0, 0}, r, nullptr, s));
     int64_t at = 0;
     for (int64_t v0 = 0; v0 < h.vocab; v0 += f.piece) {
-      if (!f.w_as_is) TRY(launch_pad(piece_of(h, f, v0, nullptr, w_copy, nullptr), r, s));
+      if (!f.w_as_is) TRY(launch_pad(piece_of(h, f, v0, nullptr, w_copy, nullptr), r, nullptr, s));
       const HeadProduct p = logits_of(h, f, f.x_as_is ? r.x : x_copy, f.x_as_is ? h.ldx : f.d8, r.tokens, v0, f.w_as_is ? nullptr : w_copy);
       TRY(launch_head_forward(mode_of(h), p, {c, r.targets, h.target_bytes, h.vocab, v0, part, f.part_ld, at, sum}, stream));
       at += head_parts(mode_of(h), p);
     }
-    loss_kernel<<<(unsigned)((r.tokens + 3) / 4), kThreads, 0, s>>>(r, c, part, f.part_ld, (int)at, sum, loss + t0, lse + t0);
-    TRY((int)hipGetLastError());
+    TRY(launch_loss(r, c, part, f.part_ld, (int)at, sum, loss + t0, lse + t0, s));
   }
   return (int)hipSuccess;
 }
@@ -417,13 +470,9 @@ int launch_head_loss_backward(const skew_head_desc &h, const float *lse, const f
   const int tops = (int)(1 + 2 * b.d8);
   zero_kernel<<<(tops + kThreads - 1) / kThreads, kThreads, 0, s>>>(coef, tops);
   TRY((int)hipGetLastError());
-  TRY(launch_column_top(x, h.ldx, h.tokens, h.d, h, true, x_top, s));
-  const int64_t groups = (h.tokens + kThreads - 1) / kThreads;
-  factor_top_kernel<<<(unsigned)std::min(groups, (int64_t)64), kThreads, 0, s>>>(h, dloss, dlse, coef);
-  TRY((int)hipGetLastError());
-  rows_kernel<<<(unsigned)groups, kThreads, 0, s>>>(h, c, lse, dloss, dlse, coef, row);
-  TRY((int)hipGetLastError());
-  TRY(launch_pad({x, h.ldx, h.tokens, h.d, h.tokens, b.d8, x16, x_copy, x_top, 1}, h, s));
+  const Factors factors = {lse, dloss, dlse, coef, row, c};
+  TRY(launch_tops(x, h.ldx, h.tokens, h.d, x_top, h, &factors, s));
+  TRY(launch_pad({x, h.ldx, h.tokens, h.d, h.tokens, b.d8, x16, x_copy, x_top, 1, 0}, h, &factors, s));
   for (int64_t v0 = 0; v0 < h.vocab; v0 += b.piece) {
     const Padded p = piece_of(h, b, v0, w16, w_copy, w_top);
     const bool first = v0 == 0, last = v0 + b.piece >= h.vocab;
@@ -432,8 +481,8 @@ int launch_head_loss_backward(const skew_head_desc &h, const float *lse, const f
         zero_kernel<<<(unsigned)((b.d8 + kThreads - 1) / kThreads), kThreads, 0, s>>>(w_top, (int)b.d8);
         TRY((int)hipGetLastError());
       }
-      TRY(launch_column_top(p.x, p.ld, p.rows, p.cols, h, false, w_top, s));
-      TRY(launch_pad(p, h, s));
+      TRY(launch_tops(p.x, p.ld, p.rows, p.cols, w_top, h, nullptr, s));
+      TRY(launch_pad(p, h, nullptr, s));
     } else {
       pad_rows_kernel<<<(unsigned)p.rows8, kThreads, 0, s>>>(p, w_top);
       TRY((int)hipGetLastError());

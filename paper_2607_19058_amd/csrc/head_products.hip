@@ -92,10 +92,15 @@ __global__ __launch_bounds__(256) void join_kernel(HeadResult r, int64_t rows, i
   const Place p = c.at(0);
   if (!p.there) return;
   float v[8] = {};
+#pragma unroll 4
   for (int i = 0; i < parts; i++) {
-    const float *y = part + ((int64_t)i * rows + p.row) * ld + p.col;
+    const f32x4 *y = reinterpret_cast<const f32x4 *>(part + ((int64_t)i * rows + p.row) * ld + p.col);
+    const f32x4 lo = y[0], hi = y[1];
 #pragma unroll
-    for (int q = 0; q < 8; q++) v[q] += y[q];
+    for (int q = 0; q < 4; q++) {
+      v[q] += lo[q];
+      v[4 + q] += hi[q];
+    }
   }
   const int64_t n = cols - p.col;
   const int coef = half_exponent(*r.coef);

@@ -147,6 +147,19 @@ __device__ __forceinline__ void store8(float *p, int64_t n, const float *v) {
   }
 }
 
+// 8 values at p, of which the first n exist (n <= 0: none)
+__device__ __forceinline__ u32x4 load_chunk(const bf16_t *p, int64_t n) {
+  u32x4 u = {0, 0, 0, 0};
+  if (n >= 8) {
+    u = *reinterpret_cast<const u32x4_a2 *>(p);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 7; i++)
+      if (i < n) u[i >> 1] |= (uint32_t)p[i].v << (16 * (i & 1));
+  }
+  return u;
+}
+
 // One 16-byte access: kVec neighbouring values; n < kVec: only the first n exist.
 template <class T>
 constexpr int kVec = 16 / sizeof(T);

@@ -115,19 +115,6 @@ struct FragT {
   }
 };
 
-// 8 values at p, of which the first n exist (n <= 0: none)
-__device__ __forceinline__ u32x4 load_chunk(const bf16_t *p, int64_t n) {
-  u32x4 u = {0, 0, 0, 0};
-  if (n >= 8) {
-    u = *reinterpret_cast<const u32x4_a2 *>(p);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 7; i++)
-      if (i < n) u[i >> 1] |= (uint32_t)p[i].v << (16 * (i & 1));
-  }
-  return u;
-}
-
 // 16 bytes a lane from global memory (a scalar base and the lane's byte offset) to LDS: lane i of the wave to byte
 // `to` + 16 i of LDS (`to` the same in every lane).
 // Written out because the compiler, which cannot tell the stage buffers apart, would wait for these loads

@@ -51,7 +51,8 @@ def check(x, w, targets, dloss, dlse, tied, scale=1.0, dtype=None, ref=None):
 
 
 SMALL = [(1, 1, 1), (1, 8, 8), (1, 64, 1000), (2, 3, 2), (3, 33, 17), (5, 40, 129), (64, 64, 64), (65, 128, 300), (70, 31, 257),
-         (130, 256, 512), (257, 40, 1001), (300, 130, 777), (31, 2048, 96), (40, 2000, 264), (1, 1031, 4100)]
+         (130, 256, 512), (257, 40, 1001), (300, 130, 777), (31, 2048, 96), (40, 2000, 264), (1, 1031, 4100),
+         (1, 1, 16385), (1, 2048, 16401), (2, 33, 17001), (16, 100, 20003), (17, 100, 20003), (9, 523, 16388)]
 
 
 @pytest.mark.parametrize("tied", [False, True])
