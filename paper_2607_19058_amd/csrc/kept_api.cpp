@@ -14,6 +14,7 @@ int64_t blocks_of(int64_t cols) { return (cols + SKEW_KEPT_BLOCK - 1) / SKEW_KEP
 bool kept_ok(int64_t rows, int64_t cols) {
   return rows >= 0 && cols_ok(cols) && rows <= kMaxPlaces / blocks_of(cols);
 }
+constexpr int64_t kTileRows = 256;   // rows that a lane's 32-bit offset spans
 bool codes_ok(const int8_t *codes, const uint8_t *scales) {
   return codes != nullptr && scales != nullptr && ((uintptr_t)codes & 15) == 0;
 }
@@ -29,17 +30,28 @@ bool grad_kept_ok(const skew_rows *r, const skew_product_desc *p) {
   q.ldx = 32 * blocks_of(p->n);
   if (!product_ok(r, &q, true)) return false;
   const int64_t places = r->tokens * r->k;
-  return kept_ok(p->flags & SKEW_GATHER ? r->tokens : places, p->n) && (p->out_dtype == SKEW_BF16 || places <= kMaxPlaces / 2);
+  return kept_ok(places, p->n) && (p->out_dtype == SKEW_BF16 || places <= kMaxPlaces / 2);
 }
-// the restored rows, and what the product needs behind them
-size_t restored_bytes(const skew_rows *r, const skew_product_desc *p) {
-  return pad256((size_t)(p->flags & SKEW_GATHER ? r->tokens : r->tokens * r->k) * blocks_of(p->n) * 64);
-}
-skew_product_desc restored(const skew_product_desc *p, void *workspace) {
-  skew_product_desc q = *p;
-  q.x = workspace;
-  q.ldx = 32 * blocks_of(p->n);
-  return q;
+// The workspace: restored rows (bf16 d: one a place; float32: those that are kept, as the product of a float32 d looks them up), then what
+// the product needs, or rows of d where theirs do not begin at 16-byte positions.
+struct KeptPlan {
+  int64_t rows, ldx, ldd;   // ldd 0: d as it is
+  size_t rest, bytes;
+};
+KeptPlan kept_plan(const skew_rows *r, const skew_product_desc *p) {
+  const int64_t places = r->tokens * r->k, kept = p->flags & SKEW_GATHER ? r->tokens : places;
+  KeptPlan k = {p->out_dtype == SKEW_F32 ? kept : places, 32 * blocks_of(p->n), 0, 0, 0};
+  k.rest = pad256((size_t)k.rows * k.ldx * 2);
+  if (p->out_dtype == SKEW_F32) {
+    skew_product_desc q = *p;
+    q.ldx = k.ldx;
+    k.bytes = k.rest + product_grad_f32_scratch(*r, q);
+  } else {
+    const bool as_is = ((uintptr_t)p->y & 15) == 0 && p->ldy % 8 == 0 && p->m % 8 == 0 && short_rows(kTileRows, p->ldy);
+    if (!as_is) k.ldd = (p->m + 7) / 8 * 8;
+    k.bytes = k.rest + (size_t)places * k.ldd * 2;
+  }
+  return k;
 }
 
 }  // namespace
@@ -83,27 +95,34 @@ int skew_expert_act_backward(const skew_act_desc *d, void *stream) {
 
 int skew_expert_matmul_grad_kept_bytes(const skew_rows *r, const skew_product_desc *p, size_t *bytes) {
   if (!grad_kept_ok(r, p) || bytes == nullptr) return SKEW_EINVAL;
-  *bytes = 0;
-  if (r->tokens > 0)
-    *bytes = restored_bytes(r, p) + (p->out_dtype == SKEW_F32 ? product_grad_f32_scratch(*r, restored(p, nullptr)) : 0);
+  *bytes = r->tokens > 0 ? kept_plan(r, p).bytes : 0;
   return SKEW_OK;
 }
 
 int skew_expert_matmul_grad_kept(const skew_rows *r, const skew_product_desc *p, const int8_t *codes, const uint8_t *scales,
                                  void *workspace, size_t workspace_bytes, void *stream) {
-  size_t need;
-  if (skew_expert_matmul_grad_kept_bytes(r, p, &need) != SKEW_OK || p->w == nullptr) return SKEW_EINVAL;
+  if (!grad_kept_ok(r, p) || p->w == nullptr) return SKEW_EINVAL;
   if (r->tokens == 0) return status(launch_product_grad(*r, *p, stream));   // (nothing but dW is touched)
   if (p->y == nullptr || !codes_ok(codes, scales)) return SKEW_EINVAL;
-  if (workspace_bytes < need) return SKEW_ENOSPACE;
+  const KeptPlan k = kept_plan(r, p);
+  if (workspace_bytes < k.bytes) return SKEW_ENOSPACE;
   if (workspace == nullptr) return SKEW_EINVAL;
-  const int64_t rows = p->flags & SKEW_GATHER ? r->tokens : r->tokens * r->k;
-  const skew_product_desc q = restored(p, workspace);
+  const bool gather = (p->flags & SKEW_GATHER) != 0;
+  char *rest = static_cast<char *>(workspace) + k.rest;
   // whole blocks: the columns past a row's end are 0, as their codes are
-  const int e = launch_restore8(codes, scales, rows, q.ldx, workspace, SKEW_BF16, q.ldx, stream);
+  int e = gather && p->out_dtype == SKEW_BF16
+              ? launch_restore_places(*r, codes, scales, k.ldx, workspace, k.ldx, stream)
+              : launch_restore8(codes, scales, k.rows, k.ldx, workspace, SKEW_BF16, k.ldx, stream);
   if (e != (int)hipSuccess) return SKEW_EHIP;
-  char *rest = static_cast<char *>(workspace) + restored_bytes(r, p);
-  return status(p->out_dtype == SKEW_F32 ? launch_product_grad_f32(*r, q, rest, stream) : launch_product_grad(*r, q, stream));
+  if (p->out_dtype == SKEW_F32) {
+    skew_product_desc q = *p;
+    q.x = workspace;
+    q.ldx = k.ldx;
+    return status(launch_product_grad_f32(*r, q, rest, stream));
+  }
+  if (k.ldd > 0) e = launch_copy_rows(p->y, r->tokens * r->k, p->m, p->ldy, rest, k.ldd, stream);
+  if (e != (int)hipSuccess) return SKEW_EHIP;
+  return status(launch_grad_rows(*r, *p, workspace, k.ldx, k.ldd > 0 ? rest : p->y, k.ldd > 0 ? k.ldd : p->ldy, stream));
 }
 
 }  // extern "C"

@@ -114,6 +114,41 @@ __global__ __launch_bounds__(kThreads) void restore_kernel(const int8_t *codes, 
   }
 }
 
+__global__ __launch_bounds__(kThreads) void restore_places_kernel(const int8_t *codes, const uint8_t *scales, int64_t cols, bf16_t *x,
+                                                                  int64_t ldx, const int32_t *rows, int64_t places, int32_t k) {
+  const Chunks c(places, chunks_of(cols), kTile);
+  Place p[kUnroll];
+  KeptChunk v[kUnroll];
+#pragma unroll
+  for (int i = 0; i < kUnroll; i++) {
+    p[i] = c.at(i);
+    const int32_t pair = p[i].there ? rows[p[i].row] : -1;
+    p[i].there = pair >= 0;
+    if (p[i].there) v[i] = get_kept(c, {pair / k, p[i].col, true}, codes, scales);
+  }
+#pragma unroll
+  for (int i = 0; i < kUnroll; i++) {
+    if (!p[i].there) continue;
+    float o[8];
+    restore(v[i].codes, v[i].b, o);
+    store8(x + p[i].row * ldx + p[i].col, 8, o);
+  }
+}
+
+__global__ __launch_bounds__(kThreads) void copy_rows_kernel(const bf16_t *x, int64_t rows, int64_t cols, int64_t ldx, bf16_t *y, int64_t ldy) {
+  const Chunks c(rows, ldy / 8, kTile);
+  Place p[kUnroll];
+  u32x4 v[kUnroll];
+#pragma unroll
+  for (int i = 0; i < kUnroll; i++) {
+    p[i] = c.at(i);
+    v[i] = load_chunk(x + p[i].row * ldx + p[i].col, p[i].there ? cols - p[i].col : 0);
+  }
+#pragma unroll
+  for (int i = 0; i < kUnroll; i++)
+    if (p[i].there) *reinterpret_cast<u32x4 *>(y + p[i].row * ldy + p[i].col) = v[i];
+}
+
 // f(g) and f'(g). s = 1 / (1 + exp(-y)) and 1 - s from exp(-|y|), so that neither cancels.
 template <int KIND>
 __device__ __forceinline__ void act(float g, float *f, float *df) {
@@ -256,6 +291,19 @@ int launch_restore8(const int8_t *codes, const uint8_t *scales, int64_t rows, in
   hipStream_t s = static_cast<hipStream_t>(stream);
   if (dtype == SKEW_BF16) restore_kernel<<<grid, kThreads, 0, s>>>(codes, scales, rows, cols, static_cast<bf16_t *>(x), ldx);
   else restore_kernel<<<grid, kThreads, 0, s>>>(codes, scales, rows, cols, static_cast<float *>(x), ldx);
+  return (int)hipGetLastError();
+}
+
+int launch_restore_places(const skew_rows &r, const int8_t *codes, const uint8_t *scales, int64_t cols, void *x, int64_t ldx, void *stream) {
+  const int64_t places = r.tokens * r.k;
+  restore_places_kernel<<<(unsigned)groups(places, cols), kThreads, 0, static_cast<hipStream_t>(stream)>>>(
+      codes, scales, cols, static_cast<bf16_t *>(x), ldx, r.rows, places, r.k);
+  return (int)hipGetLastError();
+}
+
+int launch_copy_rows(const void *x, int64_t rows, int64_t cols, int64_t ldx, void *y, int64_t ldy, void *stream) {
+  copy_rows_kernel<<<(unsigned)((rows * (ldy / 8) + kTile - 1) / kTile), kThreads, 0, static_cast<hipStream_t>(stream)>>>(
+      static_cast<const bf16_t *>(x), rows, cols, ldx, static_cast<bf16_t *>(y), ldy);
   return (int)hipGetLastError();
 }
 

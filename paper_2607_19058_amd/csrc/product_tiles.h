@@ -19,7 +19,7 @@ namespace {
 //   kForward   a in the contraction, b along the result
 //   kBackward  both in the contraction
 //   kWeights   both along the result; the contraction is an expert's places, and a's rows are looked up
-//   kOuter     both along the result; the contraction is the rows of both
+//   kOuter     both along the result; the contraction is the rows of both, from Tile::first on
 enum { kForward = 0, kBackward = 1, kWeights = 2, kOuter = 3 };
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
@@ -176,6 +176,9 @@ __device__ __forceinline__ bool patch_tile(bool in_patches, uint32_t rows, uint3
 // in their L2s.
 constexpr int kRound = kDies * kPatchR * kPatchC;
 __host__ __device__ inline int64_t plain_grid(int64_t total) { return total / kRound * kRound + (total % kRound + kDies - 1) / kDies * kDies; }
+// BANDS: bands of kPatchR rows, column by column, instead of strips: for results that are most of the bytes, whose rows the dies then write
+// side by side (32 experts' weights' gradient of 2048 x 8192: 684 us, in strips 839).
+template <bool BANDS = false>
 __device__ __forceinline__ bool plain_tile(uint32_t rows, uint32_t cols, uint32_t parts, uint32_t *row, uint32_t *col, uint32_t *part) {
   const uint32_t total = rows * cols * parts, whole = total / kRound * kRound;   // (below 2^31)
   const uint32_t die = blockIdx.x % kDies, i = blockIdx.x / kDies;
@@ -189,10 +192,13 @@ __device__ __forceinline__ bool plain_tile(uint32_t rows, uint32_t cols, uint32_
   }
   *part = at / (rows * cols);
   at -= *part * (rows * cols);
-  const uint32_t strip = at / (rows * kPatchC), width = cols - strip * kPatchC < kPatchC ? cols - strip * kPatchC : kPatchC;
-  at -= strip * rows * kPatchC;
-  *row = at / width;
-  *col = strip * kPatchC + at - *row * width;
+  const uint32_t along = BANDS ? cols : rows, across = BANDS ? rows : cols;
+  constexpr uint32_t kWide = BANDS ? kPatchR : kPatchC;
+  const uint32_t strip = at / (along * kWide), width = across - strip * kWide < kWide ? across - strip * kWide : kWide;
+  at -= strip * along * kWide;
+  const uint32_t a = at / width, b = strip * kWide + at - a * width;
+  *row = BANDS ? b : a;
+  *col = BANDS ? a : b;
   return true;
 }
 
@@ -318,6 +324,8 @@ __device__ __forceinline__ void tile_body(ProductArgs a, const Op &op) {
   if (MODE == kWeights) {
     xb += 2 * t.first * a.ldw;
   } else if (MODE == kOuter) {
+    xa += 2 * t.first * a.ldx;
+    xb += 2 * t.first * a.ldw;
     step_a = 2 * BK * a.ldx;
   } else {
     xb += 2 * (int64_t)(K ? t.expert : 0) * a.slice;
