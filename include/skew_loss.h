@@ -26,8 +26,9 @@ extern "C" {
  * Gradients, from those of loss (dloss) and lse (dlse; NULL: 0), G being that of the logits:
  *   G_tv = scale ((dloss_t + dlse_t) exp(z_tv - lse_t) - dloss_t [v = y_t]);   dx = G w^T;   dw = x^T G
  * computed in pieces of the vocabulary: G and the operand beside it are float16 numbers (11 bits, 8 times finer than bf16) times powers
- * of two: of G the largest coefficient's, of x and w their columns' d largest values', so that an entry smaller than its column's
- * largest by 2^29 or more keeps fewer bits, and one smaller by 2^40 none. dx and dw are rounded once more.
+ * of two: of G's rows, by their tokens' larger factor, and of the columns of x and w (their d), by their largest values. So an entry
+ * of G below 2^-28 of its row's factor, or one of x or w below 2^-29 of its column's largest, keeps fewer bits, down to none 11 powers
+ * further (for dw, of x times its token's factor). dx and dw are rounded once more.
  * NaN and infinities in x and w give NaN where they reach; a logit of +inf gives NaN.
  *   x      bf16 [tokens x d], row stride ldx;  0 <= tokens <= SKEW_MAX_LOSS_TOKENS;  1 <= d <= SKEW_MAX_HEAD_WIDTH
  *   w      bf16: column v of [d x vocab] is word v; with SKEW_TRANSPOSE row v of [vocab x d], as an embedding's

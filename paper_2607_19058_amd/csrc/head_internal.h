@@ -7,7 +7,7 @@
 namespace moe {
 
 // A token as the gradients' kernels take it: the base-2 exponent of its sum, the logits' gradient's factors times the power
-// of two that G is kept with, and its target (-1: no token).
+// of two that its row of G is kept with, and its target (-1: no token).
 struct HeadRow {
   float l2, both, one;
   int32_t target;
@@ -77,16 +77,18 @@ struct HeadGrad {
 };
 int launch_head_grad(int mode, const HeadProduct &p, const HeadGrad &g, void *stream);
 
-// result = 2^e (a b) + prev, of float16 operands. e is minus an exponent that G is kept with, plus those that the rows or columns of the other
-// operand are kept with (top: bits of their largest magnitudes).
+// result = 2^e (a b) + prev, of float16 operands. e is the sum of the exponents that they are kept with: of the result's rows or columns (top:
+// bits of their largest magnitudes), and of G: of each row (row_exponent), or the largest of all (coef), which the rows of x then make up for.
 struct HeadResult {
   void *y;
   int64_t ldy;
   int32_t y_dtype;
   const float *prev;          // NULL, or float [rows x ldprev] that is added
   int64_t ldprev;
-  const uint32_t *top, *coef; // per column, or per row; of G's coefficients
+  const uint32_t *top;        // per column, or per row
   int32_t by_row;
+  const int32_t *row_exponent;   // NULL: *coef
+  const uint32_t *coef;
 };
 size_t head_result_scratch(int mode, const HeadProduct &p);
 int launch_head_result(int mode, const HeadProduct &p, const HeadResult &r, char *ws, void *stream);
@@ -95,6 +97,8 @@ int launch_head_result(int mode, const HeadProduct &p, const HeadResult &r, char
 // that the largest lies in [2^14, 2^15).
 constexpr int kHalfTop = 14;
 __host__ __device__ inline int half_exponent(uint32_t top) { return (int)(top >> 23) - 127 - kHalfTop; }
+// The same of a row of G, from its larger factor: an entry is at most twice it.
+__host__ __device__ inline int factor_exponent(uint32_t top) { return half_exponent(top) + 1; }
 
 // The calls of skew_loss.h, after their checks.
 size_t head_forward_scratch(const skew_head_desc &h);

@@ -94,10 +94,17 @@ __device__ __forceinline__ void factors(const skew_head_desc &h, const float *dl
 }
 struct Factors {
   const float *lse, *dloss, *dlse;
-  uint32_t *top;    // bits of their largest sum
+  uint32_t *top;    // bits of the largest
   HeadRow *row;
+  int32_t *exponent;   // of each row of G
   float c;
 };
+// the larger of a token's, as bits
+__device__ __forceinline__ uint32_t factor_bits(const skew_head_desc &h, const Factors &f, int64_t t) {
+  float both, one;
+  factors(h, f.dloss, f.dlse, t, &both, &one);
+  return max(finite_bits(both), finite_bits(one));
+}
 
 // The largest m of a work-group's threads, in every one of them.
 __device__ __forceinline__ uint32_t largest(uint32_t m) {
@@ -123,11 +130,7 @@ __global__ __launch_bounds__(kThreads) void top_kernel(Tops p, skew_head_desc h,
     uint32_t m = 0;
     const int64_t step = (int64_t)(gridDim.x - p.groups) * kThreads;
     for (int64_t t = (blockIdx.x - p.groups) * kThreads + threadIdx.x; t < h.tokens; t += step)
-      if (is_token(h, t)) {
-        float both, one;
-        factors(h, f.dloss, f.dlse, t, &both, &one);
-        m = max(m, finite_bits(fabsf(both) + fabsf(one)));
-      }
+      if (is_token(h, t)) m = max(m, factor_bits(h, f, t));
     m = largest(m);
     if (threadIdx.x == 0 && m) atomicMax(f.top, m);
     return;
@@ -155,13 +158,13 @@ __global__ __launch_bounds__(kThreads) void top_kernel(Tops p, skew_head_desc h,
   if (strip * 256 + c < p.cols && all) atomicMax(p.top + strip * 256 + c, all);   // (an old value looked up first: 37 -> 66 us for 103 M values)
 }
 
-// 8 bf16 values to float16 times 2^-e
-__device__ __forceinline__ u32x4 to_half8(u32x4 v, const int *e) {
+// 8 bf16 values to float16 times 2^-(e + more)
+__device__ __forceinline__ u32x4 to_half8(u32x4 v, const int *e, int more) {
   u32x4 u;
 #pragma unroll
   for (int i = 0; i < 4; i++) {
-    const float a = __builtin_ldexpf(__uint_as_float(v[i] << 16), -e[2 * i]);
-    const float b = __builtin_ldexpf(__uint_as_float(v[i] & 0xFFFF0000u), -e[2 * i + 1]);
+    const float a = __builtin_ldexpf(__uint_as_float(v[i] << 16), -e[2 * i] - more);
+    const float b = __builtin_ldexpf(__uint_as_float(v[i] & 0xFFFF0000u), -e[2 * i + 1] - more);
     u[i] = __builtin_bit_cast(uint16_t, (_Float16)a) | (uint32_t)__builtin_bit_cast(uint16_t, (_Float16)b) << 16;
   }
   return u;
@@ -186,15 +189,17 @@ __global__ __launch_bounds__(kThreads) void pad_kernel(Padded p, skew_head_desc 
     const int64_t t = (blockIdx.x - p.groups) * kThreads + threadIdx.x;
     if (t >= h.tokens) return;
     HeadRow r = {0.0f, 0.0f, 0.0f, -1};
+    int e = 0;
     if (is_token(h, t)) {
       factors(h, f.dloss, f.dlse, t, &r.both, &r.one);
-      const int e = half_exponent(*f.top);
+      e = factor_exponent(factor_bits(h, f, t));
       r.both = __builtin_ldexpf(r.both, -e);
       r.one = __builtin_ldexpf(r.one, -e);
       r.l2 = (float)((double)f.lse[t] * ((double)f.c / (double)h.scale));
       r.target = (int32_t)id_at(h.targets, h.target_bytes, t);
     }
     f.row[t] = r;
+    f.exponent[t] = e;
     return;
   }
   const uint32_t wide = (uint32_t)pad_wide(p.cols8), side = kThreads / wide, at = threadIdx.x / wide;
@@ -212,14 +217,19 @@ __global__ __launch_bounds__(kThreads) void pad_kernel(Padded p, skew_head_desc 
 #pragma unroll
   for (int i = 0; i < kPadRows; i++)
     if (!token[i]) v[i] = u32x4{0, 0, 0, 0};
-  int e[8];
+  int e[8], less[kPadRows];   // of the columns; how much less than the largest row of G a token's row is
 #pragma unroll
   for (int q = 0; q < 8; q++) e[q] = p.half && col + q < p.cols ? half_exponent(p.top[col + q]) : 0;
 #pragma unroll
   for (int i = 0; i < kPadRows; i++) {
+    less[i] = 0;
+    if (p.half && p.masked && token[i]) less[i] = factor_exponent(*f.top) - factor_exponent(factor_bits(h, f, row0 + (int64_t)i * side));
+  }
+#pragma unroll
+  for (int i = 0; i < kPadRows; i++) {
     const int64_t row = row0 + (int64_t)i * side, to = row * p.cols8 + col;
     if (row >= p.rows8) break;
-    if (p.half) *reinterpret_cast<u32x4 *>(p.half + to) = to_half8(v[i], e);
+    if (p.half) *reinterpret_cast<u32x4 *>(p.half + to) = to_half8(v[i], e, less[i]);
     if (p.copy) *reinterpret_cast<u32x4 *>(p.copy + to) = v[i];
   }
 }
@@ -244,7 +254,7 @@ __global__ __launch_bounds__(kThreads) void pad_rows_kernel(Padded p, uint32_t *
 #pragma unroll 4
   for (int64_t col = threadIdx.x * 8; col < p.cols8; col += kThreads * 8) {
     const u32x4 v = load_chunk(x + col, cols - col);
-    *reinterpret_cast<u32x4 *>(p.half + row * p.cols8 + col) = to_half8(v, e);
+    *reinterpret_cast<u32x4 *>(p.half + row * p.cols8 + col) = to_half8(v, e, 0);
     if (p.copy) *reinterpret_cast<u32x4 *>(p.copy + row * p.cols8 + col) = v;
   }
 }
@@ -366,7 +376,7 @@ ForwardPlan forward_plan(const skew_head_desc &h) {
 }
 
 struct BackwardPlan : HeadPlan {
-  size_t tops, row, x16, x, w16, w, g, dx, rest, bytes;
+  size_t tops, row, exponent, x16, x, w16, w, g, dx, rest, bytes;
   int64_t ldg;
 };
 // the three products of a piece
@@ -389,6 +399,7 @@ BackwardPlan backward_plan(const skew_head_desc &h) {
   Regions r;
   b.tops = r.take((size_t)(1 + 2 * b.d8) * 4);   // of G's factors, of x's columns, of w's
   b.row = r.take((size_t)h.tokens * sizeof(HeadRow));
+  b.exponent = r.take((size_t)h.tokens * 4);
   b.x16 = r.take(x);
   b.x = b.x_as_is ? 0 : r.take(x);
   b.w16 = r.take(w);
@@ -470,7 +481,8 @@ int launch_head_loss_backward(const skew_head_desc &h, const float *lse, const f
   const int tops = (int)(1 + 2 * b.d8);
   zero_kernel<<<(tops + kThreads - 1) / kThreads, kThreads, 0, s>>>(coef, tops);
   TRY((int)hipGetLastError());
-  const Factors factors = {lse, dloss, dlse, coef, row, c};
+  int32_t *exponent = reinterpret_cast<int32_t *>(ws + b.exponent);
+  const Factors factors = {lse, dloss, dlse, coef, row, exponent, c};
   TRY(launch_tops(x, h.ldx, h.tokens, h.d, x_top, h, &factors, s));
   TRY(launch_pad({x, h.ldx, h.tokens, h.d, h.tokens, b.d8, x16, x_copy, x_top, 1, 0}, h, &factors, s));
   for (int64_t v0 = 0; v0 < h.vocab; v0 += b.piece) {
@@ -489,10 +501,10 @@ int launch_head_loss_backward(const skew_head_desc &h, const float *lse, const f
     }
     TRY(launch_head_grad(mode_of(h), logits_of(h, b, b.x_as_is ? h.x : x_copy, b.x_as_is ? h.ldx : b.d8, h.tokens, v0, w_copy),
                          {c, row, h.vocab, v0, g, b.ldg}, stream));
-    HeadResult to_dx = {last ? dx : dx_sum, last ? lddx : b.d8, last ? dx_dtype : SKEW_F32, first ? nullptr : dx_sum, b.d8, w_top, coef, 0};
+    HeadResult to_dx = {last ? dx : dx_sum, last ? lddx : b.d8, last ? dx_dtype : SKEW_F32, first ? nullptr : dx_sum, b.d8, w_top, 0, exponent, coef};
     TRY(launch_head_result(dx_mode(h), dx_of(h, b, g, w16, v0), to_dx, ws + b.rest, stream));
     bf16_t *to = static_cast<bf16_t *>(dw) + (tied(h) ? v0 * lddw : v0);
-    TRY(launch_head_result(kOuter, dw_of(h, b, x16, g, v0), {to, lddw, SKEW_BF16, nullptr, 0, x_top, coef, !tied(h)}, ws + b.rest, stream));
+    TRY(launch_head_result(kOuter, dw_of(h, b, x16, g, v0), {to, lddw, SKEW_BF16, nullptr, 0, x_top, !tied(h), nullptr, coef}, ws + b.rest, stream));
   }
   return (int)hipSuccess;
 }

@@ -40,8 +40,8 @@ struct ResultOp {
       }
       return;
     }
-    const int coef = half_exponent(*r.coef);
-    auto power = [&](int64_t at, int64_t end) { return at < end ? half_exponent(r.top[at]) + coef : 0; };
+    const int all = r.row_exponent ? 0 : factor_exponent(*r.coef);
+    auto power = [&](int64_t at, int64_t end) { return at < end ? half_exponent(r.top[at]) + all : 0; };
     int ec[FN][4];
     if (!r.by_row) {
 #pragma unroll
@@ -53,13 +53,13 @@ struct ResultOp {
 #pragma unroll
     for (int i = 0; i < FM; i++) {
       const int64_t row = row0 + i * 16;
-      const int er = r.by_row ? power(row, rows) : 0;
+      const int er = (r.by_row ? power(row, rows) : 0) + (r.row_exponent && row < rows ? r.row_exponent[row] : 0);
 #pragma unroll
       for (int j = 0; j < FN; j++) {
         const int64_t n = row < rows ? cols - col0 - j * 16 : 0;
         f32x4 v;
 #pragma unroll
-        for (int q = 0; q < 4; q++) v[q] = __builtin_ldexpf(acc[i][j][q], r.by_row ? er : ec[j][q]);
+        for (int q = 0; q < 4; q++) v[q] = __builtin_ldexpf(acc[i][j][q], r.by_row ? er : er + ec[j][q]);
         if (r.prev && n > 0) {   // (rows of whole fours)
           v += *reinterpret_cast<const f32x4 *>(r.prev + row * r.ldprev + col0 + j * 16);
         }
@@ -103,10 +103,10 @@ __global__ __launch_bounds__(256) void join_kernel(HeadResult r, int64_t rows, i
     }
   }
   const int64_t n = cols - p.col;
-  const int coef = half_exponent(*r.coef);
+  const int of_g = r.row_exponent ? r.row_exponent[p.row] : factor_exponent(*r.coef);
 #pragma unroll
   for (int q = 0; q < 8; q++) {
-    if (q < n) v[q] = __builtin_ldexpf(v[q], coef + half_exponent(r.top[r.by_row ? p.row : p.col + q]));
+    if (q < n) v[q] = __builtin_ldexpf(v[q], of_g + half_exponent(r.top[r.by_row ? p.row : p.col + q]));
     if (r.prev && q < n) v[q] += r.prev[p.row * r.ldprev + p.col + q];
   }
   if (r.y_dtype == SKEW_F32) store8(static_cast<float *>(r.y) + p.row * r.ldy + p.col, n, v);
@@ -179,6 +179,7 @@ HeadResult result_of(const HeadResult &r, int64_t row, int64_t col) {
   q.y = static_cast<char *>(r.y) + (row * r.ldy + col) * (r.y_dtype == SKEW_F32 ? 4 : 2);
   if (r.prev) q.prev = r.prev + row * r.ldprev + col;
   q.top = r.top + (r.by_row ? row : col);
+  if (r.row_exponent) q.row_exponent = r.row_exponent + row;
   return q;
 }
 int64_t part_ld(int64_t cols) { return (cols + 7) / 8 * 8; }

@@ -14,7 +14,7 @@ import torch
 
 U32 = 2.0**-24
 UBF = 2.0**-8
-F16, F16_LOW = 2.0**-11, 2.0**-39
+F16, F16_LOW = 2.0**-11, 2.0**-39   # half a step; half a step below the normal numbers, of a largest value kept as 2^14 or more
 
 
 class Ref:
@@ -51,14 +51,16 @@ class Ref:
         G[n, self.y] = rest
         e = self.ez + self.e_lse[:, None] + (4 * self.z.abs() + 16) * U32
         eG = (both.abs() + one.abs())[:, None] * p * e.expm1().clamp(max=1e3)
-        top = (both.abs() + one.abs()).max() if T else 0.0
-        eG += (F16 + 8 * U32) * G.abs() + F16_LOW * top
+        factor = torch.maximum(both.abs(), one.abs())
+        eG += (F16 + 8 * U32) * G.abs() + 2 * F16_LOW * factor[:, None]
         eG = torch.where(self.there[:, None], eG, 0.0)
         ew, ex = F16_LOW * self.w.abs().amax(0), F16_LOW * self.x.abs().amax(0) if T else torch.zeros_like(self.w[0])
         Ga = G.abs() + eG
         dx, dw = G @ self.w, G.T.contiguous() @ self.x
         bx = eG @ self.w.abs() + Ga.sum(1, keepdim=True) * ew + (2 * self.V + 16) * U32 * (Ga @ self.w.abs())
-        bw = eG.T.contiguous() @ self.x.abs() + Ga.sum(0)[:, None] * ex + (2 * T + 16) * U32 * (Ga.T.contiguous() @ self.x.abs())
+        # what is left out of x_t is relative to its column's largest times the largest factor, where the token's own is its share of G
+        share = torch.where(factor > 0, factor.max() / factor, 0.0) if T else factor
+        bw = eG.T.contiguous() @ self.x.abs() + (Ga * share[:, None]).sum(0)[:, None] * ex + (2 * T + 16) * U32 * (Ga.T.contiguous() @ self.x.abs())
         bx = bx * 1.01 + (UBF if out16 else U32) * dx.abs() * 1.01 + 1e-37
         bw = bw * 1.01 + UBF * dw.abs() * 1.01 + 1e-37
         return dx, bx, (dw if self.tied else dw.T), (bw if self.tied else bw.T)

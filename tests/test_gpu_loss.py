@@ -145,6 +145,9 @@ def test_ranges(T, tied):
     check(x, w, targets, dloss, None, tied, scale=20.0)
     check(x, w, targets, dloss * 1e-30, dlse * 1e-30, tied)
     check(x, w, targets, dloss * 1e30, None, tied)
+    far = 10.0**torch.linspace(-30, 0, T, device=DEV)   # tokens whose weights differ by as much: each row of dx has its own power of two
+    check(x, w, targets, dloss * far, None, tied)
+    check(x, w, targets, dloss * far, dlse * far.flip(0), tied, dtype=F32)
     check(x, w, targets, torch.zeros_like(dloss), dlse, tied)
     check(x, w, targets, torch.zeros_like(dloss), None, tied)
     check(torch.zeros_like(x), w, targets, dloss, None, tied)
