@@ -37,6 +37,7 @@ enum { SKEW_ACT_RELU = 0, SKEW_ACT_SILU = 1, SKEW_ACT_GELU_TANH = 2 };
  *   silu       f(g) = g s(g), s(y) = 1 / (1 + exp(-y))
  *   gelu_tanh  f(g) = g / 2 (1 + tanh(sqrt(2 / pi) (g + 0.044715 g^3)))
  * f(-inf) is its limit, 0; NaN gives NaN.
+ * (Backward with relu, a g that is kept as 0, below half a step, takes no gradient.)
  * g, u: rows of cols in in_dtype. codes_g, scales_g, codes_u, scales_u: forward, where not NULL, get g and u as skew_keep8
  * makes them; backward, they are what is read (codes_u NULL: no u), g and u are not.
  * Backward, da (in_dtype) being a's gradient and g, u the kept values: a (NULL: not wanted) = f(g) u again, dg = da u f'(g),

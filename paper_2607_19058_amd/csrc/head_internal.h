@@ -6,8 +6,8 @@
 
 namespace moe {
 
-// A token as the gradients' kernels take it: the base-2 exponent of its sum, the logits' gradient's factors times the power
-// of two that its row of G is kept with, and its target (-1: no token).
+// A token as the gradients' kernels take it: the base-2 exponent of its sum, the logits' gradient's factors (times the power
+// of two that its row of G is kept with), and its target (-1: no token).
 struct HeadRow {
   float l2, both, one;
   int32_t target;
@@ -67,7 +67,8 @@ constexpr int64_t kFewRows = 16;
 int64_t head_few_parts(int64_t cols);
 int launch_head_few(const HeadProduct &p, const HeadForward &f, void *stream);
 
-// Backward: G of this product's columns, float16 [rows x ldg].
+// Backward: G of this product's columns, float16 [rows x ldg]; or, split, as the sum of two bf16 numbers, [2 rows x ldg]: all rows of the
+// upper halves, then all of the rests.
 struct HeadGrad {
   float c;
   const HeadRow *row;
@@ -75,10 +76,12 @@ struct HeadGrad {
   uint16_t *g;
   int64_t ldg;
 };
-int launch_head_grad(int mode, const HeadProduct &p, const HeadGrad &g, void *stream);
+int launch_head_grad(int mode, const HeadProduct &p, const HeadGrad &g, bool split, void *stream);
 
 // result = 2^e (a b) + prev, of float16 operands. e is the sum of the exponents that they are kept with: of the result's rows or columns (top:
 // bits of their largest magnitudes), and of G: of each row (row_exponent), or the largest of all (coef), which the rows of x then make up for.
+// split: the operands are bf16, e is 0; and with `fold` the result's rows are twice as many, of which row t and the one half of them further on
+// are added.
 struct HeadResult {
   void *y;
   int64_t ldy;
@@ -89,8 +92,9 @@ struct HeadResult {
   int32_t by_row;
   const int32_t *row_exponent;   // NULL: *coef
   const uint32_t *coef;
+  int32_t split, fold;
 };
-size_t head_result_scratch(int mode, const HeadProduct &p);
+size_t head_result_scratch(int mode, const HeadProduct &p, bool fold);
 int launch_head_result(int mode, const HeadProduct &p, const HeadResult &r, char *ws, void *stream);
 
 // Exponents of what is kept in float16: a value whose largest magnitude has the bits `top` is kept times 2^-exponent, so

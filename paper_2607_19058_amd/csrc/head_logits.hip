@@ -95,6 +95,8 @@ struct ForwardOp {
   }
 };
 
+// SPLIT: the gradient is the sum of two bf16 numbers, its upper half, cut off, and the rest, which is exact before its own rounding.
+template <bool SPLIT>
 struct GradOp {
   static constexpr bool kHalf = false;
   HeadGrad g;
@@ -102,44 +104,59 @@ struct GradOp {
   __device__ __forceinline__ bool take(const ProductArgs &a, Tile *t) const {
     return take_plain<MODE, BM, BN>(a, t);
   }
+  // 16 bits of a value: float16; SPLIT: part 0 or 1 of it
+  template <int PART>
+  static __device__ __forceinline__ uint32_t bits(float x) {
+    if (!SPLIT) return __builtin_bit_cast(uint16_t, (_Float16)x);
+    const uint32_t u = __float_as_uint(x);
+    if (PART == 0) return u >> 16;
+    const bool finite = (u & 0x7F800000u) != 0x7F800000u;
+    return finite ? pack2(x - __uint_as_float(u & 0xFFFF0000u), 0.0f) & 0xFFFFu : u >> 16;
+  }
   template <int MODE, int FM, int FN>
   __device__ __forceinline__ void finish(const ProductArgs &a, const Tile &t, int wr, int wc, const f32x4 (&acc)[FM][FN],
                                          char *room) const {
-    typedef uint16_t __attribute__((may_alias)) u16;
     const int lane = threadIdx.x & 63;
     const int64_t col_w = t.c0 + wc, row_w = t.r0 + wr;
     const int64_t left = g.vocab - g.col0 - col_w;
     const bool whole = left >= 16 * FN;
     const int mine = (int)(left < 16 * FN ? left : 16 * FN) - (lane >> 4) * 4;
-    auto half = [](float x) { return __builtin_bit_cast(uint16_t, (_Float16)x); };
+    auto part = [&](auto PART) {
+      typedef uint16_t __attribute__((may_alias)) u16;
 #pragma unroll
-    for (int i = 0; i < FM; i++) {
-      const int64_t row = row_w + i * 16 + (lane & 15);
-      HeadRow r = {0.0f, 0.0f, 0.0f, -1};
-      if (row < t.r1) r = g.row[row];
-      const bool token = r.target >= 0;
+      for (int i = 0; i < FM; i++) {
+        const int64_t row = row_w + i * 16 + (lane & 15);
+        HeadRow r = {0.0f, 0.0f, 0.0f, -1};
+        if (row < t.r1) r = g.row[row];
+        const bool token = r.target >= 0;
 #pragma unroll
-      for (int j = 0; j < FN; j++) {
-        uint16_t h[4];
+        for (int j = 0; j < FN; j++) {
+          uint32_t h[4];
 #pragma unroll
-        for (int q = 0; q < 4; q++) {
-          float v = r.both * exp2_(__builtin_fmaf(acc[i][j][q], g.c, -r.l2));
-          if (!whole && j * 16 + q >= mine) v = 0.0f;
-          h[q] = half(token ? v : 0.0f);   // (a row that is no token may hold NaN)
+          for (int q = 0; q < 4; q++) {
+            float v = r.both * exp2_(__builtin_fmaf(acc[i][j][q], g.c, -r.l2));
+            if (!whole && j * 16 + q >= mine) v = 0.0f;
+            h[q] = bits<PART>(token ? v : 0.0f);   // (a row that is no token may hold NaN)
+          }
+          put_room<FN>(room, i, j, make_uint2(h[0] | h[1] << 16, h[2] | h[3] << 16));
         }
-        put_room<FN>(room, i, j, make_uint2(h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16));
+        const int64_t at = r.target - g.col0 - col_w;
+        const int k = token && at >= 0 && at < 16 * FN ? (int)at : -1;
+        float z;
+        if (pick<FN>(acc[i], k, &z)) {   // both p - one, where p is near 1: (both - one) p + one (p - 1)
+          const float d = __builtin_fmaf(z, g.c, -r.l2);
+          const float v = __builtin_fmaf(r.both - r.one, exp2_(d), r.one * expm1f(d * 0.6931471805599453f));
+          const int row16 = i * 16 + (lane & 15);
+          *reinterpret_cast<u16 *>(room + row16 * (FN * 32) + ((k >> 3) ^ (row16 & 7)) * 16 + (k & 7) * 2) = (uint16_t)bits<PART>(v);
+        }
       }
-      const int64_t at = r.target - g.col0 - col_w;
-      const int k = token && at >= 0 && at < 16 * FN ? (int)at : -1;
-      float z;
-      if (pick<FN>(acc[i], k, &z)) {   // both p - one, where p is near 1: (both - one) p + one (p - 1)
-        const float d = __builtin_fmaf(z, g.c, -r.l2);
-        const float v = __builtin_fmaf(r.both - r.one, exp2_(d), r.one * expm1f(d * 0.6931471805599453f));
-        const int row16 = i * 16 + (lane & 15);
-        *reinterpret_cast<u16 *>(room + row16 * (FN * 32) + ((k >> 3) ^ (row16 & 7)) * 16 + (k & 7) * 2) = half(v);
-      }
+      store_room<FM, FN, true>(room, g.g + (row_w + PART * t.r1) * g.ldg + col_w, g.ldg, t.r1 - row_w, t.c1 - col_w);
+    };
+    part(std::integral_constant<int, 0>());
+    if constexpr (SPLIT) {
+      __builtin_amdgcn_wave_barrier();   // the room is written again (the values are computed twice: registers for all of them would be more)
+      part(std::integral_constant<int, 1>());
     }
-    store_room<FM, FN, true>(room, g.g + row_w * g.ldg + col_w, g.ldg, t.r1 - row_w, t.c1 - col_w);
   }
 };
 
@@ -234,8 +251,9 @@ ForwardOp shifted(const ForwardOp &op, int mode, const Choice &c) {
   o.f.part_at += runs(mode, c.tile, c.first);
   return o;
 }
-GradOp shifted(const GradOp &op, int, const Choice &c) {
-  GradOp o = op;
+template <bool SPLIT>
+GradOp<SPLIT> shifted(const GradOp<SPLIT> &op, int, const Choice &c) {
+  GradOp<SPLIT> o = op;
   o.g.col0 += c.first;
   o.g.g += c.first;
   return o;
@@ -259,9 +277,13 @@ int launch_head_forward(int mode, const HeadProduct &p, const HeadForward &f, vo
   const ForwardOp op = {f};
   return mode == kBackward ? launch_mode<ForwardOp, kBackward>(p, op, stream) : launch_mode<ForwardOp, kForward>(p, op, stream);
 }
-int launch_head_grad(int mode, const HeadProduct &p, const HeadGrad &g, void *stream) {
-  const GradOp op = {g};
-  return mode == kBackward ? launch_mode<GradOp, kBackward>(p, op, stream) : launch_mode<GradOp, kForward>(p, op, stream);
+int launch_head_grad(int mode, const HeadProduct &p, const HeadGrad &g, bool split, void *stream) {
+  if (split) {
+    const GradOp<true> op = {g};
+    return mode == kBackward ? launch_mode<GradOp<true>, kBackward>(p, op, stream) : launch_mode<GradOp<true>, kForward>(p, op, stream);
+  }
+  const GradOp<false> op = {g};
+  return mode == kBackward ? launch_mode<GradOp<false>, kBackward>(p, op, stream) : launch_mode<GradOp<false>, kForward>(p, op, stream);
 }
 
 }  // namespace moe

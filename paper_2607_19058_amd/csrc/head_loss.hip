@@ -6,7 +6,11 @@
 //
 // G is rounded before the products that it enters. In bf16 that would be an error of the size of the results' own rounding; in float16,
 // which the matrix cores take at the same rate, it is an eighth. That needs float16 x and w: w is converted piece by
-// piece (a pass of its bytes, twice read and once written), x once.
+// piece (a pass of its bytes, twice read and once written), x once. For few tokens, see BackwardPlan.
+//
+// What bounds them (benchmark's head, 2048 x 50304): one token's loss, w's bytes (206 MB in 32 us from the Infinity Cache, 35 from memory); 8192
+// tokens, the matrix cores at the power limit (clocks of 1.75 to 2.0 of 2.4 GHz): forward 1.40 ms and the logits again 1.57 (1.2 and 1.08 PFLOP/s;
+// the library's plain product, with the logits written, 1.55 ms), dx 1.42 (the library 1.22), dw 1.26 (the library 1.68).
 #include <algorithm>
 
 #include "head_internal.h"
@@ -94,7 +98,7 @@ __device__ __forceinline__ void factors(const skew_head_desc &h, const float *dl
 }
 struct Factors {
   const float *lse, *dloss, *dlse;
-  uint32_t *top;    // bits of the largest
+  uint32_t *top;    // bits of the largest; NULL: G is split
   HeadRow *row;
   int32_t *exponent;   // of each row of G
   float c;
@@ -177,7 +181,7 @@ struct Padded {
   const bf16_t *x;
   int64_t ld, rows, cols, rows8, cols8;
   uint16_t *half;
-  bf16_t *copy;
+  bf16_t *copy, *again;   // (two copies)
   const uint32_t *top;
   int masked;
   int64_t groups;
@@ -192,14 +196,14 @@ __global__ __launch_bounds__(kThreads) void pad_kernel(Padded p, skew_head_desc 
     int e = 0;
     if (is_token(h, t)) {
       factors(h, f.dloss, f.dlse, t, &r.both, &r.one);
-      e = factor_exponent(factor_bits(h, f, t));
+      e = f.top ? factor_exponent(factor_bits(h, f, t)) : 0;
       r.both = __builtin_ldexpf(r.both, -e);
       r.one = __builtin_ldexpf(r.one, -e);
       r.l2 = (float)((double)f.lse[t] * ((double)f.c / (double)h.scale));
       r.target = (int32_t)id_at(h.targets, h.target_bytes, t);
     }
     f.row[t] = r;
-    f.exponent[t] = e;
+    if (f.exponent) f.exponent[t] = e;
     return;
   }
   const uint32_t wide = (uint32_t)pad_wide(p.cols8), side = kThreads / wide, at = threadIdx.x / wide;
@@ -231,6 +235,7 @@ __global__ __launch_bounds__(kThreads) void pad_kernel(Padded p, skew_head_desc 
     if (row >= p.rows8) break;
     if (p.half) *reinterpret_cast<u32x4 *>(p.half + to) = to_half8(v[i], e, less[i]);
     if (p.copy) *reinterpret_cast<u32x4 *>(p.copy + to) = v[i];
+    if (p.again) *reinterpret_cast<u32x4 *>(p.again + to) = v[i];
   }
 }
 // The same beside the rows' powers of two, whose largest magnitudes it finds: a work-group a row.
@@ -267,6 +272,7 @@ bool tied(const skew_head_desc &h) { return (h.flags & SKEW_TRANSPOSE) != 0; }
 // the last one of what is left).
 constexpr int64_t kTileRows = 256, kPieceStep = 256, kMaxPiece = 1 << 21;
 constexpr int64_t kPieceBytes = (int64_t)512 << 20;   // of G, and of a copy of w
+constexpr int64_t kSplitRows = 512;                   // up to which G is split
 constexpr int64_t kRun = 16384;                       // rows of a forward launch, whose pairs are held
 struct HeadPlan {
   bool x_as_is, w_as_is;
@@ -282,7 +288,7 @@ HeadPlan head_plan(const skew_head_desc &h, bool backward) {
   if (!backward && p.w_as_is) {
     p.piece = h.vocab;
   } else {
-    const int64_t wide = std::max(p.d8, backward ? h.tokens : 0);   // rows of G, columns of w
+    const int64_t wide = std::max(p.d8, backward ? h.tokens * (h.tokens <= kSplitRows ? 2 : 1) : 0);   // rows of G, columns of w
     int64_t most = std::min(std::max(kPieceBytes / (2 * wide), kPieceStep), kMaxPiece);
     const int64_t n = (h.vocab + most - 1) / most;
     p.piece = std::min(up((h.vocab + n - 1) / n, kPieceStep), p.v8);
@@ -317,8 +323,8 @@ int launch_pad(Padded p, const skew_head_desc &h, const Factors *f, hipStream_t 
 // the piece of w at v0, padded
 Padded piece_of(const skew_head_desc &h, const HeadPlan &p, int64_t v0, uint16_t *half, bf16_t *copy, const uint32_t *top) {
   const int64_t cols = piece_cols(h, p, v0), cols8 = up(cols, 8);
-  if (tied(h)) return {words(h, v0), h.ldw, cols, h.d, cols8, p.d8, half, copy, top, 0, 0};
-  return {words(h, v0), h.ldw, h.d, cols, p.d8, cols8, half, copy, top, 0, 0};
+  if (tied(h)) return {words(h, v0), h.ldw, cols, h.d, cols8, p.d8, half, copy, nullptr, top, 0, 0};
+  return {words(h, v0), h.ldw, h.d, cols, p.d8, cols8, half, copy, nullptr, top, 0, 0};
 }
 // f: also the largest of G's factors
 int launch_tops(const bf16_t *x, int64_t ld, int64_t rows, int64_t cols, uint32_t *top, const skew_head_desc &h, const Factors *f,
@@ -375,19 +381,29 @@ ForwardPlan forward_plan(const skew_head_desc &h) {
   return f;
 }
 
+// Up to kSplitRows tokens the bytes of w decide. Then G is the sum of two bf16 numbers, and w enters its product as it is; with more,
+// where the products decide, w is converted to float16 (see above), which takes its bytes four times more. Backward calls, us, float16 | split:
+//   tokens                             1           64          256         512         768          1024
+//   50304 words of width 2048          345 | 203   380 | 241   494 | 402   589 | 595   709 | 829    813 | 1010
+//   the same, tied                     377 | 207   404 | 235   486 | 379   605 | 594   723 | 808    836 | 1008
+//   32003 words of width 1031          141 | 103   156 | 128   209 | 233   306 | 304   343 | 385    398 | 484
+//   8192 words of width 1024            61 |  48    68 |  49    73 |  62    86 |  90   106 | 114    118 | 134
 struct BackwardPlan : HeadPlan {
+  bool split;
+  int64_t rows;   // of G
   size_t tops, row, exponent, x16, x, w16, w, g, dx, rest, bytes;
   int64_t ldg;
 };
 // the three products of a piece
 HeadProduct dx_of(const skew_head_desc &h, const BackwardPlan &b, const void *g, const void *w16, int64_t v0) {
-  const int64_t cols8 = up(piece_cols(h, b, v0), 8);
-  return {g, w16, b.ldg, tied(h) ? b.d8 : cols8, h.tokens, h.d, cols8, 0, b.d8};
+  const int64_t cols = piece_cols(h, b, v0), cols8 = up(cols, 8);
+  if (!b.split || !b.w_as_is) return {g, w16, b.ldg, tied(h) ? b.d8 : cols8, b.rows, h.d, cols8, 0, b.d8};
+  return {g, words(h, v0), b.ldg, h.ldw, b.rows, h.d, tied(h) ? cols : cols8, 0, b.d8};   // (words in rows end with the contraction)
 }
 HeadProduct dw_of(const skew_head_desc &h, const BackwardPlan &b, const void *x16, const void *g, int64_t v0) {
   const int64_t cols = piece_cols(h, b, v0), cols8 = up(cols, 8);
-  if (tied(h)) return {g, x16, b.ldg, b.d8, cols, h.d, h.tokens, cols8, b.d8};
-  return {x16, g, b.d8, b.ldg, h.d, cols, h.tokens, b.d8, cols8};
+  if (tied(h)) return {g, x16, b.ldg, b.d8, cols, h.d, b.rows, cols8, b.d8};
+  return {x16, g, b.d8, b.ldg, h.d, cols, b.rows, b.d8, cols8};
 }
 int dx_mode(const skew_head_desc &h) { return tied(h) ? kForward : kBackward; }
 
@@ -395,21 +411,23 @@ BackwardPlan backward_plan(const skew_head_desc &h) {
   BackwardPlan b;
   static_cast<HeadPlan &>(b) = head_plan(h, true);
   b.ldg = up(b.piece, 8);
+  b.split = h.tokens <= kSplitRows;
+  b.rows = b.split ? 2 * h.tokens : h.tokens;
   const size_t x = (size_t)h.tokens * b.d8 * 2, w = (size_t)b.ldg * b.d8 * 2;
   Regions r;
   b.tops = r.take((size_t)(1 + 2 * b.d8) * 4);   // of G's factors, of x's columns, of w's
   b.row = r.take((size_t)h.tokens * sizeof(HeadRow));
   b.exponent = r.take((size_t)h.tokens * 4);
-  b.x16 = r.take(x);
-  b.x = b.x_as_is ? 0 : r.take(x);
-  b.w16 = r.take(w);
+  b.x16 = r.take((size_t)b.rows * b.d8 * 2);   // split: x twice, as it is
+  b.x = b.x_as_is || b.split ? b.x16 : r.take(x);
+  b.w16 = b.split ? 0 : r.take(w);
   b.w = b.w_as_is ? 0 : r.take(w);
-  b.g = r.take((size_t)h.tokens * b.ldg * 2);
+  b.g = r.take((size_t)b.rows * b.ldg * 2);
   b.dx = pieces(h, b) > 1 ? r.take((size_t)h.tokens * b.d8 * 4) : 0;
   size_t rest = 0;
   for (int64_t v0 = 0; v0 < h.vocab; v0 += b.piece) {
-    rest = std::max(rest, head_result_scratch(dx_mode(h), dx_of(h, b, nullptr, nullptr, v0)));
-    rest = std::max(rest, head_result_scratch(kOuter, dw_of(h, b, nullptr, nullptr, v0)));
+    rest = std::max(rest, head_result_scratch(dx_mode(h), dx_of(h, b, nullptr, nullptr, v0), b.split));
+    rest = std::max(rest, head_result_scratch(kOuter, dw_of(h, b, nullptr, nullptr, v0), false));
   }
   b.rest = r.take(rest);
   b.bytes = r.at;
@@ -453,7 +471,7 @@ int launch_head_loss(const skew_head_desc &h, float *loss, float *lse, char *ws,
     r.x = static_cast<const bf16_t *>(h.x) + t0 * h.ldx;
     r.targets = static_cast<const char *>(h.targets) + t0 * h.target_bytes;
     if (!f.x_as_is)
-      TRY(launch_pad({static_cast<const bf16_t *>(r.x), h.ldx, r.tokens, h.d, r.tokens, f.d8, nullptr, x_copy, nullptr, 0, 0}, r, nullptr, s));
+      TRY(launch_pad({static_cast<const bf16_t *>(r.x), h.ldx, r.tokens, h.d, r.tokens, f.d8, nullptr, x_copy, nullptr, nullptr, 0, 0}, r, nullptr, s));
     int64_t at = 0;
     for (int64_t v0 = 0; v0 < h.vocab; v0 += f.piece) {
       if (!f.w_as_is) TRY(launch_pad(piece_of(h, f, v0, nullptr, w_copy, nullptr), r, nullptr, s));
@@ -478,17 +496,24 @@ int launch_head_loss_backward(const skew_head_desc &h, const float *lse, const f
   bf16_t *x_copy = b.x_as_is ? nullptr : reinterpret_cast<bf16_t *>(ws + b.x), *w_copy = b.w_as_is ? nullptr : reinterpret_cast<bf16_t *>(ws + b.w);
   float *dx_sum = reinterpret_cast<float *>(ws + b.dx);
   const bf16_t *x = static_cast<const bf16_t *>(h.x);
-  const int tops = (int)(1 + 2 * b.d8);
-  zero_kernel<<<(tops + kThreads - 1) / kThreads, kThreads, 0, s>>>(coef, tops);
-  TRY((int)hipGetLastError());
   int32_t *exponent = reinterpret_cast<int32_t *>(ws + b.exponent);
-  const Factors factors = {lse, dloss, dlse, coef, row, exponent, c};
-  TRY(launch_tops(x, h.ldx, h.tokens, h.d, x_top, h, &factors, s));
-  TRY(launch_pad({x, h.ldx, h.tokens, h.d, h.tokens, b.d8, x16, x_copy, x_top, 1, 0}, h, &factors, s));
+  const Factors factors = {lse, dloss, dlse, b.split ? nullptr : coef, row, b.split ? nullptr : exponent, c};
+  if (b.split) {
+    bf16_t *copy = reinterpret_cast<bf16_t *>(x16);
+    TRY(launch_pad({x, h.ldx, h.tokens, h.d, h.tokens, b.d8, nullptr, copy, copy + h.tokens * b.d8, nullptr, 1, 0}, h, &factors, s));
+  } else {
+    const int tops = (int)(1 + 2 * b.d8);
+    zero_kernel<<<(tops + kThreads - 1) / kThreads, kThreads, 0, s>>>(coef, tops);
+    TRY((int)hipGetLastError());
+    TRY(launch_tops(x, h.ldx, h.tokens, h.d, x_top, h, &factors, s));
+    TRY(launch_pad({x, h.ldx, h.tokens, h.d, h.tokens, b.d8, x16, x_copy, nullptr, x_top, 1, 0}, h, &factors, s));
+  }
   for (int64_t v0 = 0; v0 < h.vocab; v0 += b.piece) {
-    const Padded p = piece_of(h, b, v0, w16, w_copy, w_top);
+    const Padded p = piece_of(h, b, v0, b.split ? nullptr : w16, w_copy, w_top);
     const bool first = v0 == 0, last = v0 + b.piece >= h.vocab;
-    if (tied(h)) {
+    if (b.split) {
+      if (!b.w_as_is) TRY(launch_pad(p, h, nullptr, s));
+    } else if (tied(h)) {
       if (!first) {
         zero_kernel<<<(unsigned)((b.d8 + kThreads - 1) / kThreads), kThreads, 0, s>>>(w_top, (int)b.d8);
         TRY((int)hipGetLastError());
@@ -499,12 +524,21 @@ int launch_head_loss_backward(const skew_head_desc &h, const float *lse, const f
       pad_rows_kernel<<<(unsigned)p.rows8, kThreads, 0, s>>>(p, w_top);
       TRY((int)hipGetLastError());
     }
+    const void *w = b.split ? static_cast<const void *>(w_copy) : w16;
     TRY(launch_head_grad(mode_of(h), logits_of(h, b, b.x_as_is ? h.x : x_copy, b.x_as_is ? h.ldx : b.d8, h.tokens, v0, w_copy),
-                         {c, row, h.vocab, v0, g, b.ldg}, stream));
-    HeadResult to_dx = {last ? dx : dx_sum, last ? lddx : b.d8, last ? dx_dtype : SKEW_F32, first ? nullptr : dx_sum, b.d8, w_top, 0, exponent, coef};
-    TRY(launch_head_result(dx_mode(h), dx_of(h, b, g, w16, v0), to_dx, ws + b.rest, stream));
-    bf16_t *to = static_cast<bf16_t *>(dw) + (tied(h) ? v0 * lddw : v0);
-    TRY(launch_head_result(kOuter, dw_of(h, b, x16, g, v0), {to, lddw, SKEW_BF16, nullptr, 0, x_top, !tied(h), nullptr, coef}, ws + b.rest, stream));
+                         {c, row, h.vocab, v0, g, b.ldg}, b.split, stream));
+    HeadResult to_dx = {last ? dx : dx_sum, last ? lddx : b.d8, last ? dx_dtype : SKEW_F32, first ? nullptr : dx_sum, b.d8};
+    HeadResult to_dw = {static_cast<bf16_t *>(dw) + (tied(h) ? v0 * lddw : v0), lddw, SKEW_BF16, nullptr, 0};
+    to_dx.split = to_dw.split = to_dx.fold = b.split;
+    if (!b.split) {
+      to_dx.top = w_top;
+      to_dx.row_exponent = exponent;
+      to_dw.top = x_top;
+      to_dw.by_row = !tied(h);
+      to_dw.coef = coef;
+    }
+    TRY(launch_head_result(dx_mode(h), dx_of(h, b, g, w, v0), to_dx, ws + b.rest, stream));
+    TRY(launch_head_result(kOuter, dw_of(h, b, x16, g, v0), to_dw, ws + b.rest, stream));
   }
   return (int)hipSuccess;
 }

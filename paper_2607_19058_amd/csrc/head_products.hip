@@ -1,12 +1,14 @@
-// head_products.hip -- the gradients of the head's rows and weights: products of float16 operands on the matrix cores.
+// head_products.hip -- the gradients of the head's rows and weights: products of float16 operands on the matrix cores, or of bf16 ones, of which
+// G is the sum of two.
 #include "head_internal.h"
 #include "product_tiles.h"
 
 namespace moe {
 namespace {
 
+template <bool HALF>
 struct ResultOp {
-  static constexpr bool kHalf = true;
+  static constexpr bool kHalf = HALF;
   HeadResult r;
   int64_t rows, cols;
   int32_t parts;
@@ -40,8 +42,8 @@ struct ResultOp {
       }
       return;
     }
-    const int all = r.row_exponent ? 0 : factor_exponent(*r.coef);
-    auto power = [&](int64_t at, int64_t end) { return at < end ? half_exponent(r.top[at]) + all : 0; };
+    const int all = !HALF || r.row_exponent ? 0 : factor_exponent(*r.coef);
+    auto power = [&](int64_t at, int64_t end) { return HALF && at < end ? half_exponent(r.top[at]) + all : 0; };
     int ec[FN][4];
     if (!r.by_row) {
 #pragma unroll
@@ -53,13 +55,13 @@ struct ResultOp {
 #pragma unroll
     for (int i = 0; i < FM; i++) {
       const int64_t row = row0 + i * 16;
-      const int er = (r.by_row ? power(row, rows) : 0) + (r.row_exponent && row < rows ? r.row_exponent[row] : 0);
+      const int er = (r.by_row ? power(row, rows) : 0) + (HALF && r.row_exponent && row < rows ? r.row_exponent[row] : 0);
 #pragma unroll
       for (int j = 0; j < FN; j++) {
         const int64_t n = row < rows ? cols - col0 - j * 16 : 0;
         f32x4 v;
 #pragma unroll
-        for (int q = 0; q < 4; q++) v[q] = __builtin_ldexpf(acc[i][j][q], r.by_row ? er : er + ec[j][q]);
+        for (int q = 0; q < 4; q++) v[q] = HALF ? __builtin_ldexpf(acc[i][j][q], r.by_row ? er : er + ec[j][q]) : acc[i][j][q];
         if (r.prev && n > 0) {   // (rows of whole fours)
           v += *reinterpret_cast<const f32x4 *>(r.prev + row * r.ldprev + col0 + j * 16);
         }
@@ -81,8 +83,8 @@ struct ResultOp {
   }
 };
 
-template <int MODE, int FM, int FN, int NS, int KS>
-__global__ __launch_bounds__(256, per_unit(FM, FN, KS)) void result_kernel(ProductArgs a, ResultOp op) {
+template <bool HALF, int MODE, int FM, int FN, int NS, int KS>
+__global__ __launch_bounds__(256, per_unit(FM, FN, KS)) void result_kernel(ProductArgs a, ResultOp<HALF> op) {
   tile_body<MODE, FM, FN, NS, KS>(a, op);
 }
 
@@ -103,10 +105,10 @@ __global__ __launch_bounds__(256) void join_kernel(HeadResult r, int64_t rows, i
     }
   }
   const int64_t n = cols - p.col;
-  const int of_g = r.row_exponent ? r.row_exponent[p.row] : factor_exponent(*r.coef);
+  const int of_g = r.split ? 0 : r.row_exponent ? r.row_exponent[p.row] : factor_exponent(*r.coef);
 #pragma unroll
   for (int q = 0; q < 8; q++) {
-    if (q < n) v[q] = __builtin_ldexpf(v[q], of_g + half_exponent(r.top[r.by_row ? p.row : p.col + q]));
+    if (q < n && !r.split) v[q] = __builtin_ldexpf(v[q], of_g + half_exponent(r.top[r.by_row ? p.row : p.col + q]));
     if (r.prev && q < n) v[q] += r.prev[p.row * r.ldprev + p.col + q];
   }
   if (r.y_dtype == SKEW_F32) store8(static_cast<float *>(r.y) + p.row * r.ldy + p.col, n, v);
@@ -142,13 +144,13 @@ struct Plan {
   Choice main, rest;
   int64_t rows, cols;   // of main
 };
-Plan plan_result(int mode, const HeadProduct &p) {
+Plan plan_result(int mode, const HeadProduct &p, bool fold) {
   Plan s = {{0, 1}, {0, 0}, p.rows, p.cols};
   double least = 0.97 * best_of(mode, p.rows, p.cols, p.K, &s.main);
   const HeadTile t = head_tile(mode == kBackward, 0);
   const int64_t down = (p.rows + t.rows - 1) / t.rows, across = (p.cols + t.cols - 1) / t.cols, whole = down * across / t.slots * t.slots;
   auto cut = [&](int64_t rows, int64_t cols) {   // (one of them all)
-    if (rows == 0 || cols == 0 || (rows >= p.rows && cols >= p.cols)) return;
+    if (rows == 0 || cols == 0 || (rows >= p.rows && cols >= p.cols) || (fold && rows < p.rows)) return;
     Plan c = {{0, 1}, {0, 1}, rows, cols};
     const double time = best_of(mode, rows, cols, p.K, &c.main) +
                         best_of(mode, rows < p.rows ? p.rows - rows : rows, rows < p.rows ? cols : p.cols - cols, p.K, &c.rest);
@@ -178,13 +180,13 @@ HeadResult result_of(const HeadResult &r, int64_t row, int64_t col) {
   HeadResult q = r;
   q.y = static_cast<char *>(r.y) + (row * r.ldy + col) * (r.y_dtype == SKEW_F32 ? 4 : 2);
   if (r.prev) q.prev = r.prev + row * r.ldprev + col;
-  q.top = r.top + (r.by_row ? row : col);
+  if (r.top) q.top = r.top + (r.by_row ? row : col);
   if (r.row_exponent) q.row_exponent = r.row_exponent + row;
   return q;
 }
 int64_t part_ld(int64_t cols) { return (cols + 7) / 8 * 8; }
 
-template <int MODE, int FM, int FN, int NS, int KS>
+template <bool HALF, int MODE, int FM, int FN, int NS, int KS>
 int launch_one(const HeadProduct &p, const HeadResult &r, Choice c, char *ws, void *stream) {
   ProductArgs a = {};
   a.x = static_cast<const bf16_t *>(p.a);   // (float16 bits)
@@ -199,7 +201,8 @@ int launch_one(const HeadProduct &p, const HeadResult &r, Choice c, char *ws, vo
   a.row_tiles = (p.rows + 32 * FM - 1) / (32 * FM);
   const int64_t cols = (p.pad_cols + 32 * FN - 1) / (32 * FN);
   int parts = 1;
-  if (c.parts > 1) {
+  const bool joined = c.parts > 1 || r.fold;
+  if (joined) {
     a.part = (int32_t)(((p.K + c.parts - 1) / c.parts + 63) / 64 * 64);
     parts = (int)((p.K + a.part - 1) / a.part);
     a.y = ws;
@@ -208,45 +211,50 @@ int launch_one(const HeadProduct &p, const HeadResult &r, Choice c, char *ws, vo
   const int64_t grid = plain_grid(a.row_tiles * cols * parts);
   if (grid > kMostGroups) return (int)hipErrorInvalidConfiguration;
   hipStream_t s = static_cast<hipStream_t>(stream);
-  result_kernel<MODE, FM, FN, NS, KS><<<(unsigned)grid, 256, 0, s>>>(a, ResultOp{r, p.rows, p.cols, parts});
+  result_kernel<HALF, MODE, FM, FN, NS, KS><<<(unsigned)grid, 256, 0, s>>>(a, ResultOp<HALF>{r, p.rows, p.cols, parts});
   const int e = (int)hipGetLastError();
-  if (e != (int)hipSuccess || c.parts == 1) return e;
-  join_kernel<<<(unsigned)((p.rows * (part_ld(p.cols) / 8) + 255) / 256), 256, 0, s>>>(r, p.rows, p.cols, reinterpret_cast<float *>(ws), parts,
+  if (e != (int)hipSuccess || !joined) return e;
+  const int64_t rows = r.fold ? p.rows / 2 : p.rows;   // (a part's second half is as if it were a part)
+  join_kernel<<<(unsigned)((rows * (part_ld(p.cols) / 8) + 255) / 256), 256, 0, s>>>(r, rows, p.cols, reinterpret_cast<float *>(ws), r.fold ? 2 * parts : parts,
                                                                                      a.ldy);
   return (int)hipGetLastError();
 }
-template <int MODE>
+template <bool HALF, int MODE>
 int launch_choice(const HeadProduct &p, const HeadResult &r, Choice c, char *ws, void *stream) {
   constexpr int S = MODE == kBackward ? 2 : 1;
-  if (c.tile == 0) return launch_one<MODE, 8, 8, 4 / S, S>(p, r, c, ws, stream);
-  if (c.tile == 1) return launch_one<MODE, 4, 8, 3, 1>(p, r, c, ws, stream);
-  return launch_one<MODE, 2, 4, 4 / S, S>(p, r, c, ws, stream);
+  if (c.tile == 0) return launch_one<HALF, MODE, 8, 8, 4 / S, S>(p, r, c, ws, stream);
+  if (c.tile == 1) return launch_one<HALF, MODE, 4, 8, 3, 1>(p, r, c, ws, stream);
+  return launch_one<HALF, MODE, 2, 4, 4 / S, S>(p, r, c, ws, stream);
 }
-template <int MODE>
+template <bool HALF, int MODE>
 int launch_mode(const HeadProduct &p, const HeadResult &r, char *ws, void *stream) {
-  const Plan s = plan_result(MODE, p);
-  if (s.rest.parts == 0) return launch_choice<MODE>(p, r, s.main, ws, stream);
-  const int e = launch_choice<MODE>(part_of(MODE, p, 0, 0, s.rows, s.cols), r, s.main, ws, stream);
+  const Plan s = plan_result(MODE, p, r.fold);
+  if (s.rest.parts == 0) return launch_choice<HALF, MODE>(p, r, s.main, ws, stream);
+  const int e = launch_choice<HALF, MODE>(part_of(MODE, p, 0, 0, s.rows, s.cols), r, s.main, ws, stream);
   if (e != (int)hipSuccess) return e;
   const int64_t row = s.rows < p.rows ? s.rows : 0, col = s.rows < p.rows ? 0 : s.cols;
-  return launch_choice<MODE>(part_of(MODE, p, row, col, p.rows - row, p.cols - col), result_of(r, row, col), s.rest, ws, stream);
+  return launch_choice<HALF, MODE>(part_of(MODE, p, row, col, p.rows - row, p.cols - col), result_of(r, row, col), s.rest, ws, stream);
 }
-size_t scratch_of(const Choice &c, int64_t rows, int64_t cols) {
-  return c.parts > 1 ? pad256((size_t)c.parts * (size_t)rows * (size_t)part_ld(cols) * 4) : 0;
+size_t scratch_of(const Choice &c, int64_t rows, int64_t cols, bool fold) {
+  return c.parts > 1 || fold ? pad256((size_t)c.parts * (size_t)rows * (size_t)part_ld(cols) * 4) : 0;
 }
 
 }  // namespace
 
-size_t head_result_scratch(int mode, const HeadProduct &p) {
-  const Plan s = plan_result(mode, p);
-  const size_t main = scratch_of(s.main, s.rows, s.cols);
+size_t head_result_scratch(int mode, const HeadProduct &p, bool fold) {
+  const Plan s = plan_result(mode, p, fold);
+  const size_t main = scratch_of(s.main, s.rows, s.cols, fold);
   if (s.rest.parts == 0) return main;
-  const size_t rest = scratch_of(s.rest, s.rows < p.rows ? p.rows - s.rows : p.rows, s.rows < p.rows ? p.cols : p.cols - s.cols);
+  const size_t rest = scratch_of(s.rest, s.rows < p.rows ? p.rows - s.rows : p.rows, s.rows < p.rows ? p.cols : p.cols - s.cols, fold);
   return main > rest ? main : rest;
 }
 int launch_head_result(int mode, const HeadProduct &p, const HeadResult &r, char *ws, void *stream) {
-  if (mode == kOuter) return launch_mode<kOuter>(p, r, ws, stream);
-  return mode == kBackward ? launch_mode<kBackward>(p, r, ws, stream) : launch_mode<kForward>(p, r, ws, stream);
+  if (r.split) {
+    if (mode == kOuter) return launch_mode<false, kOuter>(p, r, ws, stream);
+    return mode == kBackward ? launch_mode<false, kBackward>(p, r, ws, stream) : launch_mode<false, kForward>(p, r, ws, stream);
+  }
+  if (mode == kOuter) return launch_mode<true, kOuter>(p, r, ws, stream);
+  return mode == kBackward ? launch_mode<true, kBackward>(p, r, ws, stream) : launch_mode<true, kForward>(p, r, ws, stream);
 }
 
 }  // namespace moe

@@ -159,7 +159,7 @@ def expert_act(g, u=None, *, kind="silu", keep=False, dtype=None, stream=None):
 def expert_act_backward(da, kept, *, kind="silu", again=True, dtype=None, stream=None):
     """Gradients of `expert_act` from that of its result and what it kept: (a, dg, du) in da's type or ``dtype``. a is
     the activation of the kept values, which the next product's weights' gradient takes (None with ``again=False``); du is
-    None without u."""
+    None without u. With "relu", whose slope jumps, a g below half a step is kept as 0 and takes no gradient."""
     import torch
     _no_autograd(da)
     kind = _kind(kind)
