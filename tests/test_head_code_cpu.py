@@ -11,7 +11,7 @@ from paper_2607_19058_amd import build
 from test_kernel_code_cpu import early_reads
 
 pytestmark = pytest.mark.skipif(shutil.which(build.hipcc()) is None, reason="needs hipcc")
-FILES = {"head_logits": 4, "head_products": 3, "kept_product": 2}   # and how many kernels keep their sums in accumulation registers
+FILES = {"head_logits": 6, "head_products": 6, "kept_product": 2}   # and how many kernels keep their sums in accumulation registers
 
 
 def listing(name, out):
@@ -61,6 +61,6 @@ def test_sums_are_read_after_the_wait(listings, name):
 
 @pytest.mark.parametrize("name", FILES)
 def test_the_products_take_their_operands_type(listings, name):
-    """Logits and kept rows bf16, the gradients of rows and weights float16."""
-    ops = set(re.findall(r"v_mfma_f32_16x16x32_\w+", open(listings[name]).read()))
-    assert ops == {"v_mfma_f32_16x16x32_f16" if name == "head_products" else "v_mfma_f32_16x16x32_bf16"}
+    """Logits and kept rows bf16, the gradients of rows and weights float16, or bf16 (few tokens)."""
+    ops = set(re.findall(r"v_mfma_f32_16x16x32_(\w+)", open(listings[name]).read()))
+    assert ops == ({"f16", "bf16"} if name == "head_products" else {"bf16"})
