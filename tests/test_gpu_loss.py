@@ -186,6 +186,23 @@ def test_what_is_not_finite_reaches_its_own_rows_alone(T, tied):
 
 
 @pytest.mark.parametrize("tied", [False, True])
+def test_float16_below_its_normal_numbers(tied):
+    """One column of x is zero but for a token whose factor is 2^-30 of the largest: its entry is kept as 2^-16 or a little more, with half
+    steps of 2^-25, 2^-9 of it; G and the result are off by 2^-11 and 2^-8 more."""
+    x, w, targets, dloss, _ = inputs(600, 64, 300, tied=tied, none=0.0)
+    dloss = torch.full_like(dloss, 1.0)
+    x[:, 5], x[7, 5], dloss[7] = 0.0, 1.5, 2.0**-30
+    ref = Ref(x, w, targets, tied)
+    _, lse = P.head_loss(x, w, targets, tied=tied)
+    _, dw = P.head_loss_backward(x, w, targets, lse, dloss, tied=tied)
+    _, _, want, _ = ref.backward(dloss)
+    got, want = (t[:, 5] if tied else t[5] for t in (dw.double(), want))
+    assert float(want.abs().max()) > 0
+    error = (got - want).abs() / want.abs()
+    assert float(error.max()) <= 2.0**-9 + 2.0**-11 + 2.0**-8 + 1e-4   # (and float32's errors of the logits)
+
+
+@pytest.mark.parametrize("tied", [False, True])
 def test_gradients_against_differences(tied):
     """sum_t dloss_t loss_t + dlse_t lse_t of the definition moves by <dx, step> and <dw, step>."""
     T, d, V = 60, 48, 130
