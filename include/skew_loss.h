@@ -25,8 +25,8 @@ extern "C" {
  * and it adds nothing to dw.
  * Gradients, from those of loss (dloss) and lse (dlse; NULL: 0), G being that of the logits:
  *   G_tv = scale ((dloss_t + dlse_t) exp(z_tv - lse_t) - dloss_t [v = y_t]);   dx = G w^T;   dw = x^T G
- * computed in pieces of the vocabulary. G is rounded before these products: up to 512 tokens to the sum of two bf16 numbers, which leaves
- * out 2^-16 of an entry; with more, G and the operand beside it are float16 numbers (11 bits, 8 times finer than bf16) times powers
+ * computed in pieces of the vocabulary. G is rounded before these products: up to 512 tokens, or 2^29 of
+ * tokens * d * vocab, to the sum of two bf16 numbers, which leaves out 2^-16 of an entry; with more, G and the operand beside it are float16 numbers (11 bits, 8 times finer than bf16) times powers
  * of two: of G's rows, by their tokens' larger factor, and of the columns of x and w (their d), by their largest values. So an entry
  * of G below 2^-28 of its row's factor, or one of x or w below 2^-29 of its column's largest, keeps fewer bits, down to none 11 powers
  * further (for dw, of x times its token's factor). dx and dw are rounded once more.

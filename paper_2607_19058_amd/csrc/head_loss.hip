@@ -271,9 +271,13 @@ bool tied(const skew_head_desc &h) { return (h.flags & SKEW_TRANSPOSE) != 0; }
 // What is the same in both calls: which operands the tiles take as they are, and pieces of the vocabulary (of kPieceStep columns,
 // the last one of what is left).
 constexpr int64_t kTileRows = 256, kPieceStep = 256, kMaxPiece = 1 << 21;
-constexpr int64_t kPieceBytes = (int64_t)512 << 20;   // of G, and of a copy of w
-constexpr int64_t kSplitRows = 512;                   // up to which G is split
+constexpr int64_t kPieceBytes = (int64_t)512 << 20;   // of G, and of a copy of w (8192 tokens, 50304 words: 128 MiB 5.91 ms, 256 6.02, 512 5.72, 1024 5.71)
 constexpr int64_t kRun = 16384;                       // rows of a forward launch, whose pairs are held
+// Whether G is split (see BackwardPlan).
+bool splits(const skew_head_desc &h) {
+  constexpr int64_t kRows = 512, kSmall = (int64_t)1 << 29;   // (tokens * d is below 2^42)
+  return h.tokens <= kRows || h.tokens * h.d <= kSmall / h.vocab;
+}
 struct HeadPlan {
   bool x_as_is, w_as_is;
   int64_t d8, v8, piece, run;
@@ -288,7 +292,7 @@ HeadPlan head_plan(const skew_head_desc &h, bool backward) {
   if (!backward && p.w_as_is) {
     p.piece = h.vocab;
   } else {
-    const int64_t wide = std::max(p.d8, backward ? h.tokens * (h.tokens <= kSplitRows ? 2 : 1) : 0);   // rows of G, columns of w
+    const int64_t wide = std::max(p.d8, backward ? h.tokens * (splits(h) ? 2 : 1) : 0);   // rows of G, columns of w
     int64_t most = std::min(std::max(kPieceBytes / (2 * wide), kPieceStep), kMaxPiece);
     const int64_t n = (h.vocab + most - 1) / most;
     p.piece = std::min(up((h.vocab + n - 1) / n, kPieceStep), p.v8);
@@ -381,13 +385,17 @@ ForwardPlan forward_plan(const skew_head_desc &h) {
   return f;
 }
 
-// Up to kSplitRows tokens the bytes of w decide. Then G is the sum of two bf16 numbers, and w enters its product as it is; with more,
-// where the products decide, w is converted to float16 (see above), which takes its bytes four times more. Backward calls, us, float16 | split:
+// Up to 512 tokens the bytes of w decide. Then G is the sum of two bf16 numbers, and w enters its product as it is; with more,
+// where the products decide, w is converted to float16 (see above), which takes its bytes four times more. Where tokens, width and words
+// together are few, the conversions' launches decide. Backward calls, us, float16 | split:
 //   tokens                             1           64          256         512         768          1024
 //   50304 words of width 2048          345 | 203   380 | 241   494 | 402   589 | 595   709 | 829    813 | 1010
 //   the same, tied                     377 | 207   404 | 235   486 | 379   605 | 594   723 | 808    836 | 1008
 //   32003 words of width 1031          141 | 103   156 | 128   209 | 233   306 | 304   343 | 385    398 | 484
 //   8192 words of width 1024            61 |  48    68 |  49    73 |  62    86 |  90   106 | 114    118 | 134
+//   tokens x width x words             2048x128x512   1024x512x1024   2048x256x1024   4096x128x1024   1024x1024x1024   1024x256x4096
+//     (2^27, 2^29, .., 2^30)           43 | 37        54 | 48         53 | 48         55 | 58         58 | 55          58 | 61
+//     tied                             49 | 37        58 | 49         58 | 47         60 | 58         66 | 58          67 | 62
 struct BackwardPlan : HeadPlan {
   bool split;
   int64_t rows;   // of G
@@ -411,7 +419,7 @@ BackwardPlan backward_plan(const skew_head_desc &h) {
   BackwardPlan b;
   static_cast<HeadPlan &>(b) = head_plan(h, true);
   b.ldg = up(b.piece, 8);
-  b.split = h.tokens <= kSplitRows;
+  b.split = splits(h);
   b.rows = b.split ? 2 * h.tokens : h.tokens;
   const size_t x = (size_t)h.tokens * b.d8 * 2, w = (size_t)b.ldg * b.d8 * 2;
   Regions r;

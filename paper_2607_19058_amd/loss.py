@@ -96,8 +96,8 @@ def head_loss(x, w, targets, *, tied=False, scale=1.0, stream=None):
 
 def head_loss_backward(x, w, targets, lse, dloss, *, dlse=None, tied=False, scale=1.0, dtype=None, out=None, stream=None):
     """Gradients of `head_loss`: (dx (T, d) in bf16 or ``dtype``, dw bf16 in w's shape) from those of loss and (``dlse``) of lse,
-    float32 (T), and the lse that it gave. The logits are computed again, in pieces of the vocabulary whose gradient (16 bits, or up
-    to 512 tokens twice 16, at most 512 MiB) is held. ``out`` takes an existing tensor for dw, such as the gradient that an optimizer was given."""
+    float32 (T), and the lse that it gave. The logits are computed again, in pieces of the vocabulary whose gradient (16 bits, or for
+    few tokens twice 16, at most 512 MiB) is held. ``out`` takes an existing tensor for dw, such as the gradient that an optimizer was given."""
     import torch
     _no_autograd(x, w, lse, dloss, dlse, out)
     h = _head(x, w, targets, tied, scale)

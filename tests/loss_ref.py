@@ -6,7 +6,7 @@ Error bounds, from the arithmetic (u = 2^-24, half an ulp of float32; A_tv = sca
             of the sums (32 in a lane, the tree, the runs, one after another)
   loss      the two together
   G         exp(z - lse) is off by e = error of z and lse, relatively; the factors by 4 u; float16 by 2^-11 of the value (half
-            a step; two bf16 numbers, up to 512 tokens, by 2^-16) and, below its smallest normal number, by 2^-39 of the largest factor (2^-25 where that is 2^14 or more)
+            a step; two bf16 numbers, for few tokens or small heads, by 2^-16) and, below its smallest normal number, by 2^-39 of the largest factor (2^-25 where that is 2^14 or more)
   operands  x and w in float16 are exact but for 2^-39 of their columns' largest
   sums      float32 sums of K products: (2 K + 16) u, and the results' rounding
 """

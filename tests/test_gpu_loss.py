@@ -53,8 +53,9 @@ def check(x, w, targets, dloss, dlse, tied, scale=1.0, dtype=None, ref=None):
 SMALL = [(1, 1, 1), (1, 8, 8), (1, 64, 1000), (2, 3, 2), (3, 33, 17), (5, 40, 129), (64, 64, 64), (65, 128, 300), (70, 31, 257),
          (130, 256, 512), (257, 40, 1001), (300, 130, 777), (31, 2048, 96), (40, 2000, 264), (1, 1031, 4100),
          (1, 1, 16385), (1, 2048, 16401), (2, 33, 17001), (16, 100, 20003), (17, 100, 20003), (9, 523, 16388),
-         # more than 512 tokens: float16 operands of the gradients' products
          (512, 24, 70), (513, 8, 8), (515, 1, 9), (530, 33, 129), (700, 31, 257), (600, 200, 1001)]
+# more than 512 tokens and 2^29 of tokens * d * vocab: float16 operands of the gradients' products
+FLOAT16 = [(513, 1, 1046600), (530, 33, 30701), (513, 1024, 1024), (700, 2033, 377), (4000, 513, 263), (40000, 1031, 15), (600, 1000, 901)]
 
 
 @pytest.mark.parametrize("tied", [False, True])
@@ -65,6 +66,14 @@ def test_small(case, tied):
     again = check(x, w, targets.int(), dloss, None, tied)
     for a, b in zip(first, again):
         assert torch.equal(a, b)
+    check(x, w, targets, dloss, dlse, tied, scale=0.37, dtype=F32)
+
+
+@pytest.mark.parametrize("tied", [False, True])
+@pytest.mark.parametrize("case", FLOAT16, ids=lambda c: "x".join(map(str, c)))
+def test_float16_operands(case, tied):
+    x, w, targets, dloss, dlse = inputs(*case, tied=tied)
+    check(x, w, targets, dloss, None, tied)
     check(x, w, targets, dloss, dlse, tied, scale=0.37, dtype=F32)
 
 
@@ -91,7 +100,7 @@ def test_pieces_of_the_vocabulary(tied):
 @pytest.mark.parametrize("tied", [False, True])
 @pytest.mark.parametrize("T", [1, 16, 17, 33, 150, 600])
 def test_strides_and_existing_outputs(T, tied):
-    d, V = 72, 520
+    d, V = (72, 520) if T < 600 else (1000, 904)   # (float16 operands)
     x, w, targets, dloss, dlse = inputs(T, d, V, tied=tied, none=0.1 if T > 1 else 0.0)
     want = check(x, w, targets, dloss, dlse, tied)
     for pad, at in ((8, 8), (16, 0), (3, 1), (5, 4)):
@@ -113,7 +122,7 @@ def test_strides_and_existing_outputs(T, tied):
 @pytest.mark.parametrize("tied", [False, True])
 @pytest.mark.parametrize("T", [40, 140, 600])
 def test_rows_that_are_no_token(T, tied):
-    d, V = 64, 300
+    d, V = (64, 300) if T < 600 else (1000, 904)
     x, w, targets, dloss, dlse = inputs(T, d, V, tied=tied, none=0.3)
     targets[3], targets[4], targets[5] = -2**40, 2**40, 2**32   # (2^32 is 0 in 32 bits)
     there = (targets >= 0) & (targets < V)
@@ -139,7 +148,7 @@ def test_rows_that_are_no_token(T, tied):
 @pytest.mark.parametrize("T", [50, 200, 600])
 def test_ranges(T, tied):
     """Columns of very different size, large logits, certain tokens, gradients from 1e-30 to 1e30, zeros."""
-    d, V = 72, 400
+    d, V = (72, 400) if T < 600 else (1000, 904)
     x, w, targets, dloss, dlse = inputs(T, d, V, tied=tied, wide=True)
     check(x, w, targets, dloss, dlse, tied)
     x, w, targets, dloss, dlse = inputs(T, d, V, tied=tied, learnt=60.0)
@@ -160,7 +169,7 @@ def test_ranges(T, tied):
 @pytest.mark.parametrize("tied", [False, True])
 @pytest.mark.parametrize("T", [20, 80, 600])
 def test_what_is_not_finite_reaches_its_own_rows_alone(T, tied):
-    d, V = 64, 200
+    d, V = (64, 200) if T < 600 else (1000, 904)
     x, w, targets, dloss, dlse = inputs(T, d, V, tied=tied, none=0.0)
     want = check(x, w, targets, dloss, None, tied)
     x2 = x.clone()
@@ -189,7 +198,7 @@ def test_what_is_not_finite_reaches_its_own_rows_alone(T, tied):
 def test_float16_below_its_normal_numbers(tied):
     """One column of x is zero but for a token whose factor is 2^-30 of the largest: its entry is kept as 2^-16 or a little more, with half
     steps of 2^-25, 2^-9 of it; G and the result are off by 2^-11 and 2^-8 more."""
-    x, w, targets, dloss, _ = inputs(600, 64, 300, tied=tied, none=0.0)
+    x, w, targets, dloss, _ = inputs(600, 1000, 904, tied=tied, none=0.0)
     dloss = torch.full_like(dloss, 1.0)
     x[:, 5], x[7, 5], dloss[7] = 0.0, 1.5, 2.0**-30
     ref = Ref(x, w, targets, tied)
@@ -230,7 +239,7 @@ def test_rows_gradient_is_not_rounded_to_bf16(T, step):
     """float32 dx. Entries of G are off by `step` at most each (float16, or what two bf16 numbers leave out), at random signs, which the
     norm of the difference shows: below that of what their sizes add up to in squares, and what float32's sums (2 u a term, some
     thousand of them at random signs: 2^-17) leave."""
-    x, w, targets, dloss, _ = inputs(T, 256, 5000, none=0.0)
+    x, w, targets, dloss, _ = inputs(T, 256, 5000, none=0.0)   # (600 tokens: 2^29.5)
     ref = Ref(x, w, targets)
     dx, _, _, _ = ref.backward(dloss)
     _, lse = P.head_loss(x, w, targets)
@@ -248,7 +257,7 @@ def _all(x, w, targets, dloss, dlse, tied, stream=None):
 
 
 @pytest.mark.parametrize("tied", [False, True])
-@pytest.mark.parametrize("case", [(300, 64, 520), (90, 33, 301), (600, 64, 520), (600, 33, 301)], ids=str)
+@pytest.mark.parametrize("case", [(300, 64, 520), (90, 33, 301), (600, 1000, 904), (601, 999, 905)], ids=str)
 def test_other_streams_and_graphs(case, tied):
     args = inputs(*case, tied=tied)
     want = _all(*args, tied)
