@@ -179,7 +179,7 @@ __device__ __forceinline__ u32x4 to_half8(u32x4 v, const int *e, int more) {
 // are no token are zeros, and the work-groups past those of x make the rows' HeadRow.
 struct Padded {
   const bf16_t *x;
-  int64_t ld, rows, cols, rows8, cols8;
+  int64_t ld, rows, cols, rows8, cols8, ldto;
   uint16_t *half;
   bf16_t *copy, *again;   // (two copies)
   const uint32_t *top;
@@ -231,7 +231,7 @@ __global__ __launch_bounds__(kThreads) void pad_kernel(Padded p, skew_head_desc 
   }
 #pragma unroll
   for (int i = 0; i < kPadRows; i++) {
-    const int64_t row = row0 + (int64_t)i * side, to = row * p.cols8 + col;
+    const int64_t row = row0 + (int64_t)i * side, to = row * p.ldto + col;
     if (row >= p.rows8) break;
     if (p.half) *reinterpret_cast<u32x4 *>(p.half + to) = to_half8(v[i], e, less[i]);
     if (p.copy) *reinterpret_cast<u32x4 *>(p.copy + to) = v[i];
@@ -259,12 +259,16 @@ __global__ __launch_bounds__(kThreads) void pad_rows_kernel(Padded p, uint32_t *
 #pragma unroll 4
   for (int64_t col = threadIdx.x * 8; col < p.cols8; col += kThreads * 8) {
     const u32x4 v = load_chunk(x + col, cols - col);
-    *reinterpret_cast<u32x4 *>(p.half + row * p.cols8 + col) = to_half8(v, e, 0);
-    if (p.copy) *reinterpret_cast<u32x4 *>(p.copy + row * p.cols8 + col) = v;
+    *reinterpret_cast<u32x4 *>(p.half + row * p.ldto + col) = to_half8(v, e, 0);
+    if (p.copy) *reinterpret_cast<u32x4 *>(p.copy + row * p.ldto + col) = v;
   }
 }
 
 int64_t up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
+// The row stride of an operand in the workspace: whole 128-byte lines (3001 tokens, 32003 words of width 1031, a pass: 1067 us with chunks of 8,
+// 1000 with lines), and one more where rows would be multiples of 1024 bytes apart, on the same memory channels (8192 tokens, 16384 words of
+// width 1024, backward: 839 | 824, tied 855 | 822).
+int64_t lines(int64_t cols) { return up(cols, 64) + (up(cols, 64) % 512 == 0 ? 64 : 0); }
 bool chunks(const void *p, int64_t ld) { return ((uintptr_t)p & 15) == 0 && ld % 8 == 0; }
 bool tied(const skew_head_desc &h) { return (h.flags & SKEW_TRANSPOSE) != 0; }
 
@@ -280,12 +284,13 @@ bool splits(const skew_head_desc &h) {
 }
 struct HeadPlan {
   bool x_as_is, w_as_is;
-  int64_t d8, v8, piece, run;
+  int64_t d8, v8, ldd, piece, run;   // ldd: stride of rows of d in the workspace
 };
 HeadPlan head_plan(const skew_head_desc &h, bool backward) {
   HeadPlan p;
   p.d8 = up(h.d, 8);
   p.v8 = up(h.vocab, 8);
+  p.ldd = lines(h.d);
   p.x_as_is = chunks(h.x, h.ldx) && h.d % 8 == 0 && short_rows(kTileRows, h.ldx);
   p.w_as_is = chunks(h.w, h.ldw) && h.d % 8 == 0 && (tied(h) || h.vocab % 8 == 0) && short_rows(kTileRows, h.ldw);
   p.run = std::min(h.tokens, kRun);
@@ -302,6 +307,10 @@ HeadPlan head_plan(const skew_head_desc &h, bool backward) {
 int64_t pieces(const skew_head_desc &h, const HeadPlan &p) { return (h.vocab + p.piece - 1) / p.piece; }
 int64_t piece_cols(const skew_head_desc &h, const HeadPlan &p, int64_t v0) { return std::min(p.piece, h.vocab - v0); }
 
+// bytes of a piece of w in the workspace
+size_t words_bytes(const skew_head_desc &h, const HeadPlan &p) {
+  return 2 * (size_t)(tied(h) ? up(p.piece, 8) * p.ldd : p.d8 * lines(p.piece));
+}
 // w from word v0 on, as it is
 const bf16_t *words(const skew_head_desc &h, int64_t v0) {
   return static_cast<const bf16_t *>(h.w) + (tied(h) ? v0 * h.ldw : v0);
@@ -309,7 +318,7 @@ const bf16_t *words(const skew_head_desc &h, int64_t v0) {
 // x w of rows `rows` and the piece at v0 of `cols` words: from (a, lda) and w or its copy
 HeadProduct logits_of(const skew_head_desc &h, const HeadPlan &p, const void *a, int64_t lda, int64_t rows, int64_t v0, const void *copy) {
   const int64_t cols = piece_cols(h, p, v0), cols8 = tied(h) && !copy ? cols : up(cols, 8);   // (words in rows need no padding)
-  HeadProduct q = {a, copy ? copy : words(h, v0), lda, copy ? (tied(h) ? p.d8 : cols8) : h.ldw, rows, cols, p.d8, 0, cols8};
+  HeadProduct q = {a, copy ? copy : words(h, v0), lda, copy ? (tied(h) ? p.ldd : lines(cols)) : h.ldw, rows, cols, p.d8, 0, cols8};
   return q;
 }
 // (shapes alone)
@@ -327,8 +336,8 @@ int launch_pad(Padded p, const skew_head_desc &h, const Factors *f, hipStream_t 
 // the piece of w at v0, padded
 Padded piece_of(const skew_head_desc &h, const HeadPlan &p, int64_t v0, uint16_t *half, bf16_t *copy, const uint32_t *top) {
   const int64_t cols = piece_cols(h, p, v0), cols8 = up(cols, 8);
-  if (tied(h)) return {words(h, v0), h.ldw, cols, h.d, cols8, p.d8, half, copy, nullptr, top, 0, 0};
-  return {words(h, v0), h.ldw, h.d, cols, p.d8, cols8, half, copy, nullptr, top, 0, 0};
+  if (tied(h)) return {words(h, v0), h.ldw, cols, h.d, cols8, p.d8, p.ldd, half, copy, nullptr, top, 0, 0};
+  return {words(h, v0), h.ldw, h.d, cols, p.d8, cols8, lines(cols), half, copy, nullptr, top, 0, 0};
 }
 // f: also the largest of G's factors
 int launch_tops(const bf16_t *x, int64_t ld, int64_t rows, int64_t cols, uint32_t *top, const skew_head_desc &h, const Factors *f,
@@ -379,8 +388,8 @@ ForwardPlan forward_plan(const skew_head_desc &h) {
   Regions r;
   f.part = r.take((size_t)f.run * f.part_ld * sizeof(float2));
   f.sum = r.take((size_t)f.run * 4);
-  f.x = f.x_as_is ? 0 : r.take((size_t)f.run * f.d8 * 2);
-  f.w = f.w_as_is ? 0 : r.take((size_t)up(f.piece, 8) * f.d8 * 2);
+  f.x = f.x_as_is ? 0 : r.take((size_t)f.run * f.ldd * 2);
+  f.w = f.w_as_is ? 0 : r.take(words_bytes(h, f));
   f.bytes = r.at;
   return f;
 }
@@ -405,28 +414,28 @@ struct BackwardPlan : HeadPlan {
 // the three products of a piece
 HeadProduct dx_of(const skew_head_desc &h, const BackwardPlan &b, const void *g, const void *w16, int64_t v0) {
   const int64_t cols = piece_cols(h, b, v0), cols8 = up(cols, 8);
-  if (!b.split || !b.w_as_is) return {g, w16, b.ldg, tied(h) ? b.d8 : cols8, b.rows, h.d, cols8, 0, b.d8};
+  if (!b.split || !b.w_as_is) return {g, w16, b.ldg, tied(h) ? b.ldd : lines(cols), b.rows, h.d, cols8, 0, b.d8};
   return {g, words(h, v0), b.ldg, h.ldw, b.rows, h.d, tied(h) ? cols : cols8, 0, b.d8};   // (words in rows end with the contraction)
 }
 HeadProduct dw_of(const skew_head_desc &h, const BackwardPlan &b, const void *x16, const void *g, int64_t v0) {
   const int64_t cols = piece_cols(h, b, v0), cols8 = up(cols, 8);
-  if (tied(h)) return {g, x16, b.ldg, b.d8, cols, h.d, b.rows, cols8, b.d8};
-  return {x16, g, b.d8, b.ldg, h.d, cols, b.rows, b.d8, cols8};
+  if (tied(h)) return {g, x16, b.ldg, b.ldd, cols, h.d, b.rows, cols8, b.d8};
+  return {x16, g, b.ldd, b.ldg, h.d, cols, b.rows, b.d8, cols8};
 }
 int dx_mode(const skew_head_desc &h) { return tied(h) ? kForward : kBackward; }
 
 BackwardPlan backward_plan(const skew_head_desc &h) {
   BackwardPlan b;
   static_cast<HeadPlan &>(b) = head_plan(h, true);
-  b.ldg = up(b.piece, 8);
+  b.ldg = lines(b.piece);
   b.split = splits(h);
   b.rows = b.split ? 2 * h.tokens : h.tokens;
-  const size_t x = (size_t)h.tokens * b.d8 * 2, w = (size_t)b.ldg * b.d8 * 2;
+  const size_t x = (size_t)h.tokens * b.ldd * 2, w = words_bytes(h, b);
   Regions r;
   b.tops = r.take((size_t)(1 + 2 * b.d8) * 4);   // of G's factors, of x's columns, of w's
   b.row = r.take((size_t)h.tokens * sizeof(HeadRow));
   b.exponent = r.take((size_t)h.tokens * 4);
-  b.x16 = r.take((size_t)b.rows * b.d8 * 2);   // split: x twice, as it is
+  b.x16 = r.take((size_t)b.rows * b.ldd * 2);   // split: x twice, as it is
   b.x = b.x_as_is || b.split ? b.x16 : r.take(x);
   b.w16 = b.split ? 0 : r.take(w);
   b.w = b.w_as_is ? 0 : r.take(w);
@@ -479,11 +488,11 @@ int launch_head_loss(const skew_head_desc &h, float *loss, float *lse, char *ws,
     r.x = static_cast<const bf16_t *>(h.x) + t0 * h.ldx;
     r.targets = static_cast<const char *>(h.targets) + t0 * h.target_bytes;
     if (!f.x_as_is)
-      TRY(launch_pad({static_cast<const bf16_t *>(r.x), h.ldx, r.tokens, h.d, r.tokens, f.d8, nullptr, x_copy, nullptr, nullptr, 0, 0}, r, nullptr, s));
+      TRY(launch_pad({static_cast<const bf16_t *>(r.x), h.ldx, r.tokens, h.d, r.tokens, f.d8, f.ldd, nullptr, x_copy, nullptr, nullptr, 0, 0}, r, nullptr, s));
     int64_t at = 0;
     for (int64_t v0 = 0; v0 < h.vocab; v0 += f.piece) {
       if (!f.w_as_is) TRY(launch_pad(piece_of(h, f, v0, nullptr, w_copy, nullptr), r, nullptr, s));
-      const HeadProduct p = logits_of(h, f, f.x_as_is ? r.x : x_copy, f.x_as_is ? h.ldx : f.d8, r.tokens, v0, f.w_as_is ? nullptr : w_copy);
+      const HeadProduct p = logits_of(h, f, f.x_as_is ? r.x : x_copy, f.x_as_is ? h.ldx : f.ldd, r.tokens, v0, f.w_as_is ? nullptr : w_copy);
       TRY(launch_head_forward(mode_of(h), p, {c, r.targets, h.target_bytes, h.vocab, v0, part, f.part_ld, at, sum}, stream));
       at += head_parts(mode_of(h), p);
     }
@@ -508,13 +517,13 @@ int launch_head_loss_backward(const skew_head_desc &h, const float *lse, const f
   const Factors factors = {lse, dloss, dlse, b.split ? nullptr : coef, row, b.split ? nullptr : exponent, c};
   if (b.split) {
     bf16_t *copy = reinterpret_cast<bf16_t *>(x16);
-    TRY(launch_pad({x, h.ldx, h.tokens, h.d, h.tokens, b.d8, nullptr, copy, copy + h.tokens * b.d8, nullptr, 1, 0}, h, &factors, s));
+    TRY(launch_pad({x, h.ldx, h.tokens, h.d, h.tokens, b.d8, b.ldd, nullptr, copy, copy + h.tokens * b.ldd, nullptr, 1, 0}, h, &factors, s));
   } else {
     const int tops = (int)(1 + 2 * b.d8);
     zero_kernel<<<(tops + kThreads - 1) / kThreads, kThreads, 0, s>>>(coef, tops);
     TRY((int)hipGetLastError());
     TRY(launch_tops(x, h.ldx, h.tokens, h.d, x_top, h, &factors, s));
-    TRY(launch_pad({x, h.ldx, h.tokens, h.d, h.tokens, b.d8, x16, x_copy, nullptr, x_top, 1, 0}, h, &factors, s));
+    TRY(launch_pad({x, h.ldx, h.tokens, h.d, h.tokens, b.d8, b.ldd, x16, x_copy, nullptr, x_top, 1, 0}, h, &factors, s));
   }
   for (int64_t v0 = 0; v0 < h.vocab; v0 += b.piece) {
     const Padded p = piece_of(h, b, v0, b.split ? nullptr : w16, w_copy, w_top);
@@ -533,7 +542,7 @@ int launch_head_loss_backward(const skew_head_desc &h, const float *lse, const f
       TRY((int)hipGetLastError());
     }
     const void *w = b.split ? static_cast<const void *>(w_copy) : w16;
-    TRY(launch_head_grad(mode_of(h), logits_of(h, b, b.x_as_is ? h.x : x_copy, b.x_as_is ? h.ldx : b.d8, h.tokens, v0, w_copy),
+    TRY(launch_head_grad(mode_of(h), logits_of(h, b, b.x_as_is ? h.x : x_copy, b.x_as_is ? h.ldx : b.ldd, h.tokens, v0, w_copy),
                          {c, row, h.vocab, v0, g, b.ldg}, b.split, stream));
     HeadResult to_dx = {last ? dx : dx_sum, last ? lddx : b.d8, last ? dx_dtype : SKEW_F32, first ? nullptr : dx_sum, b.d8};
     HeadResult to_dw = {static_cast<bf16_t *>(dw) + (tied(h) ? v0 * lddw : v0), lddw, SKEW_BF16, nullptr, 0};

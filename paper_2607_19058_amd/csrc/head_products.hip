@@ -1,5 +1,5 @@
 // head_products.hip -- the gradients of the head's rows and weights: products of float16 operands on the matrix cores, or of bf16 ones, of which
-// G is the sum of two. Bound by the matrix cores: 8192 rows' gradient from 25152 words, width 2048, 704 us (1.20 PFLOP/s; words in rows 656, 1.29);
+// G is the sum of two. With tiles of 256 x 256 the compiler spills 5 to 18 registers, outside the main loop. Bound by the matrix cores: 8192 rows' gradient from 25152 words, width 2048, 704 us (1.20 PFLOP/s; words in rows 656, 1.29);
 // 24576 words' gradient from 8192 rows 594 us (1.39).
 #include "head_internal.h"
 #include "product_tiles.h"

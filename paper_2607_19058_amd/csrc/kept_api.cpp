@@ -9,6 +9,7 @@ using namespace moe;
 
 namespace {
 
+int64_t lines(int64_t cols) { return (cols + 63) / 64 * 64; }   // a row stride in whole 128-byte lines
 int64_t blocks_of(int64_t cols) { return (cols + SKEW_KEPT_BLOCK - 1) / SKEW_KEPT_BLOCK; }
 // (a work-group takes 128 blocks, and the device's grid some 2^24 work-groups)
 bool kept_ok(int64_t rows, int64_t cols) {
@@ -40,7 +41,7 @@ struct KeptPlan {
 };
 KeptPlan kept_plan(const skew_rows *r, const skew_product_desc *p) {
   const int64_t places = r->tokens * r->k, kept = p->flags & SKEW_GATHER ? r->tokens : places;
-  KeptPlan k = {p->out_dtype == SKEW_F32 ? kept : places, 32 * blocks_of(p->n), 0, 0, 0};
+  KeptPlan k = {p->out_dtype == SKEW_F32 ? kept : places, lines(p->n), 0, 0, 0};
   k.rest = pad256((size_t)k.rows * k.ldx * 2);
   if (p->out_dtype == SKEW_F32) {
     skew_product_desc q = *p;
@@ -48,7 +49,7 @@ KeptPlan kept_plan(const skew_rows *r, const skew_product_desc *p) {
     k.bytes = k.rest + product_grad_f32_scratch(*r, q);
   } else {
     const bool as_is = ((uintptr_t)p->y & 15) == 0 && p->ldy % 8 == 0 && p->m % 8 == 0 && short_rows(kTileRows, p->ldy);
-    if (!as_is) k.ldd = (p->m + 7) / 8 * 8;
+    if (!as_is) k.ldd = lines(p->m);
     k.bytes = k.rest + (size_t)places * k.ldd * 2;
   }
   return k;
@@ -109,10 +110,10 @@ int skew_expert_matmul_grad_kept(const skew_rows *r, const skew_product_desc *p,
   if (workspace == nullptr) return SKEW_EINVAL;
   const bool gather = (p->flags & SKEW_GATHER) != 0;
   char *rest = static_cast<char *>(workspace) + k.rest;
-  // whole blocks: the columns past a row's end are 0, as their codes are
+  const int64_t whole = 32 * blocks_of(p->n);   // the columns past a row's end are 0, as their codes are
   int e = gather && p->out_dtype == SKEW_BF16
-              ? launch_restore_places(*r, codes, scales, k.ldx, workspace, k.ldx, stream)
-              : launch_restore8(codes, scales, k.rows, k.ldx, workspace, SKEW_BF16, k.ldx, stream);
+              ? launch_restore_places(*r, codes, scales, whole, workspace, k.ldx, stream)
+              : launch_restore8(codes, scales, k.rows, whole, workspace, SKEW_BF16, k.ldx, stream);
   if (e != (int)hipSuccess) return SKEW_EHIP;
   if (p->out_dtype == SKEW_F32) {
     skew_product_desc q = *p;
