@@ -13,8 +13,8 @@ struct HeadRow {
   int32_t target;
 };
 
-// One product of the head on the tiles of product_tiles.h. Operands are padded to chunks of 8 in both directions; rows, cols and n8, m8
-// say where the result ends and where its operands do.
+// One product of the head on the tiles of product_tiles.h. Operands are padded to chunks of 8 where a chunk may pass their end: rows and cols say
+// where the result ends, pad_rows and pad_cols where its operands do.
 struct HeadProduct {
   const void *a, *b;          // kForward: a rows, b [K x cols]; kBackward: b [cols x K]; kOuter: a [K x rows], b [K x cols]
   int64_t lda, ldb;
@@ -47,8 +47,8 @@ inline double head_time(const HeadTile &t, int64_t n, int64_t K) {
   return ((double)(n / t.slots) * t.full + (left ? t.lone + (t.full - t.lone) * more : 0.0)) * (double)(K + 128) / 2176 + 4;
 }
 
-// Forward: of each row and each run of 128 (or 64, ...) columns that a wave has, the largest base-2 exponent and the sum
-// of the powers relative to it; the logit of the row's target.
+// Forward: of each row and each run of 128 (or 64) columns that a wave has, the largest base-2 exponent and the sum
+// of the powers relative to it; the product of the row and its target's word.
 struct HeadForward {
   float c;                    // scale log2(e)
   const void *targets;
