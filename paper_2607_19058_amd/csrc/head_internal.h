@@ -93,6 +93,7 @@ struct HeadResult {
   const int32_t *row_exponent;   // NULL: *coef
   const uint32_t *coef;
   int32_t split, fold;
+  const HeadRow *token;       // NULL, or of each row: one that is no token gets zeros, whatever b holds
 };
 size_t head_result_scratch(int mode, const HeadProduct &p, bool fold);
 int launch_head_result(int mode, const HeadProduct &p, const HeadResult &r, char *ws, void *stream);

@@ -547,6 +547,7 @@ int launch_head_loss_backward(const skew_head_desc &h, const float *lse, const f
     HeadResult to_dx = {last ? dx : dx_sum, last ? lddx : b.d8, last ? dx_dtype : SKEW_F32, first ? nullptr : dx_sum, b.d8};
     HeadResult to_dw = {static_cast<bf16_t *>(dw) + (tied(h) ? v0 * lddw : v0), lddw, SKEW_BF16, nullptr, 0};
     to_dx.split = to_dw.split = to_dx.fold = b.split;
+    to_dx.token = row;
     if (!b.split) {
       to_dx.top = w_top;
       to_dx.row_exponent = exponent;

@@ -57,12 +57,16 @@ struct ResultOp {
     for (int i = 0; i < FM; i++) {
       const int64_t row = row0 + i * 16;
       const int er = (r.by_row ? power(row, rows) : 0) + (HALF && r.row_exponent && row < rows ? r.row_exponent[row] : 0);
+      const bool none = r.token && row < rows && r.token[row].target < 0;
 #pragma unroll
       for (int j = 0; j < FN; j++) {
         const int64_t n = row < rows ? cols - col0 - j * 16 : 0;
         f32x4 v;
 #pragma unroll
-        for (int q = 0; q < 4; q++) v[q] = HALF ? __builtin_ldexpf(acc[i][j][q], r.by_row ? er : er + ec[j][q]) : acc[i][j][q];
+        for (int q = 0; q < 4; q++) {
+          v[q] = HALF ? __builtin_ldexpf(acc[i][j][q], r.by_row ? er : er + ec[j][q]) : acc[i][j][q];
+          if (none) v[q] = 0.0f;
+        }
         if (r.prev && n > 0) {   // (rows of whole fours)
           v += *reinterpret_cast<const f32x4 *>(r.prev + row * r.ldprev + col0 + j * 16);
         }
@@ -106,9 +110,11 @@ __global__ __launch_bounds__(256) void join_kernel(HeadResult r, int64_t rows, i
     }
   }
   const int64_t n = cols - p.col;
+  const bool none = r.token && r.token[p.row].target < 0;
   const int of_g = r.split ? 0 : r.row_exponent ? r.row_exponent[p.row] : factor_exponent(*r.coef);
 #pragma unroll
   for (int q = 0; q < 8; q++) {
+    if (none) v[q] = 0.0f;
     if (q < n && !r.split) v[q] = __builtin_ldexpf(v[q], of_g + half_exponent(r.top[r.by_row ? p.row : p.col + q]));
     if (r.prev && q < n) v[q] += r.prev[p.row * r.ldprev + p.col + q];
   }
@@ -183,6 +189,7 @@ HeadResult result_of(const HeadResult &r, int64_t row, int64_t col) {
   if (r.prev) q.prev = r.prev + row * r.ldprev + col;
   if (r.top) q.top = r.top + (r.by_row ? row : col);
   if (r.row_exponent) q.row_exponent = r.row_exponent + row;
+  if (r.token) q.token = r.token + row;
   return q;
 }
 int64_t part_ld(int64_t cols) { return (cols + 7) / 8 * 8; }
