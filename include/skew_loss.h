@@ -28,8 +28,10 @@ extern "C" {
  * computed in pieces of the vocabulary. G is rounded before these products: up to 512 tokens, or 2^29 of
  * tokens * d * vocab, to the sum of two bf16 numbers, which leaves out 2^-16 of an entry; with more, G and the operand beside it are float16 numbers (11 bits, 8 times finer than bf16) times powers
  * of two: of G's rows, by their tokens' larger factor, and of the columns of x and w (their d), by their largest values. So an entry
- * of G below 2^-28 of its row's factor, or one of x or w below 2^-29 of its column's largest, keeps fewer bits, down to none 11 powers
- * further (for dw, of x times its token's factor). dx and dw are rounded once more.
+ * of G below 2^-27 of its row's factor, or one of x or w below 2^-28 of its column's largest, can keep fewer bits, down to none 11 powers
+ * further (for dw, of x times its token's factor). For dw a word of which every entry of G is below 2^-31 sqrt(tokens) of its row's factor is
+ * computed again beside a power of two of its own (words between that and 2^-30 sqrt(tokens) may be), so that rare words keep 11 bits of
+ * their largest entry; calls with many such words take longer. dx and dw are rounded once more.
  * NaN and infinities in x and w give NaN where they reach; a logit of +inf gives NaN.
  *   x      bf16 [tokens x d], row stride ldx;  0 <= tokens <= SKEW_MAX_LOSS_TOKENS;  1 <= d <= SKEW_MAX_HEAD_WIDTH
  *   w      bf16: column v of [d x vocab] is word v; with SKEW_TRANSPOSE row v of [vocab x d], as an embedding's

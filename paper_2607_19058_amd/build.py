@@ -8,7 +8,8 @@ CSRC = os.path.join(HERE, "csrc")
 LIB_PATH = os.path.join(HERE, "libskewadam.so")
 SOURCES = ["skew_kernels.hip", "skew_plan.cpp", "skew_api.cpp", "moe_route.hip", "moe_order.hip", "moe_tokens.hip",
            "moe_product.hip", "moe_api.cpp", "kept_rows.hip", "kept_product.hip", "kept_api.cpp",
-           "head_loss.hip", "head_few.hip", "head_logits.hip", "head_products.hip", "head_api.cpp"]
+           "head_loss.hip", "head_few.hip", "head_logits.hip", "head_products.hip", "head_rare.hip",
+           "head_api.cpp"]
 
 
 def hipcc() -> str:

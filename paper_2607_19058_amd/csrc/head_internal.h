@@ -75,6 +75,7 @@ struct HeadGrad {
   int64_t vocab, col0;
   uint16_t *g;
   int64_t ldg;
+  uint32_t *word_top;         // of each word of the vocabulary, bits of the largest magnitude in G as it is kept (split: not wanted)
 };
 int launch_head_grad(int mode, const HeadProduct &p, const HeadGrad &g, bool split, void *stream);
 
@@ -104,6 +105,31 @@ constexpr int kHalfTop = 14;
 __host__ __device__ inline int half_exponent(uint32_t top) { return (int)(top >> 23) - 127 - kHalfTop; }
 // The same of a row of G, from its larger factor: an entry is at most twice it.
 __host__ __device__ inline int factor_exponent(uint32_t top) { return half_exponent(top) + 1; }
+
+// Float16 has no room for a word that is rare for every token: beside the tokens' factors its entries of G are below the smallest normal
+// number, and at last 0. A piece's words whose largest entry is below rare_top() are computed a second time, with a power of two of
+// their own (head_rare.hip). Below the normal numbers an entry is off by 2^-25.8 on average (2^-24 / sqrt(12)): the tokens together by
+// 2^-25.8 sqrt(tokens), which is 2^-8.8 of rare_top(), about a rounding to bf16 of the word's largest entry.
+inline float rare_top(int64_t tokens) { return 7.62939453125e-06f * __builtin_sqrtf((float)tokens); }   // 2^-17 sqrt(tokens)
+struct HeadRare {
+  const void *x, *x16;        // x as it is [tokens x d8], and as the gradients take it
+  int64_t ldx, ldx16, tokens, d, d8;
+  const void *w;              // bf16, the piece's words, anywhere
+  int64_t ldw, words;         // and how many
+  int32_t tied;
+  float c;
+  const HeadRow *row;
+  const uint32_t *word_top, *x_top, *coef;   // of the piece's words, ..
+  int64_t word0;              // the piece's first word
+  int32_t *list;              // [1 + words]: how many are rare, and which, in order
+  void *copy;                 // their words in w's layout, rows of d8 values, or d8 rows
+  int64_t ldcopy;
+  uint16_t *g;                // and their G
+  int64_t ldg;
+  void *dw;                   // the piece's first word in dw
+  int64_t lddw;
+};
+int launch_head_rare(const HeadRare &r, void *stream);
 
 // The calls of skew_loss.h, after their checks.
 size_t head_forward_scratch(const skew_head_desc &h);

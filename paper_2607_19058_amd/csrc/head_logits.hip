@@ -96,6 +96,31 @@ struct ForwardOp {
   }
 };
 
+// The largest of 16 lanes' bits, in each of them.
+__device__ __forceinline__ uint32_t row_max(uint32_t x) {
+  x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x128, 0xF, 0xF, true));   // the lanes 8, 4, 2, 1 further on
+  x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x124, 0xF, 0xF, true));
+  x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x122, 0xF, 0xF, true));
+  return max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x121, 0xF, 0xF, true));
+}
+// The largest of each column of a wave joins `to`, which is at the wave's first column: `left` columns there. Of the 4 FN columns that
+// 16 lanes share, lane i takes i and (FN = 8) 16 + i.
+template <int FN>
+__device__ __forceinline__ void put_tops(const float (&top)[FN][4], uint32_t *to, int64_t left) {
+  const int lane = threadIdx.x & 63;
+  uint32_t mine[FN / 4] = {};
+#pragma unroll
+  for (int s = 0; s < 4 * FN; s++) {
+    const uint32_t m = row_max(__float_as_uint(top[s >> 2][s & 3]));
+    if ((lane & 15) == (s & 15)) mine[s >> 4] = m;
+  }
+#pragma unroll
+  for (int i = 0; i < FN / 4; i++) {
+    const int col = (i * 4 + ((lane & 15) >> 2)) * 16 + (lane >> 4) * 4 + (lane & 3);
+    if (mine[i] && col < left) atomicMax(to + col, mine[i]);
+  }
+}
+
 // SPLIT: the gradient is the sum of two bf16 numbers, its upper half, cut off, and the rest, which is exact before its own rounding.
 template <bool SPLIT>
 struct GradOp {
@@ -124,6 +149,7 @@ struct GradOp {
     const int mine = (int)(left < 16 * FN ? left : 16 * FN) - (lane >> 4) * 4;
     auto part = [&](auto PART) {
       typedef uint16_t __attribute__((may_alias)) u16;
+      float top[FN][4] = {};   // of the lane's columns, over its rows
 #pragma unroll
       for (int i = 0; i < FM; i++) {
         const int64_t row = row_w + i * 16 + (lane & 15);
@@ -137,7 +163,9 @@ struct GradOp {
           for (int q = 0; q < 4; q++) {
             float v = r.both * exp2_(__builtin_fmaf(acc[i][j][q], g.c, -r.l2));
             if (!whole && j * 16 + q >= mine) v = 0.0f;
-            h[q] = bits<PART>(token ? v : 0.0f);   // (a row that is no token may hold NaN)
+            v = token ? v : 0.0f;   // (a row that is no token may hold NaN)
+            h[q] = bits<PART>(v);
+            if (!SPLIT) top[j][q] = fmaxf(top[j][q], fabsf(v));
           }
           put_room<FN>(room, i, j, make_uint2(h[0] | h[1] << 16, h[2] | h[3] << 16));
         }
@@ -149,8 +177,10 @@ struct GradOp {
           const float v = __builtin_fmaf(r.both - r.one, exp2_(d), r.one * expm1f(d * 0.6931471805599453f));
           const int row16 = i * 16 + (lane & 15);
           *reinterpret_cast<u16 *>(room + row16 * (FN * 32) + ((k >> 3) ^ (row16 & 7)) * 16 + (k & 7) * 2) = (uint16_t)bits<PART>(v);
+          if (!SPLIT) atomicMax(g.word_top + r.target, __float_as_uint(v) & 0x7FFFFFFFu);
         }
       }
+      if (!SPLIT) put_tops<FN>(top, g.word_top + g.col0 + col_w, left);
       store_room<FM, FN, true>(room, g.g + (row_w + PART * t.r1) * g.ldg + col_w, g.ldg, t.r1 - row_w, t.c1 - col_w);
     };
     part(std::integral_constant<int, 0>());

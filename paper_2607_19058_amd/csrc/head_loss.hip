@@ -6,7 +6,8 @@
 //
 // G is rounded before the products that it enters. In bf16 that would be an error of the size of the results' own rounding; in float16,
 // which the matrix cores take at the same rate, it is an eighth. That needs float16 x and w: w is converted piece by
-// piece (a pass of its bytes, twice read and once written), x once. For few tokens, see BackwardPlan.
+// piece (a pass of its bytes, twice read and once written), x once. For few tokens, see BackwardPlan. Words that float16 has no room for beside
+// the tokens' factors get their part of dw from a second pass (head_rare.hip).
 //
 // What bounds them (benchmark's head, 2048 x 50304): one token's loss, w's bytes (206 MB in 32 us from the Infinity Cache, 35 from memory); 8192
 // tokens, the matrix cores at the power limit (clocks of 1.75 to 2.0 of 2.4 GHz): forward 1.40 ms and the logits again 1.57 (1.2 and 1.08 PFLOP/s;
@@ -408,7 +409,8 @@ ForwardPlan forward_plan(const skew_head_desc &h) {
 struct BackwardPlan : HeadPlan {
   bool split;
   int64_t rows;   // of G
-  size_t tops, row, exponent, x16, x, w16, w, g, dx, rest, bytes;
+  int64_t top_count;   // bits of largest magnitudes: of G's factors, x's columns, w's; of each word's G
+  size_t tops, row, exponent, list, x16, x, w16, w, g, dx, rest, bytes;
   int64_t ldg;
 };
 // the three products of a piece
@@ -432,9 +434,11 @@ BackwardPlan backward_plan(const skew_head_desc &h) {
   b.rows = b.split ? 2 * h.tokens : h.tokens;
   const size_t x = (size_t)h.tokens * b.ldd * 2, w = words_bytes(h, b);
   Regions r;
-  b.tops = r.take((size_t)(1 + 2 * b.d8) * 4);   // of G's factors, of x's columns, of w's
+  b.top_count = b.split ? 0 : 1 + 2 * b.d8 + b.v8;
+  b.tops = r.take((size_t)b.top_count * 4);
   b.row = r.take((size_t)h.tokens * sizeof(HeadRow));
   b.exponent = r.take((size_t)h.tokens * 4);
+  b.list = b.split ? 0 : r.take((size_t)(1 + b.piece) * 4);
   b.x16 = r.take((size_t)b.rows * b.ldd * 2);   // split: x twice, as it is
   b.x = b.x_as_is || b.split ? b.x16 : r.take(x);
   b.w16 = b.split ? 0 : r.take(w);
@@ -506,7 +510,7 @@ int launch_head_loss_backward(const skew_head_desc &h, const float *lse, const f
   const BackwardPlan b = backward_plan(h);
   hipStream_t s = static_cast<hipStream_t>(stream);
   const float c = log2_scale(h);
-  uint32_t *coef = reinterpret_cast<uint32_t *>(ws + b.tops), *x_top = coef + 1, *w_top = x_top + b.d8;
+  uint32_t *coef = reinterpret_cast<uint32_t *>(ws + b.tops), *x_top = coef + 1, *w_top = x_top + b.d8, *word_top = w_top + b.d8;
   HeadRow *row = reinterpret_cast<HeadRow *>(ws + b.row);
   uint16_t *x16 = reinterpret_cast<uint16_t *>(ws + b.x16), *w16 = reinterpret_cast<uint16_t *>(ws + b.w16),
            *g = reinterpret_cast<uint16_t *>(ws + b.g);
@@ -519,8 +523,7 @@ int launch_head_loss_backward(const skew_head_desc &h, const float *lse, const f
     bf16_t *copy = reinterpret_cast<bf16_t *>(x16);
     TRY(launch_pad({x, h.ldx, h.tokens, h.d, h.tokens, b.d8, b.ldd, nullptr, copy, copy + h.tokens * b.ldd, nullptr, 1, 0}, h, &factors, s));
   } else {
-    const int tops = (int)(1 + 2 * b.d8);
-    zero_kernel<<<(tops + kThreads - 1) / kThreads, kThreads, 0, s>>>(coef, tops);
+    zero_kernel<<<(unsigned)((b.top_count + kThreads - 1) / kThreads), kThreads, 0, s>>>(coef, (int)b.top_count);
     TRY((int)hipGetLastError());
     TRY(launch_tops(x, h.ldx, h.tokens, h.d, x_top, h, &factors, s));
     TRY(launch_pad({x, h.ldx, h.tokens, h.d, h.tokens, b.d8, b.ldd, x16, x_copy, nullptr, x_top, 1, 0}, h, &factors, s));
@@ -543,7 +546,7 @@ int launch_head_loss_backward(const skew_head_desc &h, const float *lse, const f
     }
     const void *w = b.split ? static_cast<const void *>(w_copy) : w16;
     TRY(launch_head_grad(mode_of(h), logits_of(h, b, b.x_as_is ? h.x : x_copy, b.x_as_is ? h.ldx : b.ldd, h.tokens, v0, w_copy),
-                         {c, row, h.vocab, v0, g, b.ldg}, b.split, stream));
+                         {c, row, h.vocab, v0, g, b.ldg, word_top}, b.split, stream));
     HeadResult to_dx = {last ? dx : dx_sum, last ? lddx : b.d8, last ? dx_dtype : SKEW_F32, first ? nullptr : dx_sum, b.d8};
     HeadResult to_dw = {static_cast<bf16_t *>(dw) + (tied(h) ? v0 * lddw : v0), lddw, SKEW_BF16, nullptr, 0};
     to_dx.split = to_dw.split = to_dx.fold = b.split;
@@ -557,6 +560,10 @@ int launch_head_loss_backward(const skew_head_desc &h, const float *lse, const f
     }
     TRY(launch_head_result(dx_mode(h), dx_of(h, b, g, w, v0), to_dx, ws + b.rest, stream));
     TRY(launch_head_result(kOuter, dw_of(h, b, x16, g, v0), to_dw, ws + b.rest, stream));
+    if (!b.split)   // (the float16 words and G are no longer read)
+      TRY(launch_head_rare({b.x_as_is ? h.x : x_copy, x16, b.x_as_is ? h.ldx : b.ldd, b.ldd, h.tokens, h.d, b.d8, words(h, v0), h.ldw,
+                            piece_cols(h, b, v0), tied(h), c, row, word_top + v0, x_top, coef, v0, reinterpret_cast<int32_t *>(ws + b.list), w16,
+                            tied(h) ? b.ldd : lines(b.piece), g, b.ldg, to_dw.y, lddw}, stream));
   }
   return (int)hipSuccess;
 }
