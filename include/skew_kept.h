@@ -24,7 +24,7 @@ extern "C" {
  * (by s at most where |x| > 127.5 2^121). Codes past the end of a row are 0. bf16 rows: 1.03 of 2 bytes a value. */
 #define SKEW_KEPT_BLOCK 32
 
-/* Errors of each: SKEW_EINVAL, SKEW_EHIP. rows * ceil(cols / 32) < 2^31; dtype SKEW_BF16 or SKEW_F32. */
+/* Errors of each: SKEW_EINVAL, SKEW_EHIP. rows * ceil(cols / 32) <= 2^31 - 128; dtype SKEW_BF16 or SKEW_F32. */
 int skew_keep8(const void *x, int32_t dtype, int64_t rows, int64_t cols, int64_t ldx, int8_t *codes, uint8_t *scales,
                void *stream);
 int skew_restore8(const int8_t *codes, const uint8_t *scales, int64_t rows, int64_t cols, void *x, int32_t dtype,

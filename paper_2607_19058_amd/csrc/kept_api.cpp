@@ -11,9 +11,10 @@ namespace {
 
 int64_t lines(int64_t cols) { return (cols + 63) / 64 * 64; }   // a row stride in whole 128-byte lines
 int64_t blocks_of(int64_t cols) { return (cols + SKEW_KEPT_BLOCK - 1) / SKEW_KEPT_BLOCK; }
-// (a work-group takes 128 blocks, and the device's grid some 2^24 work-groups)
+// A work-group of 256 threads takes 128 blocks, and a launch has fewer than 2^32 threads.
+constexpr int64_t kMostBlocks = ((int64_t)1 << 31) - 128;
 bool kept_ok(int64_t rows, int64_t cols) {
-  return rows >= 0 && cols_ok(cols) && rows <= kMaxPlaces / blocks_of(cols);
+  return rows >= 0 && cols_ok(cols) && rows <= kMostBlocks / blocks_of(cols);
 }
 constexpr int64_t kTileRows = 256;   // rows that a lane's 32-bit offset spans
 bool codes_ok(const int8_t *codes, const uint8_t *scales) {

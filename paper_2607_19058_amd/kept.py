@@ -23,6 +23,7 @@ from .moe import (BF16, F32, GATHER, MAX_COLS, MAX_PLACES, Kept8, ProductDesc, _
 from .skewadam import lib
 
 BLOCK = 32
+MAX_BLOCKS = 2**31 - 128
 KINDS = {"relu": 0, "silu": 1, "gelu_tanh": 2}
 
 # names that include/skew_kept.h declares (checked by the CPU test suite)
@@ -64,8 +65,8 @@ def _lib():
 def _size(rows, cols):
     """Blocks of a row."""
     blocks = -(-cols // BLOCK)
-    if not 1 <= cols <= MAX_COLS or rows * blocks > MAX_PLACES:
-        raise ValueError(f"{rows} x {cols} values are not supported (rows of 1 to {MAX_COLS}, fewer than 2^31 blocks of {BLOCK})")
+    if not 1 <= cols <= MAX_COLS or rows * blocks > MAX_BLOCKS:
+        raise ValueError(f"{rows} x {cols} values are not supported (rows of 1 to {MAX_COLS}, at most 2^31 - 128 blocks of {BLOCK})")
     return blocks
 
 
