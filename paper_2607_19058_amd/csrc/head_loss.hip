@@ -463,10 +463,15 @@ size_t head_forward_scratch(const skew_head_desc &h) { return forward_plan(h).by
 size_t head_backward_scratch(const skew_head_desc &h) { return backward_plan(h).bytes; }
 
 int launch_fill_zero(void *dw, int64_t rows, int64_t cols, int64_t ld, void *stream) {
-  const int64_t grid = (rows * ((cols + 7) / 8) + kThreads - 1) / kThreads;
-  if (grid > kMostGroups) return (int)hipErrorInvalidConfiguration;
-  fill_zero_kernel<<<(unsigned)grid, kThreads, 0, static_cast<hipStream_t>(stream)>>>(static_cast<bf16_t *>(dw), rows, cols, ld);
-  return (int)hipGetLastError();
+  const int64_t per = (cols + 7) / 8, most = (kMostGroups - 1) * kThreads / per;   // rows of a launch (a row has 2^21 chunks at most)
+  for (int64_t row = 0; row < rows; row += most) {
+    const int64_t n = std::min(most, rows - row);
+    fill_zero_kernel<<<(unsigned)((n * per + kThreads - 1) / kThreads), kThreads, 0, static_cast<hipStream_t>(stream)>>>(
+        static_cast<bf16_t *>(dw) + row * ld, n, cols, ld);
+    const int e = (int)hipGetLastError();
+    if (e != (int)hipSuccess) return e;
+  }
+  return (int)hipSuccess;
 }
 
 #define TRY(call)                             \
