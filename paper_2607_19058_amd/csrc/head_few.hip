@@ -97,12 +97,10 @@ __global__ __launch_bounds__(64 * kWaves, 4) void few_kernel(Few p, HeadForward 
   for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
   sum *= exp2_(m - or_zero(top));
   for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
-  if ((tid & 31) == 0 && row < p.rows) f.part[row * f.part_ld + blockIdx.x] = make_float2(top, sum);
+  if ((tid & 31) == 0 && row < p.rows) f.part[row * f.part_ld + blockIdx.x] = HeadPair{top, sum};
 }
 
 }  // namespace
-
-int64_t head_few_parts(int64_t cols) { return (cols + 127) / 128; }
 
 int launch_head_few(const HeadProduct &p, const HeadForward &f, void *stream) {
   const Few q = {static_cast<const bf16_t *>(p.a), static_cast<const bf16_t *>(p.b), p.lda, p.ldb, p.rows, p.cols, p.K};

@@ -49,22 +49,24 @@ inline double head_time(const HeadTile &t, int64_t n, int64_t K) {
 
 // Forward: of each row and each run of 128 (or 64) columns that a wave has, the largest base-2 exponent and the sum
 // of the powers relative to it; the product of the row and its target's word.
+struct alignas(8) HeadPair {
+  float top, sum;
+};
 struct HeadForward {
   float c;                    // scale log2(e)
   const void *targets;
   int32_t target_bytes;
   int64_t vocab, col0;        // of the whole; the first column of this product
-  float2 *part;               // [rows x part_ld], runs of this product from part_at on
+  HeadPair *part;             // [rows x part_ld], runs of this product from part_at on
   int64_t part_ld, part_at;
   float *target_sum;          // [rows]: <x, w_y>
 };
-int head_parts(int mode, const HeadProduct &p);   // runs that a row's columns fall into
 int launch_head_forward(int mode, const HeadProduct &p, const HeadForward &f, void *stream);
 
 // The same (kForward) for up to 16 rows: any position and alignment, K and cols as they are (no padding); 32 rows of b lie within 2^31
 // bytes. One pair a row and work-group.
 constexpr int64_t kFewRows = 16;
-int64_t head_few_parts(int64_t cols);
+inline int64_t head_few_parts(int64_t cols) { return (cols + 127) / 128; }
 int launch_head_few(const HeadProduct &p, const HeadForward &f, void *stream);
 
 // Backward: G of this product's columns, float16 [rows x ldg]; or, split, as the sum of two bf16 numbers, [2 rows x ldg]: all rows of the
@@ -96,15 +98,14 @@ struct HeadResult {
   int32_t split, fold;
   const HeadRow *token;       // NULL, or of each row: one that is no token gets zeros, whatever b holds
 };
-size_t head_result_scratch(int mode, const HeadProduct &p, bool fold);
 int launch_head_result(int mode, const HeadProduct &p, const HeadResult &r, char *ws, void *stream);
 
 // Exponents of what is kept in float16: a value whose largest magnitude has the bits `top` is kept times 2^-exponent, so
 // that the largest lies in [2^14, 2^15).
 constexpr int kHalfTop = 14;
-__host__ __device__ inline int half_exponent(uint32_t top) { return (int)(top >> 23) - 127 - kHalfTop; }
+constexpr int half_exponent(uint32_t top) { return (int)(top >> 23) - 127 - kHalfTop; }
 // The same of a row of G, from its larger factor: an entry is at most twice it.
-__host__ __device__ inline int factor_exponent(uint32_t top) { return half_exponent(top) + 1; }
+constexpr int factor_exponent(uint32_t top) { return half_exponent(top) + 1; }
 
 // Float16 has no room for a word that is rare for every token: beside the tokens' factors its entries of G are below the smallest normal
 // number, and at last 0. A piece's words whose largest entry is below rare_top() are computed a second time, with a power of two of

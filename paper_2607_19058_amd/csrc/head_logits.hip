@@ -6,7 +6,7 @@
 // place, which leaves through LDS as float16. Per logit that is some 32 cycles of a SIMD (16 of them the exponential's), 8200 for a tile of
 // 256 x 256, beside its 64 K / 32 matrix instructions of 16. 8192 rows, 50304 words of width 2048: forward 1.38 ms, with words in rows 1.48; the
 // gradient 1.58 (matrix cores busy 59% at 1.9 GHz). 1024 rows: 195 us. One row: 32 us for w's 206 MB.
-#include "head_internal.h"
+#include "head_plan.h"
 #include "product_tiles.h"
 
 namespace moe {
@@ -91,7 +91,7 @@ struct ForwardOp {
       s *= exp2_(m - (top == -INFINITY ? 0.0f : top));
       s += __shfl_xor(s, 16);
       s += __shfl_xor(s, 32);
-      if (lane < 16 && row < t.r1) f.part[row * f.part_ld + f.part_at + col_w / (16 * FN)] = make_float2(top, s);
+      if (lane < 16 && row < t.r1) f.part[row * f.part_ld + f.part_at + col_w / (16 * FN)] = HeadPair{top, s};
     }
   }
 };
@@ -198,38 +198,6 @@ __global__ __launch_bounds__(256, per_unit(FM, FN, KS)) void logits_kernel(Produ
 
 constexpr int64_t kMostGroups = 1 << 24;
 
-// Which tile: the one that takes the least time. Where the last round of large tiles would be nearly empty, the columns past the whole
-// rounds (first to last) get tiles of their own.
-struct Choice {
-  int tile;
-  int64_t first;   // columns that `tile` takes; the rest has `rest`
-  int rest;
-};
-double best_of(int mode, int64_t rows, int64_t cols, int64_t K, int *tile) {
-  double least = 1e300;
-  for (int i = 0; i < kHeadTiles; i++) {
-    const HeadTile t = head_tile(mode == kBackward, i);
-    const double time = head_time(t, head_count(t, rows, cols), K);
-    if (time < least) {
-      least = time;
-      *tile = i;
-    }
-  }
-  return least;
-}
-Choice choose_logits(int mode, const HeadProduct &p) {
-  Choice c = {0, p.cols, 0};
-  const double all = best_of(mode, p.rows, p.cols, p.K, &c.tile);
-  const HeadTile large = head_tile(mode == kBackward, 0);
-  const int64_t down = (p.rows + large.rows - 1) / large.rows;
-  const int64_t first = head_count(large, p.rows, p.cols) / large.slots * large.slots / down * large.cols;
-  if (first > 0 && first < p.cols) {
-    int rest;
-    const double time = head_time(large, first / large.cols * down, p.K) + best_of(mode, p.rows, p.cols - first, p.K, &rest);
-    if (time < 0.97 * all) c = {0, first, rest};
-  }
-  return c;
-}
 // The columns of a product from `at` on, `cols` of them (at: a multiple of every tile's).
 HeadProduct columns(int mode, const HeadProduct &p, int64_t at, int64_t cols) {
   HeadProduct q = p;
@@ -272,18 +240,14 @@ int launch_tiles(const HeadProduct &p, const Op &op, int tile, void *stream) {
     default: return launch_one<Op, MODE, 2, 4, 4 / S, S>(p, op, tile, stream);
   }
 }
-int runs(int mode, int tile, int64_t cols) {   // of a wave's columns
-  const int w = head_tile(mode == kBackward, tile).cols;
-  return (int)((cols + w - 1) / w) * 2;
-}
-ForwardOp shifted(const ForwardOp &op, int mode, const Choice &c) {
+ForwardOp shifted(const ForwardOp &op, int mode, const LogitsChoice &c) {
   ForwardOp o = op;
   o.f.col0 += c.first;
-  o.f.part_at += runs(mode, c.tile, c.first);
+  o.f.part_at += head_runs(mode, c.tile, c.first);
   return o;
 }
 template <bool SPLIT>
-GradOp<SPLIT> shifted(const GradOp<SPLIT> &op, int, const Choice &c) {
+GradOp<SPLIT> shifted(const GradOp<SPLIT> &op, int, const LogitsChoice &c) {
   GradOp<SPLIT> o = op;
   o.g.col0 += c.first;
   o.g.g += c.first;
@@ -291,7 +255,7 @@ GradOp<SPLIT> shifted(const GradOp<SPLIT> &op, int, const Choice &c) {
 }
 template <class Op, int MODE>
 int launch_mode(const HeadProduct &p, const Op &op, void *stream) {
-  const Choice c = choose_logits(MODE, p);
+  const LogitsChoice c = choose_logits(MODE, p);
   if (c.first == p.cols) return launch_tiles<Op, MODE>(p, op, c.tile, stream);
   const int e = launch_tiles<Op, MODE>(columns(MODE, p, 0, c.first), op, c.tile, stream);
   if (e != (int)hipSuccess) return e;
@@ -300,10 +264,6 @@ int launch_mode(const HeadProduct &p, const Op &op, void *stream) {
 
 }  // namespace
 
-int head_parts(int mode, const HeadProduct &p) {
-  const Choice c = choose_logits(mode, p);
-  return runs(mode, c.tile, c.first) + (c.first < p.cols ? runs(mode, c.rest, p.cols - c.first) : 0);
-}
 int launch_head_forward(int mode, const HeadProduct &p, const HeadForward &f, void *stream) {
   const ForwardOp op = {f};
   return mode == kBackward ? launch_mode<ForwardOp, kBackward>(p, op, stream) : launch_mode<ForwardOp, kForward>(p, op, stream);

@@ -14,12 +14,11 @@
 // the library's plain product, with the logits written, 1.55 ms), dx 1.42 (the library 1.22), dw 1.26 (the library 1.68).
 #include <algorithm>
 
-#include "head_internal.h"
+#include "head_plan.h"
 
 namespace moe {
 namespace {
 
-enum { kForward = 0, kBackward = 1, kOuter = 3 };   // as in product_tiles.h
 constexpr int kThreads = 256;
 constexpr int64_t kMostGroups = 1 << 24;   // of a launch
 
@@ -56,7 +55,7 @@ __device__ __forceinline__ Pair joined(Pair a, Pair b) {
   return {top, a.s * __builtin_amdgcn_exp2f(a.m - base) + b.s * __builtin_amdgcn_exp2f(b.m - base)};
 }
 template <int W>
-__global__ __launch_bounds__(kThreads) void loss_kernel(skew_head_desc h, float c, const float2 *part, int64_t ld, int parts,
+__global__ __launch_bounds__(kThreads) void loss_kernel(skew_head_desc h, float c, const HeadPair *part, int64_t ld, int parts,
                                                         const float *target_sum, float *loss, float *lse) {
   constexpr int kRowsHere = kThreads / 64 / W;
   __shared__ Pair held[kThreads / 64];
@@ -66,8 +65,8 @@ __global__ __launch_bounds__(kThreads) void loss_kernel(skew_head_desc h, float 
   if (t < h.tokens) {
 #pragma unroll 4
     for (int i = in; i < parts; i += 64 * W) {
-      const float2 q = part[t * ld + i];
-      p = joined(p, {q.x, q.y});
+      const HeadPair q = part[t * ld + i];
+      p = joined(p, {q.top, q.sum});
     }
   }
   for (int o = 32; o > 0; o >>= 1) p = joined(p, {__shfl_xor(p.m, o), __shfl_xor(p.s, o)});
@@ -85,7 +84,7 @@ __global__ __launch_bounds__(kThreads) void loss_kernel(skew_head_desc h, float 
     loss[t] = token ? (float)(all - (double)h.scale * (double)target_sum[t]) : 0.0f;
   }
 }
-int launch_loss(const skew_head_desc &h, float c, const float2 *part, int64_t ld, int parts, const float *target_sum, float *loss, float *lse,
+int launch_loss(const skew_head_desc &h, float c, const HeadPair *part, int64_t ld, int parts, const float *target_sum, float *loss, float *lse,
                 hipStream_t s) {
   if (h.tokens <= 64) loss_kernel<4><<<(unsigned)h.tokens, kThreads, 0, s>>>(h, c, part, ld, parts, target_sum, loss, lse);
   else loss_kernel<1><<<(unsigned)((h.tokens + 3) / 4), kThreads, 0, s>>>(h, c, part, ld, parts, target_sum, loss, lse);
@@ -265,66 +264,6 @@ __global__ __launch_bounds__(kThreads) void pad_rows_kernel(Padded p, uint32_t *
   }
 }
 
-int64_t up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
-// The row stride of an operand in the workspace: whole 128-byte lines (3001 tokens, 32003 words of width 1031, a pass: 1067 us with chunks of 8,
-// 1000 with lines), and one more where rows would be multiples of 1024 bytes apart, on the same memory channels (8192 tokens, 16384 words of
-// width 1024, backward: 839 | 824, tied 855 | 822).
-int64_t lines(int64_t cols) { return up(cols, 64) + (up(cols, 64) % 512 == 0 ? 64 : 0); }
-bool chunks(const void *p, int64_t ld) { return ((uintptr_t)p & 15) == 0 && ld % 8 == 0; }
-bool tied(const skew_head_desc &h) { return (h.flags & SKEW_TRANSPOSE) != 0; }
-
-// What is the same in both calls: which operands the tiles take as they are, and pieces of the vocabulary (of kPieceStep columns,
-// the last one of what is left).
-constexpr int64_t kTileRows = 256, kPieceStep = 256, kMaxPiece = 1 << 21;
-constexpr int64_t kPieceBytes = (int64_t)512 << 20;   // of G, and of a copy of w (8192 tokens, 50304 words: 128 MiB 5.91 ms, 256 6.02, 512 5.72, 1024 5.71)
-constexpr int64_t kRun = 16384;                       // rows of a forward launch, whose pairs are held
-// Whether G is split (see BackwardPlan).
-bool splits(const skew_head_desc &h) {
-  constexpr int64_t kRows = 512, kSmall = (int64_t)1 << 29;   // (tokens * d is below 2^42)
-  return h.tokens <= kRows || h.tokens * h.d <= kSmall / h.vocab;
-}
-struct HeadPlan {
-  bool x_as_is, w_as_is;
-  int64_t d8, v8, ldd, piece, run;   // ldd: stride of rows of d in the workspace
-};
-HeadPlan head_plan(const skew_head_desc &h, bool backward) {
-  HeadPlan p;
-  p.d8 = up(h.d, 8);
-  p.v8 = up(h.vocab, 8);
-  p.ldd = lines(h.d);
-  p.x_as_is = chunks(h.x, h.ldx) && h.d % 8 == 0 && short_rows(kTileRows, h.ldx);
-  p.w_as_is = chunks(h.w, h.ldw) && h.d % 8 == 0 && (tied(h) || h.vocab % 8 == 0) && short_rows(kTileRows, h.ldw);
-  p.run = std::min(h.tokens, kRun);
-  if (!backward && p.w_as_is) {
-    p.piece = h.vocab;
-  } else {
-    const int64_t wide = std::max(p.d8, backward ? h.tokens * (splits(h) ? 2 : 1) : 0);   // rows of G, columns of w
-    int64_t most = std::min(std::max(kPieceBytes / (2 * wide), kPieceStep), kMaxPiece);
-    const int64_t n = (h.vocab + most - 1) / most;
-    p.piece = std::min(up((h.vocab + n - 1) / n, kPieceStep), p.v8);
-  }
-  return p;
-}
-int64_t pieces(const skew_head_desc &h, const HeadPlan &p) { return (h.vocab + p.piece - 1) / p.piece; }
-int64_t piece_cols(const skew_head_desc &h, const HeadPlan &p, int64_t v0) { return std::min(p.piece, h.vocab - v0); }
-
-// bytes of a piece of w in the workspace
-size_t words_bytes(const skew_head_desc &h, const HeadPlan &p) {
-  return 2 * (size_t)(tied(h) ? up(p.piece, 8) * p.ldd : p.d8 * lines(p.piece));
-}
-// w from word v0 on, as it is
-const bf16_t *words(const skew_head_desc &h, int64_t v0) {
-  return static_cast<const bf16_t *>(h.w) + (tied(h) ? v0 * h.ldw : v0);
-}
-// x w of rows `rows` and the piece at v0 of `cols` words: from (a, lda) and w or its copy
-HeadProduct logits_of(const skew_head_desc &h, const HeadPlan &p, const void *a, int64_t lda, int64_t rows, int64_t v0, const void *copy) {
-  const int64_t cols = piece_cols(h, p, v0), cols8 = tied(h) && !copy ? cols : up(cols, 8);   // (words in rows need no padding)
-  HeadProduct q = {a, copy ? copy : words(h, v0), lda, copy ? (tied(h) ? p.ldd : lines(cols)) : h.ldw, rows, cols, p.d8, 0, cols8};
-  return q;
-}
-// (shapes alone)
-int mode_of(const skew_head_desc &h) { return tied(h) ? kBackward : kForward; }
-
 // f: also the rows of G (p.x are the tokens' rows)
 int launch_pad(Padded p, const skew_head_desc &h, const Factors *f, hipStream_t s) {
   const int64_t strips = (p.cols8 / 8 + kThreads - 1) / kThreads, side = kThreads / pad_wide(p.cols8) * kPadRows;
@@ -337,8 +276,9 @@ int launch_pad(Padded p, const skew_head_desc &h, const Factors *f, hipStream_t 
 // the piece of w at v0, padded
 Padded piece_of(const skew_head_desc &h, const HeadPlan &p, int64_t v0, uint16_t *half, bf16_t *copy, const uint32_t *top) {
   const int64_t cols = piece_cols(h, p, v0), cols8 = up(cols, 8);
-  if (tied(h)) return {words(h, v0), h.ldw, cols, h.d, cols8, p.d8, p.ldd, half, copy, nullptr, top, 0, 0};
-  return {words(h, v0), h.ldw, h.d, cols, p.d8, cols8, lines(cols), half, copy, nullptr, top, 0, 0};
+  const bf16_t *w = reinterpret_cast<const bf16_t *>(words(h, v0));
+  if (tied(h)) return {w, h.ldw, cols, h.d, cols8, p.d8, p.ldd, half, copy, nullptr, top, 0, 0};
+  return {w, h.ldw, h.d, cols, p.d8, cols8, lines(cols), half, copy, nullptr, top, 0, 0};
 }
 // f: also the largest of G's factors
 int launch_tops(const bf16_t *x, int64_t ld, int64_t rows, int64_t cols, uint32_t *top, const skew_head_desc &h, const Factors *f,
@@ -352,108 +292,8 @@ int launch_tops(const bf16_t *x, int64_t ld, int64_t rows, int64_t cols, uint32_
   return (int)hipGetLastError();
 }
 
-// a region of the workspace
-struct Regions {
-  size_t at = 0;
-  size_t take(size_t bytes) {
-    const size_t here = at;
-    at += pad256(bytes);
-    return here;
-  }
-};
-
 // x w as they are
 HeadProduct whole_of(const skew_head_desc &h) { return {h.x, h.w, h.ldx, h.ldw, h.tokens, h.vocab, h.d, 0, h.vocab}; }
-
-struct ForwardPlan : HeadPlan {
-  bool few;
-  int64_t part_ld;
-  size_t part, sum, x, w, bytes;
-};
-ForwardPlan forward_plan(const skew_head_desc &h) {
-  ForwardPlan f;
-  static_cast<HeadPlan &>(f) = head_plan(h, false);
-  // One row and words at odd positions, in pieces copied for the tiles | as they are (us): width 2048, 8001 words 34 | 46, 16001 47 | 44,
-  // 24001 59 | 52, 50257 117 | 77; width 512, 50257 36 | 26; width 4096, 16001 79 | 78.
-  f.few = !f.w_as_is && !tied(h) && h.tokens <= kFewRows && h.vocab >= 16384 && (h.d == 1 || short_rows(kTileRows, h.ldw));
-  if (f.few) f.x_as_is = f.w_as_is = true;   // (whatever their alignment)
-  // rows of the last run may be fewer, and their tiles narrower
-  f.part_ld = f.few ? head_few_parts(h.vocab) : 0;
-  const int64_t last = h.tokens % f.run ? h.tokens % f.run : f.run;
-  for (const int64_t rows : {f.run, last}) {
-    if (f.few) break;
-    int64_t ld = 0;
-    for (int64_t v0 = 0; v0 < h.vocab; v0 += f.piece) ld += head_parts(mode_of(h), logits_of(h, f, nullptr, 0, rows, v0, nullptr));
-    f.part_ld = std::max(f.part_ld, ld);
-  }
-  Regions r;
-  f.part = r.take((size_t)f.run * f.part_ld * sizeof(float2));
-  f.sum = r.take((size_t)f.run * 4);
-  f.x = f.x_as_is ? 0 : r.take((size_t)f.run * f.ldd * 2);
-  f.w = f.w_as_is ? 0 : r.take(words_bytes(h, f));
-  f.bytes = r.at;
-  return f;
-}
-
-// Up to 512 tokens the bytes of w decide. Then G is the sum of two bf16 numbers, and w enters its product as it is; with more,
-// where the products decide, w is converted to float16 (see above), which takes its bytes four times more. Where tokens, width and words
-// together are few, the conversions' launches decide. Backward calls, us, float16 | split:
-//   tokens                             1           64          256         512         768          1024
-//   50304 words of width 2048          345 | 203   380 | 241   494 | 402   589 | 595   709 | 829    813 | 1010
-//   the same, tied                     377 | 207   404 | 235   486 | 379   605 | 594   723 | 808    836 | 1008
-//   32003 words of width 1031          141 | 103   156 | 128   209 | 233   306 | 304   343 | 385    398 | 484
-//   8192 words of width 1024            61 |  48    68 |  49    73 |  62    86 |  90   106 | 114    118 | 134
-//   tokens x width x words             2048x128x512   1024x512x1024   2048x256x1024   4096x128x1024   1024x1024x1024   1024x256x4096
-//     (2^27, 2^29, .., 2^30)           43 | 37        54 | 48         53 | 48         55 | 58         58 | 55          58 | 61
-//     tied                             49 | 37        58 | 49         58 | 47         60 | 58         66 | 58          67 | 62
-struct BackwardPlan : HeadPlan {
-  bool split;
-  int64_t rows;   // of G
-  int64_t top_count;   // bits of largest magnitudes: of G's factors, x's columns, w's; of each word's G
-  size_t tops, row, exponent, list, x16, x, w16, w, g, dx, rest, bytes;
-  int64_t ldg;
-};
-// the three products of a piece
-HeadProduct dx_of(const skew_head_desc &h, const BackwardPlan &b, const void *g, const void *w16, int64_t v0) {
-  const int64_t cols = piece_cols(h, b, v0), cols8 = up(cols, 8);
-  if (!b.split || !b.w_as_is) return {g, w16, b.ldg, tied(h) ? b.ldd : lines(cols), b.rows, h.d, cols8, 0, b.d8};
-  return {g, words(h, v0), b.ldg, h.ldw, b.rows, h.d, tied(h) ? cols : cols8, 0, b.d8};   // (words in rows end with the contraction)
-}
-HeadProduct dw_of(const skew_head_desc &h, const BackwardPlan &b, const void *x16, const void *g, int64_t v0) {
-  const int64_t cols = piece_cols(h, b, v0), cols8 = up(cols, 8);
-  if (tied(h)) return {g, x16, b.ldg, b.ldd, cols, h.d, b.rows, cols8, b.d8};
-  return {x16, g, b.ldd, b.ldg, h.d, cols, b.rows, b.d8, cols8};
-}
-int dx_mode(const skew_head_desc &h) { return tied(h) ? kForward : kBackward; }
-
-BackwardPlan backward_plan(const skew_head_desc &h) {
-  BackwardPlan b;
-  static_cast<HeadPlan &>(b) = head_plan(h, true);
-  b.ldg = lines(b.piece);
-  b.split = splits(h);
-  b.rows = b.split ? 2 * h.tokens : h.tokens;
-  const size_t x = (size_t)h.tokens * b.ldd * 2, w = words_bytes(h, b);
-  Regions r;
-  b.top_count = b.split ? 0 : 1 + 2 * b.d8 + b.v8;
-  b.tops = r.take((size_t)b.top_count * 4);
-  b.row = r.take((size_t)h.tokens * sizeof(HeadRow));
-  b.exponent = r.take((size_t)h.tokens * 4);
-  b.list = b.split ? 0 : r.take((size_t)(1 + b.piece) * 4);
-  b.x16 = r.take((size_t)b.rows * b.ldd * 2);   // split: x twice, as it is
-  b.x = b.x_as_is || b.split ? b.x16 : r.take(x);
-  b.w16 = b.split ? 0 : r.take(w);
-  b.w = b.w_as_is ? 0 : r.take(w);
-  b.g = r.take((size_t)b.rows * b.ldg * 2);
-  b.dx = pieces(h, b) > 1 ? r.take((size_t)h.tokens * b.d8 * 4) : 0;
-  size_t rest = 0;
-  for (int64_t v0 = 0; v0 < h.vocab; v0 += b.piece) {
-    rest = std::max(rest, head_result_scratch(dx_mode(h), dx_of(h, b, nullptr, nullptr, v0), b.split));
-    rest = std::max(rest, head_result_scratch(kOuter, dw_of(h, b, nullptr, nullptr, v0), false));
-  }
-  b.rest = r.take(rest);
-  b.bytes = r.at;
-  return b;
-}
 
 float log2_scale(const skew_head_desc &h) { return (float)((double)h.scale * 1.4426950408889634); }
 
@@ -484,7 +324,7 @@ int launch_head_loss(const skew_head_desc &h, float *loss, float *lse, char *ws,
   const ForwardPlan f = forward_plan(h);
   hipStream_t s = static_cast<hipStream_t>(stream);
   const float c = log2_scale(h);
-  float2 *part = reinterpret_cast<float2 *>(ws + f.part);
+  HeadPair *part = reinterpret_cast<HeadPair *>(ws + f.part);
   float *sum = reinterpret_cast<float *>(ws + f.sum);
   bf16_t *x_copy = reinterpret_cast<bf16_t *>(ws + f.x), *w_copy = reinterpret_cast<bf16_t *>(ws + f.w);
   if (f.few) {

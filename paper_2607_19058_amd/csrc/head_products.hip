@@ -1,7 +1,7 @@
 // head_products.hip -- the gradients of the head's rows and weights: products of float16 operands on the matrix cores, or of bf16 ones, of which
 // G is the sum of two. With tiles of 256 x 256 the compiler spills 5 to 18 registers, outside the main loop. Bound by the matrix cores: 8192 rows' gradient from 25152 words, width 2048, 704 us (1.20 PFLOP/s; words in rows 656, 1.29);
 // 24576 words' gradient from 8192 rows 594 us (1.39).
-#include "head_internal.h"
+#include "head_plan.h"
 #include "product_tiles.h"
 
 namespace moe {
@@ -124,54 +124,6 @@ __global__ __launch_bounds__(256) void join_kernel(HeadResult r, int64_t rows, i
 
 constexpr int64_t kMostGroups = 1 << 24;
 
-// Which tile, and how many work-groups share a contraction (their parts go through memory, and join_kernel adds them up: a launch, and
-// the bytes at some 4 TB/s).
-struct Choice {
-  int tile, parts;
-};
-double best_of(int mode, int64_t rows, int64_t cols, int64_t K, Choice *c) {
-  double least = 1e300;
-  for (const int tile : {0, 1, 3}) {
-    const HeadTile t = head_tile(mode == kBackward, tile);
-    const int64_t n = head_count(t, rows, cols);
-    for (const int parts : {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 48, 64}) {
-      if (parts > 1 && (K / parts < 128 || n * parts > 2 * t.slots)) break;
-      const double time = head_time(t, n * parts, K / parts) + (parts > 1 ? 4 + (double)parts * rows * cols * 4 * 2 / 4e6 : 0);
-      if (time < least) {
-        least = time;
-        *c = {tile, parts};
-      }
-    }
-  }
-  return least;
-}
-// Where the last round of large tiles would be nearly empty, or the last row or column of them, what lies past the whole ones is
-// a product of its own.
-struct Plan {
-  Choice main, rest;
-  int64_t rows, cols;   // of main
-};
-Plan plan_result(int mode, const HeadProduct &p, bool fold) {
-  Plan s = {{0, 1}, {0, 0}, p.rows, p.cols};
-  double least = 0.97 * best_of(mode, p.rows, p.cols, p.K, &s.main);
-  const HeadTile t = head_tile(mode == kBackward, 0);
-  const int64_t down = (p.rows + t.rows - 1) / t.rows, across = (p.cols + t.cols - 1) / t.cols, whole = down * across / t.slots * t.slots;
-  auto cut = [&](int64_t rows, int64_t cols) {   // (one of them all)
-    if (rows == 0 || cols == 0 || (rows >= p.rows && cols >= p.cols) || (fold && rows < p.rows)) return;
-    Plan c = {{0, 1}, {0, 1}, rows, cols};
-    const double time = best_of(mode, rows, cols, p.K, &c.main) +
-                        best_of(mode, rows < p.rows ? p.rows - rows : rows, rows < p.rows ? cols : p.cols - cols, p.K, &c.rest);
-    if (time < least) {
-      least = time;
-      s = c;
-    }
-  };
-  cut(whole / across * t.rows, p.cols);
-  cut(p.rows, whole / down * t.cols);
-  cut(p.rows / t.rows * t.rows, p.cols);
-  cut(p.rows, p.cols / t.cols * t.cols);
-  return s;
-}
 // The part of a product from (row, col) on, and of its result.
 HeadProduct part_of(int mode, const HeadProduct &p, int64_t row, int64_t col, int64_t rows, int64_t cols) {
   HeadProduct q = p;
@@ -192,10 +144,8 @@ HeadResult result_of(const HeadResult &r, int64_t row, int64_t col) {
   if (r.token) q.token = r.token + row;
   return q;
 }
-int64_t part_ld(int64_t cols) { return (cols + 7) / 8 * 8; }
-
 template <bool HALF, int MODE, int FM, int FN, int NS, int KS>
-int launch_one(const HeadProduct &p, const HeadResult &r, Choice c, char *ws, void *stream) {
+int launch_one(const HeadProduct &p, const HeadResult &r, ResultChoice c, char *ws, void *stream) {
   ProductArgs a = {};
   a.x = static_cast<const bf16_t *>(p.a);   // (float16 bits)
   a.w = static_cast<const bf16_t *>(p.b);
@@ -228,7 +178,7 @@ int launch_one(const HeadProduct &p, const HeadResult &r, Choice c, char *ws, vo
   return (int)hipGetLastError();
 }
 template <bool HALF, int MODE>
-int launch_choice(const HeadProduct &p, const HeadResult &r, Choice c, char *ws, void *stream) {
+int launch_choice(const HeadProduct &p, const HeadResult &r, ResultChoice c, char *ws, void *stream) {
   constexpr int S = MODE == kBackward ? 2 : 1;
   if (c.tile == 0) return launch_one<HALF, MODE, 8, 8, 4 / S, S>(p, r, c, ws, stream);
   if (c.tile == 1) return launch_one<HALF, MODE, 4, 8, 3, 1>(p, r, c, ws, stream);
@@ -236,26 +186,15 @@ int launch_choice(const HeadProduct &p, const HeadResult &r, Choice c, char *ws,
 }
 template <bool HALF, int MODE>
 int launch_mode(const HeadProduct &p, const HeadResult &r, char *ws, void *stream) {
-  const Plan s = plan_result(MODE, p, r.fold);
+  const ResultPlan s = plan_result(MODE, p, r.fold);
   if (s.rest.parts == 0) return launch_choice<HALF, MODE>(p, r, s.main, ws, stream);
   const int e = launch_choice<HALF, MODE>(part_of(MODE, p, 0, 0, s.rows, s.cols), r, s.main, ws, stream);
   if (e != (int)hipSuccess) return e;
   const int64_t row = s.rows < p.rows ? s.rows : 0, col = s.rows < p.rows ? 0 : s.cols;
   return launch_choice<HALF, MODE>(part_of(MODE, p, row, col, p.rows - row, p.cols - col), result_of(r, row, col), s.rest, ws, stream);
 }
-size_t scratch_of(const Choice &c, int64_t rows, int64_t cols, bool fold) {
-  return c.parts > 1 || fold ? pad256((size_t)c.parts * (size_t)rows * (size_t)part_ld(cols) * 4) : 0;
-}
-
 }  // namespace
 
-size_t head_result_scratch(int mode, const HeadProduct &p, bool fold) {
-  const Plan s = plan_result(mode, p, fold);
-  const size_t main = scratch_of(s.main, s.rows, s.cols, fold);
-  if (s.rest.parts == 0) return main;
-  const size_t rest = scratch_of(s.rest, s.rows < p.rows ? p.rows - s.rows : p.rows, s.rows < p.rows ? p.cols : p.cols - s.cols, fold);
-  return main > rest ? main : rest;
-}
 int launch_head_result(int mode, const HeadProduct &p, const HeadResult &r, char *ws, void *stream) {
   if (r.split) {
     if (mode == kOuter) return launch_mode<false, kOuter>(p, r, ws, stream);

@@ -8,6 +8,13 @@
 
 namespace moe {
 
+// How the operands of a product lie: a (rows of the result) and b (its columns), contiguous in the contraction or along the result.
+//   kForward   a in the contraction, b along the result
+//   kBackward  both in the contraction
+//   kWeights   both along the result; the contraction is an expert's places, and a's rows are looked up
+//   kOuter     both along the result; the contraction is the rows of both, from Tile::first on
+enum { kForward = 0, kBackward = 1, kWeights = 2, kOuter = 3 };
+
 constexpr int kMaxDigit = 9;             // radix digits of the sort: up to 512 bins
 
 // Number of bits that hold 0 .. x.

@@ -15,13 +15,6 @@
 namespace moe {
 namespace {
 
-// How the operands lie: a (rows of the result) and b (its columns), contiguous in the contraction or along the result.
-//   kForward   a in the contraction, b along the result
-//   kBackward  both in the contraction
-//   kWeights   both along the result; the contraction is an expert's places, and a's rows are looked up
-//   kOuter     both along the result; the contraction is the rows of both, from Tile::first on
-enum { kForward = 0, kBackward = 1, kWeights = 2, kOuter = 3 };
-
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
