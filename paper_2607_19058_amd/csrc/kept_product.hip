@@ -61,19 +61,13 @@ int launch_tiles(const ProductArgs &a, int64_t n, int64_t m, hipStream_t s) {
   grad_kernel<FM, FN, NS><<<(unsigned)grid, 256, 0, s>>>(a, GradOp<CHUNKS>{n, m});
   return (int)hipGetLastError();
 }
-// Which tile: us with tiles of 256 x 256, 128 x 256 and 64 x 128, and from rows in bf16 (moe_product.hip, which looks them up):
-//   32 experts of 2048 x 8192, uneven rows, mean   32   314 227 292 | 275          8 experts of 1024 x 1024, 1024 rows   42  37  35 | 32
-//                                                 128   388 343 420 | 394          8 of 256 x 1024, 250                  21  21  21 | 15
-//                                                 256   483 486 565 | 505          8 of 2048 x 2048, 2048               126 144 192 | 122
-//                                                 512   677 713 880 | 710          4 of 2048 x 8192, 2048               223 250 331 | 237
-//   16 experts of 2765 x 1031, 563 rows                 108  99 116 | 115          128 of 512 x 2048, 128               105 103 131 | 110
 template <bool CHUNKS>
 int launch(const ProductArgs &a, int64_t n, int64_t m, hipStream_t s) {
-  const int64_t rows = a.places / a.experts;   // of an expert, on average
-  auto tiles = [&](int64_t bm, int64_t bn) { return a.experts * ((n + bm - 1) / bm) * ((m + bn - 1) / bn); };
-  if ((rows >= 384 && tiles(256, 256) >= 2048) || (rows >= 1024 && tiles(256, 256) >= 512)) return launch_tiles<8, 8, 4, CHUNKS>(a, n, m, s);
-  if (tiles(128, 256) >= 512) return launch_tiles<4, 8, 3, CHUNKS>(a, n, m, s);
-  return launch_tiles<2, 4, 4, CHUNKS>(a, n, m, s);
+  switch (kept_tile(a.places, a.experts, n, m)) {
+    case 0: return launch_tiles<8, 8, 4, CHUNKS>(a, n, m, s);
+    case 1: return launch_tiles<4, 8, 3, CHUNKS>(a, n, m, s);
+    default: return launch_tiles<2, 4, 4, CHUNKS>(a, n, m, s);
+  }
 }
 
 }  // namespace
