@@ -56,7 +56,8 @@ int skew_expert_act(const skew_act_desc *d, void *stream);
 int skew_expert_act_backward(const skew_act_desc *d, void *stream);
 
 /* skew_expert_matmul_grad() with the rows of x kept: tokens (SKEW_GATHER) or tokens * k rows of n values. p->x is NULL and
- * p->ldx not read; p->out_dtype is the type of d (p->y). The values are restored into the workspace, exactly; its size (host only)
+ * p->ldx not read; p->out_dtype is the type of d (p->y). The values are restored into the workspace, exactly, in bf16: a row for each place (tokens * k, also with
+ * SKEW_GATHER), with a float32 d for each kept row. Rows of d at other than 16-byte positions are copied too. The size (host only)
  * depends on shapes and on d's alignment and stride.
  * Errors: SKEW_EINVAL, SKEW_ENOSPACE, SKEW_EHIP. */
 int skew_expert_matmul_grad_kept_bytes(const skew_rows *r, const skew_product_desc *p, size_t *bytes);

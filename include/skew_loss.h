@@ -46,7 +46,15 @@ typedef struct skew_head_desc {
   int32_t reserved;
 } skew_head_desc;
 
-/* Scratch bytes of the two calls (host only; they depend on shapes, strides and alignments). Errors: SKEW_EINVAL. */
+/* Scratch bytes of the two calls (host only; they depend on shapes, strides and alignments). Errors: SKEW_EINVAL. Copies are made of x or w where
+ * its rows do not begin at 16-byte positions or are more than 4178004 elements apart, or d (of an untied w, vocab too) is no multiple of 8.
+ *   forward   8 bytes for each row and 64 or 128 words (1/16 or 1/32 of the logits in bf16), of 16384 tokens at most;
+ *             the copies: x of these tokens, and 512 MiB of w at most
+ *   backward  G of a piece of the vocabulary in 16 bits, or twice 16: 512 MiB, or 256 words where that is more (512 bytes a token, or
+ *             1024), at most; where G is float16, the piece's words in float16; x in 16 bits, once or twice; the copies of x and of the piece's
+ *             words; float32 dx where there are several pieces; float32 parts of dx and dw that several work-groups share.
+ *             Rows in the workspace are up to 136 elements longer than their values, pieces up to 256 words longer.
+ *             8192 tokens, 50304 words of width 2048: 647 MB (bf16 logits: 824); 4096 tokens: 704 (412), as all of G is one piece. */
 int skew_head_loss_bytes(const skew_head_desc *h, size_t *bytes);
 int skew_head_loss_backward_bytes(const skew_head_desc *h, size_t *bytes);
 

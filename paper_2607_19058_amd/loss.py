@@ -77,7 +77,8 @@ def head_loss(x, w, targets, *, tied=False, scale=1.0, stream=None):
 
     ``x`` bf16 (T, d); ``w`` bf16 (d, V), or with ``tied`` the embedding's table (V, d). lse is the logits' log-sum-exp, loss = lse
     less the target's logit. A target outside [0, V) is no token: both are 0, and its row of x may hold anything. The
-    logits are never held: besides x and w the call needs some 1/32 of their bf16 bytes for at most 16384 tokens at a time.
+    logits are never held: the scratch is 1/32 to 1/16 of their bf16 bytes, of at most 16384 tokens; where rows do not begin at 16-byte
+    positions, or d or V is no multiple of 8, also copies of these tokens' rows and of w (512 MiB of it at most).
     """
     import torch
     _no_autograd(x, w)
@@ -96,8 +97,15 @@ def head_loss(x, w, targets, *, tied=False, scale=1.0, stream=None):
 
 def head_loss_backward(x, w, targets, lse, dloss, *, dlse=None, tied=False, scale=1.0, dtype=None, out=None, stream=None):
     """Gradients of `head_loss`: (dx (T, d) in bf16 or ``dtype``, dw bf16 in w's shape) from those of loss and (``dlse``) of lse,
-    float32 (T), and the lse that it gave. The logits are computed again, in pieces of the vocabulary whose gradient (16 bits, or for
-    few tokens twice 16, at most 512 MiB) is held. ``out`` takes an existing tensor for dw, such as the gradient that an optimizer was given."""
+    float32 (T), and the lse that it gave. A target outside [0, V) gives a row of zeros in dx and nothing to dw. ``out`` takes an existing
+    tensor for dw, such as the gradient that an optimizer was given.
+
+    The logits are computed again, in pieces of the vocabulary whose gradient G is held, rounded: up to 512 tokens (or 2^29 of T d V) to twice
+    16 bits, which leaves out 2^-16 of an entry, else to float16 (2^-11) beside powers of two of its rows and of the columns of x and w, in
+    which entries below 2^-27 of a token's factor lose bits and those below 2^-38 are 0. Words that are so rare for all tokens are
+    computed again with powers of two of their own. include/skew_loss.h has the limits, and what the scratch holds: a piece of G is 512 MiB at
+    most, or 256 words where that is more; with 16-bit copies of the piece's words and of x, 8192 tokens of 50304 words of width 2048 take
+    647 MB, 4096 tokens 704."""
     import torch
     _no_autograd(x, w, lse, dloss, dlse, out)
     h = _head(x, w, targets, tied, scale)

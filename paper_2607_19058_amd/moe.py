@@ -371,7 +371,8 @@ def expert_matmul_grad(x, dy, plan, *, gather=False, out=None, stream=None):
     """The weights' gradient bf16 (E, n, m): each expert's sum of x's rows (one a place, or with ``gather`` one a
     token) times ``dy`` (T k, m), bf16 or float32; zero for an expert without rows. A float32 ``dy`` is taken as
     two bf16 numbers (2^-16 of a value is left out), in up to twice the time. ``out`` takes an existing
-    tensor, such as the gradient that an optimizer was given. ``x`` may be rows kept in 8 bits (`Kept8`)."""
+    tensor, such as the gradient that an optimizer was given. ``x`` may be rows kept in 8 bits (`Kept8`), which are restored into scratch:
+    2 bytes a value of each place's row (with a float32 ``dy`` of each kept row)."""
     import torch
     if isinstance(x, Kept8):
         from .kept import _matmul_grad_kept
