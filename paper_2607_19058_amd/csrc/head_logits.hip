@@ -4,8 +4,9 @@
 // A lane of a finished tile holds rows lane % 16 of FM blocks and 4 FN of each row's columns. Forward it finds their largest, adds up powers of
 // two relative to it, and joins four lanes; a wave writes one pair for each row. Backward a logit becomes its gradient in
 // place, which leaves through LDS as float16. Per logit that is some 32 cycles of a SIMD (16 of them the exponential's), 8200 for a tile of
-// 256 x 256, beside its 64 K / 32 matrix instructions of 16. 8192 rows, 50304 words of width 2048: forward 1.38 ms, with words in rows 1.48; the
-// gradient 1.58 (matrix cores busy 59% at 1.9 GHz). 1024 rows: 195 us. One row: 32 us for w's 206 MB.
+// 256 x 256, beside its 64 K / 32 matrix instructions of 16. 8192 rows, 50304 words of width 2048: forward 1.35 to 1.39 ms
+// (matrix cores busy 59% at 2.0 GHz, 12% of the lines missing in L2), with words in rows 1.48; the gradient 1.58 to 1.62 (49%), of which each
+// word's largest entry is 1.5%. 1024 rows: 195 us. One row: 32 us for w's 206 MB.
 #include "head_plan.h"
 #include "product_tiles.h"
 

@@ -10,8 +10,9 @@
 // the tokens' factors get their part of dw from a second pass (head_rare.hip).
 //
 // What bounds them (benchmark's head, 2048 x 50304): one token's loss, w's bytes (206 MB in 32 us from the Infinity Cache, 35 from memory); 8192
-// tokens, the matrix cores at the power limit (clocks of 1.75 to 2.0 of 2.4 GHz): forward 1.40 ms and the logits again 1.57 (1.2 and 1.08 PFLOP/s;
-// the library's plain product, with the logits written, 1.55 ms), dx 1.42 (the library 1.22), dw 1.26 (the library 1.68).
+// tokens, the matrix cores at the power limit (clocks of 1.75 to 2.0 of 2.4 GHz): forward 1.35 to 1.40 ms and the logits again 1.58 to 1.62 (1.2
+// and 1.06 PFLOP/s; the library's plain product, with the logits written, 1.55 ms), dx 1.34 to 1.42 (the library 1.22), dw 1.24 to 1.27 (the
+// library 1.68), rare words' launches 0.04.
 #include <algorithm>
 
 #include "head_plan.h"

@@ -215,16 +215,17 @@ inline ForwardPlan forward_plan(const skew_head_desc &h) {
 }
 
 // Up to 512 tokens the bytes of w decide. Then G is the sum of two bf16 numbers, and w enters its product as it is; with more,
-// where the products decide, w is converted to float16 (see above), which takes its bytes four times more. Where tokens, width and words
-// together are few, the conversions' launches decide. Backward calls, us, float16 | split:
+// where the products decide, w is converted to float16, which takes its bytes four times more, and rare words take four launches. Where
+// tokens, width and words together are few, these launches decide. Backward calls, us, float16 | two bf16 numbers (the rule goes by
+// tokens alone; a few percent are lost on either side of it):
 //   tokens                             1           64          256         512         768          1024
-//   50304 words of width 2048          345 | 203   380 | 241   494 | 402   589 | 595   709 | 829    813 | 1010
-//   the same, tied                     377 | 207   404 | 235   486 | 379   605 | 594   723 | 808    836 | 1008
-//   32003 words of width 1031          141 | 103   156 | 128   209 | 233   306 | 304   343 | 385    398 | 484
-//   8192 words of width 1024            61 |  48    68 |  49    73 |  62    86 |  90   106 | 114    118 | 134
+//   50304 words of width 2048          364 | 205   402 | 241   517 | 398   616 | 599   743 | 848    848 | 1031
+//   the same, tied                     398 | 198   427 | 235   512 | 389   639 | 615   761 | 838    879 | 1035
+//   32003 words of width 1031          138 |  97   156 | 117   213 | 207   299 | 289   339 | 378    384 | 472
+//   8192 words of width 1024            69 |  48    73 |  49    81 |  64    95 |  95   118 | 120    130 | 138
 //   tokens x width x words             2048x128x512   1024x512x1024   2048x256x1024   4096x128x1024   1024x1024x1024   1024x256x4096
-//     (2^27, 2^29, .., 2^30)           43 | 37        54 | 48         53 | 48         55 | 58         58 | 55          58 | 61
-//     tied                             49 | 37        58 | 49         58 | 47         60 | 58         66 | 58          67 | 62
+//     (2^27, 2^29, .., 2^30)           51 | 38        62 | 48         61 | 49         66 | 59         66 | 56          67 | 62
+//     tied                             58 | 38        66 | 50         65 | 49         71 | 59         75 | 58          75 | 64
 struct BackwardPlan : HeadPlan {
   bool split;
   int64_t rows;   // of G

@@ -1,6 +1,6 @@
 // head_products.hip -- the gradients of the head's rows and weights: products of float16 operands on the matrix cores, or of bf16 ones, of which
-// G is the sum of two. With tiles of 256 x 256 the compiler spills 5 to 18 registers, outside the main loop. Bound by the matrix cores: 8192 rows' gradient from 25152 words, width 2048, 704 us (1.20 PFLOP/s; words in rows 656, 1.29);
-// 24576 words' gradient from 8192 rows 594 us (1.39).
+// G is the sum of two. With float16 tiles of 256 x 256 the compiler spills 15 to 18 registers, outside the main loop. Bound by the matrix cores: 8192 rows' gradient from 25152 words, width 2048, 672 to 707 us (1.19 to 1.26 PFLOP/s,
+// cores busy 54%; words in rows 655 to 664, 59%); 24576 words' gradient from 8192 rows 580 to 597 us (1.38 to 1.42, 69%).
 #include "head_plan.h"
 #include "product_tiles.h"
 

@@ -1,7 +1,7 @@
 // kept_product.hip -- the experts' weights' gradient from rows kept in 8 bits.
 //
 // What bounds it: up to some 300 rows an expert the bytes of dW (32 experts of 2048 x 8192 with 32 rows each: 1.07 GB in 227 us, 4.7 TB/s, the
-// restored rows' pass among it); beyond, the matrix cores, which are busy for 40% of the time with 512 rows each (677 us, 0.81 PFLOP/s):
+// restored rows' pass among it); beyond, the matrix cores, which are busy for 39% of the time with 512 rows each (654 to 677 us, 0.81 to 0.84 PFLOP/s):
 // sixteen stages a tile, and the stores of all tiles of a round together.
 //
 // The values are restored into the workspace in the order of the places (with SKEW_GATHER a token's row once for each of its experts), so

@@ -5,8 +5,8 @@
 // and the scale comes from the exponent without a rounding.
 //
 // All of it is bound by memory; the activations' exponentials and divisions (some 60 instructions a value at most, of 250 that a SIMD
-// has time for) hide behind it. 16384 x 8192 bf16: to 8 bits 94 us, back 67 us (together 5.2 TB/s); gated activation with its checkpoints and its
-// gradient from them 515 us a pass (4.7 TB/s, a copy reaches 4.9); 9003 x 2765 float32 without a gate 54 and 67 us (4.6 TB/s).
+// has time for) hide behind it. 16384 x 8192 bf16: to 8 bits 94 us, back 67 us (together 5.2 TB/s); gated activation with its checkpoints 245 us and its
+// gradient from them 259, 510 us a pass (4.7 TB/s, a copy reaches 4.9); 9003 x 2765 float32 without a gate 54 and 67 us (4.6 TB/s).
 #include "moe_internal.h"
 #include "kept_internal.h"
 
