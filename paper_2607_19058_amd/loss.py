@@ -102,7 +102,7 @@ def head_loss_backward(x, w, targets, lse, dloss, *, dlse=None, tied=False, scal
 
     The logits are computed again, in pieces of the vocabulary whose gradient G is held, rounded: up to 512 tokens (or 2^29 of T d V) to twice
     16 bits, which leaves out 2^-16 of an entry, else to float16 (2^-11) beside powers of two of its rows and of the columns of x and w, in
-    which entries below 2^-27 of a token's factor lose bits and those below 2^-38 are 0. Words that are so rare for all tokens are
+    which entries below 2^-27 of a token's factor can lose bits and those below 2^-38 be 0. Words that are so rare for all tokens are
     computed again with powers of two of their own. include/skew_loss.h has the limits, and what the scratch holds: a piece of G is 512 MiB at
     most, or 256 words where that is more; with 16-bit copies of the piece's words and of x, 8192 tokens of 50304 words of width 2048 take
     647 MB, 4096 tokens 704."""
