@@ -62,7 +62,7 @@ int skew_head_loss_backward_bytes(const skew_head_desc *h, size_t *bytes);
 int skew_head_loss(const skew_head_desc *h, float *loss, float *lse, void *workspace, size_t workspace_bytes, void *stream);
 
 /* lse as skew_head_loss gave it. dx [tokens x d] in dx_dtype, stride lddx; dw bf16 in w's layout, stride lddw, every row of it
- * written. Errors: SKEW_EINVAL, SKEW_ENOSPACE, SKEW_EHIP. */
+ * written. Outputs share no memory with inputs, which are read after parts of the outputs are written. Errors: SKEW_EINVAL, SKEW_ENOSPACE, SKEW_EHIP. */
 int skew_head_loss_backward(const skew_head_desc *h, const float *lse, const float *dloss, const float *dlse, void *dx,
                             int32_t dx_dtype, int64_t lddx, void *dw, int64_t lddw, void *workspace,
                             size_t workspace_bytes, void *stream);

@@ -72,6 +72,21 @@ def _rows(t, what, T, device):
     _dense(t, what, (T,))
 
 
+def _apart(out, t, what):
+    """Refuses an output that shares memory with an input, which is read after parts of the output are written. (Columns of the same
+    rows, side by side, do not.)"""
+    if out.untyped_storage().data_ptr() != t.untyped_storage().data_ptr() or not out.numel() or not t.numel():
+        return
+    (a, la), (b, lb) = ((v.data_ptr(), v.element_size() * _ld(v, name)) for v, name in ((out, "out"), (t, what)))
+    ends = [p + (v.shape[0] - 1) * ld + v.shape[1] * v.element_size() for v, p, ld in ((out, a, la), (t, b, lb))]
+    if ends[0] <= b or ends[1] <= a:
+        return
+    row_a, row_b = (v.shape[1] * v.element_size() for v in (out, t))
+    if la == lb and row_a <= (b - a) % la <= la - row_b:
+        return
+    raise ValueError(f"out shares memory with {what}")
+
+
 def head_loss(x, w, targets, *, tied=False, scale=1.0, stream=None):
     """Softmax cross entropy of ``targets`` (int32 or int64 (T)) under the logits ``scale`` x w: (loss, lse), float32 (T).
 
@@ -98,7 +113,7 @@ def head_loss(x, w, targets, *, tied=False, scale=1.0, stream=None):
 def head_loss_backward(x, w, targets, lse, dloss, *, dlse=None, tied=False, scale=1.0, dtype=None, out=None, stream=None):
     """Gradients of `head_loss`: (dx (T, d) in bf16 or ``dtype``, dw bf16 in w's shape) from those of loss and (``dlse``) of lse,
     float32 (T), and the lse that it gave. A target outside [0, V) gives a row of zeros in dx and nothing to dw. ``out`` takes an existing
-    tensor for dw, such as the gradient that an optimizer was given.
+    tensor for dw, such as the gradient that an optimizer was given; it shares no memory with x or w.
 
     The logits are computed again, in pieces of the vocabulary whose gradient G is held, rounded: up to 512 tokens (or 2^29 of T d V) to twice
     16 bits, which leaves out 2^-16 of an entry, else to float16 (2^-11) beside powers of two of its rows and of the columns of x and w, in
@@ -120,6 +135,8 @@ def head_loss_backward(x, w, targets, lse, dloss, *, dlse=None, tied=False, scal
         _tensor(out, "out", (torch.bfloat16,), 2, dev)
         if out.shape != w.shape:
             raise ValueError(f"out must have shape {tuple(w.shape)}, not {tuple(out.shape)}")
+        for t, what in ((x, "x"), (w, "w")):
+            _apart(out, t, what)
     s, here = _on(dev, stream, x, w, targets, lse, dloss, dlse, out)
     with here:
         dx = torch.empty((T, h.d), dtype=dtype, device=dev)

@@ -31,3 +31,24 @@ def test_rows_that_are_no_token_are_zeros_whatever_w_holds(case, tied):
     loss, lse = P.head_loss(x, w, none, tied=tied)
     dx, dw = P.head_loss_backward(x, w, none, lse, dloss, dlse=dlse, tied=tied)
     assert not loss.any() and not lse.any() and not dx.any() and not dw.any()
+
+
+@pytest.mark.parametrize("tied", [False, True])
+def test_outputs_that_share_memory_with_inputs_are_refused(tied):
+    T, d, V = 40, 64, 100
+    x, w, targets, dloss, _ = inputs(T, d, V, tied=tied, none=0.0)
+    _, lse = P.head_loss(x, w, targets, tied=tied)
+    _, want = P.head_loss_backward(x, w, targets, lse, dloss, tied=tied)
+    n, m = w.shape
+    both = torch.zeros(n + 1, 2 * m, dtype=BF, device="cuda")
+    flat = torch.zeros(2 * n * m + T * d, dtype=BF, device="cuda")
+    wide, rows, shared = both[:n, :m], flat[:n * m].view(n, m), flat[:T * d].view(T, d)
+    for v, t in ((wide, w), (rows, w)):
+        v.copy_(t)
+    for out, xv, wv in ((wide, x, wide), (both[1:, :m], x, wide), (both[:n, 1:m + 1], x, wide), (both[:n, m - 1:2 * m - 1], x, wide), (rows, x, rows),
+                        (flat[n * m - 1:2 * n * m - 1].view(n, m), x, rows), (rows, shared, w)):
+        with pytest.raises(ValueError, match="shares memory"):
+            P.head_loss_backward(xv, wv, targets, lse, dloss, tied=tied, out=out)
+    for out, wv in ((both[:n, m:], wide), (flat[n * m:2 * n * m].view(n, m), rows)):   # beside it, and behind it
+        _, dw = P.head_loss_backward(x, wv, targets, lse, dloss, tied=tied, out=out)
+        assert dw is out and torch.equal(dw, want) and torch.equal(wv, w)
